@@ -368,6 +368,94 @@ int dedloc_accumulate(float *acc, const void *grad, int32_t grad_codec, uint64_t
 int dedloc_finalize(float *acc, uint64_t n, uint32_t count, int32_t codec, uint32_t block,
                     void *codes, float *scales, int32_t reset, void *stream);
 
+/* Element types of the operators below. */
+enum { DEDLOC_DTYPE_F32 = 0, DEDLOC_DTYPE_FP16 = 1, DEDLOC_DTYPE_BF16 = 2 };
+
+/* Orthogonalised updates (the Muon optimizer's): with X the matrix, or its
+ * transpose where it has more rows than columns,
+ *   X_0 = G / (||G||_F + eps);   steps times:
+ *   A = X X^T,  B = b A + c A^2,  X <- a X + B X
+ * which takes every singular value towards 1 by the same odd polynomial and
+ * leaves the singular vectors alone.  The usual coefficients are a = 3.4445,
+ * b = -4.7750, c = 2.0315 with 5 steps (host struct). */
+typedef struct {
+    float a, b, c, eps;
+    uint32_t steps; /* 1 to DEDLOC_ORTHO_MAX_STEPS */
+} dedloc_ortho_cfg;
+#define DEDLOC_ORTHO_MAX_STEPS 64
+/* Limits of a matrix: its shorter side, and its longer. */
+#define DEDLOC_ORTHO_MAX_SHORT 32768
+#define DEDLOC_ORTHO_MAX_LONG (1u << 26)
+
+/* One matrix (host struct): element (i, j) is in[i * ld_in + j], its result
+ * out[i * ld_out + j].  out may be in with ld_out = ld_in; otherwise no
+ * result may overlap any matrix.  rows == 0 or cols == 0: nothing to do. */
+typedef struct {
+    const void *in;
+    void *out;
+    uint64_t ld_in, ld_out; /* elements, at least cols */
+    uint32_t rows, cols;
+} dedloc_matrix;
+
+/* Orthogonalise n matrices of one dtype (a DEDLOC_DTYPE_*).  All of them
+ * take part in every launch, so that small ones fill the GPU together.
+ * The norm is summed in fp64.  Every factor of a product is held as a pair of
+ * fp16 numbers (22 bits) and the products are summed in fp32, so that an fp32
+ * result is as near to the formula as fp32 products make it; 16-bit results
+ * are rounded once, at the end.  The arithmetic takes |X|, |A| and |B| up to 15,
+ * 63 and 63: coefficients that leave that range give infinities or NaN.  A zero
+ * matrix gives zeros; one that holds an infinity or NaN gives NaN throughout.
+ * Results are the same bits for the same call, whatever the other matrices.
+ * ws: dedloc_orthogonalize_workspace_bytes (0 for invalid arguments; it looks
+ * at the sides and their limits only), 256-byte aligned, contents arbitrary.
+ * About 12 bytes an element and 8 a square of the shorter side; calls that
+ * share one workspace must not overlap in time.
+ * Errors: mats or cfg NULL, n == 0, an unknown dtype, steps out of range, a
+ * side above its limit, ld < cols, a NULL pointer of a non-empty matrix ->
+ * INVALID_ARG; a pointer not aligned to the element -> ALIGN; ws NULL or too
+ * small -> WORKSPACE, not 256-byte aligned -> ALIGN. */
+size_t dedloc_orthogonalize_workspace_bytes(const dedloc_matrix *mats, uint32_t n);
+int dedloc_orthogonalize(const dedloc_matrix *mats, uint32_t n, int32_t dtype,
+                         const dedloc_ortho_cfg *cfg, void *ws, size_t ws_bytes, void *stream);
+
+/* Muon hyper-parameters (host struct). */
+typedef struct {
+    float lr, momentum, weight_decay, rms;
+    int32_t nesterov;
+    dedloc_ortho_cfg ortho;
+} dedloc_muon_cfg;
+
+/* One Muon step over a flat parameter buffer of matrices: momentum, the
+ * update orthogonalised per matrix, decoupled weight decay:
+ *   m' = fma(mu, m, g);   u = fma(mu, m', g) with nesterov, else m'
+ *   o_t = u_t as rows[t] x cols[t], orthogonalised (dedloc_orthogonalize)
+ *   s_t = rms * sqrt(max(rows[t], cols[t])), or 1 if the tensor lacks
+ *         DEDLOC_TENSOR_ADAPT (rms = 0.2 gives the updates about the size of Adam's)
+ *   x' = fma(-(lr * s_t), o, (1 - lr * lambda_t) * x)
+ * lambda_t as for LAMB.
+ *   x, m        fp32[P], updated in place;
+ *   grad, grad_scales, grad_codec, offsets, flags: as for dedloc_lamb_step (the
+ *               gradient an fp32 vector or the gathered message);
+ *   rows, cols  host uint32[n_tensors], row-major; a tensor's length is rows *
+ *               cols rounded up to at most the next multiple of 8 (the rest, up
+ *               to 7 elements, is neither read nor written).  rows == 0 or cols
+ *               == 0: not a matrix, x and m of the tensor are left alone.
+ * A model's gains, biases and tables take LAMB: keep them behind the matrices
+ * in the flat vector and call both steps on their part of the same message
+ * (an int8 message splits at a multiple of its block).
+ * Non-finite gradients are not filtered: they make their matrix NaN.
+ * Errors: cfg NULL, P > 0 with x, m or grad NULL, offsets, rows, cols or flags
+ * NULL, n_tensors 0, offsets not tiling [0, P), a length that does not fit its
+ * sides, a side above its limit, steps out of range, an unknown codec, int8
+ * without aligned scales -> INVALID_ARG; an offset (other than P) not a
+ * multiple of 8, a buffer not 16-byte aligned -> ALIGN; ws as for
+ * dedloc_orthogonalize. */
+size_t dedloc_muon_workspace_bytes(const uint32_t *rows, const uint32_t *cols, uint32_t n_tensors);
+int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_scales, int32_t grad_codec,
+                     uint32_t block, uint64_t P, const uint64_t *offsets, const uint32_t *rows,
+                     const uint32_t *cols, const uint8_t *flags, uint32_t n_tensors,
+                     const dedloc_muon_cfg *cfg, void *ws, size_t ws_bytes, void *stream);
+
 /* Load balancer (Section 3.2, Appendix B): the relaxed linear program
  * (Eq. main_problem_appendix_relaxed) that maximises training steps per
  * second xi over the send rates a_ij (peer i -> reducer j), the return rates

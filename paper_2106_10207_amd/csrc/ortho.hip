@@ -1,0 +1,333 @@
+// gfx950 kernels of the orthogonalised update (Newton-Schulz steps) and the
+// Muon step built on it.
+//
+// With s the shorter side of a matrix and l the longer, X [s][l] is taken
+// towards the nearest matrix with orthogonal rows by
+//   X0 = G / (|G|_F + eps),   A = X X^T,   B = b A + c A^2,   X <- a X + B X,
+// three products a step on the matrix cores.  A singular value far below 1
+// grows by a (3.4) in a step, and a rounding error of X with it, so five
+// steps multiply it by up to a^5 = 485: operands of 11 bits (fp16) lose 1e-2 of
+// the result of an ill-conditioned gradient, 8 bits (bf16) 1e-1.  So every
+// operand is held in two fp16 planes, hi + lo, 22 bits, and a product takes
+// three of them,
+//   hi hi' + hi lo' + lo hi'
+// in fp32 accumulators.  X is stored times 2^12, A and B times 2^10: their entries
+// are at most about 1.3 and 3, and the low planes of entries of the usual
+// size (1 / sqrt(s l)) then stay in fp16's normal range.
+//
+// Layout of a two-plane matrix: 32 columns of a row are 128 bytes, 64 of hi then
+// 64 of lo, so 128 bytes of a row are what one step of a product's loop reads.
+// Both factors of every product have the summed index along their rows (A and
+// B are symmetric; X^T is kept beside X).
+#include "ops_internal.h"
+
+namespace dedloc {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+namespace {
+
+constexpr float kXScale = 4096.0f;  // of X
+constexpr float kAScale = 1024.0f;  // of A and B
+
+struct Sides {
+    uint32_t s, l, S, L;
+    bool tall;  // rows > cols: X is the transpose
+};
+__host__ __device__ inline Sides sides(const NsMat &m) {
+    Sides d;
+    d.tall = m.rows > m.cols;
+    d.s = d.tall ? m.cols : m.rows;
+    d.l = d.tall ? m.rows : m.cols;
+    d.S = (d.s + kNsPad - 1) / kNsPad * kNsPad;
+    d.L = (d.l + kNsPad - 1) / kNsPad * kNsPad;
+    return d;
+}
+
+// The parts of a matrix' region.
+__device__ inline char *at_x(const NsArgs &a, const NsMat &m) { return a.ws + m.base; }
+__device__ inline char *at_xt(const NsArgs &a, const NsMat &m, const Sides &d, int k) {
+    return a.ws + m.base + (uint64_t)(1 + k) * d.S * d.L * 4;
+}
+__device__ inline char *at_a(const NsArgs &a, const NsMat &m, const Sides &d) {
+    return a.ws + m.base + (uint64_t)3 * d.S * d.L * 4;
+}
+__device__ inline char *at_b(const NsArgs &a, const NsMat &m, const Sides &d) {
+    return at_a(a, m, d) + (uint64_t)d.S * d.S * 4;
+}
+// Byte offset of element (i, j) of a matrix of `width` columns: its hi; lo is 64 bytes on.
+__device__ inline uint64_t at_planes(uint32_t i, uint32_t j, uint32_t width) {
+    return ((uint64_t)i * width + (j & ~31u)) * 4 + (j & 31u) * 2;
+}
+
+__device__ inline void split(float v, _Float16 &hi, _Float16 &lo) {
+    hi = (_Float16)v;
+    lo = (_Float16)(v - (float)hi);
+}
+
+// The matrix that workgroup `wg` belongs to.
+__device__ inline uint32_t find(const NsTable &t, uint32_t wg) {
+    uint32_t k = 0;
+    while (k + 1 < t.n && t.m[k + 1].begin <= wg) k++;
+    return k;
+}
+
+// Entry `e` (flat, absolute) of an averaged gradient.
+template <int SRC>
+__device__ inline float grad_at(const NsArgs &a, uint64_t e) {
+    if (SRC == kNsMuonF32) return ((const float *)a.grad)[e];
+    if (SRC == kNsMuonFP16) return (float)((const _Float16 *)a.grad)[e];
+    return (float)((const int8_t *)a.grad)[e] * a.scales[e >> 10];
+}
+
+template <int SRC>
+__device__ inline float entry(const NsArgs &a, const NsMat &m, uint32_t row, uint32_t col) {
+    if (SRC >= kNsMuonF32) {
+        const uint64_t e = m.ld_in + (uint64_t)row * m.cols + col;
+        const float mom = a.mom[e];
+        return a.nesterov ? fmaf(a.mu, mom, grad_at<SRC>(a, e)) : mom;
+    }
+    const uint64_t e = (uint64_t)row * m.ld_in + col;
+    if (SRC == kNsF32) return ((const float *)m.in)[e];
+    if (SRC == kNsFP16) return (float)((const _Float16 *)m.in)[e];
+    return (float)((const __bf16 *)m.in)[e];
+}
+
+__device__ inline double block_sum(double v) {
+    __shared__ double red[4];
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = (red[0] + red[1]) + (red[2] + red[3]);
+    __syncthreads();
+    return v;
+}
+
+}  // namespace
+
+// Sums of squares in 64 bits, one per block of kNsTile rows and columns.
+template <int SRC>
+__global__ __launch_bounds__(256) void ns_sum_kernel(NsTable t, NsArgs a) {
+    const NsMat &m = t.m[find(t, blockIdx.x)];
+    const uint32_t k = blockIdx.x - m.begin, across = (m.cols + kNsTile - 1) / kNsTile;
+    const uint32_t r0 = k / across * kNsTile, col = k % across * kNsTile + threadIdx.x % kNsTile;
+    double sum = 0.0;
+    if (col < m.cols)
+        for (uint32_t r = r0 + threadIdx.x / kNsTile; r < r0 + kNsTile && r < m.rows; r += 256 / kNsTile) {
+            const double v = entry<SRC>(a, m, r, col);
+            sum = fma(v, v, sum);
+        }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) a.part[m.part + k] = sum;
+}
+
+// Muon: m' = fma(mu, m, g), and the sums of squares of the update, one per
+// kSumChunk elements.
+template <int SRC>
+__global__ __launch_bounds__(256) void muon_sum_kernel(NsTable t, NsArgs a) {
+    const NsMat &m = t.m[find(t, blockIdx.x)];
+    const uint32_t k = blockIdx.x - m.begin;
+    const uint64_t n = (uint64_t)m.rows * m.cols, end = (uint64_t)(k + 1) * kSumChunk < n ? (uint64_t)(k + 1) * kSumChunk : n;
+    double sum = 0.0;
+    for (uint64_t i = (uint64_t)k * kSumChunk + threadIdx.x; i < end; i += 256) {
+        const uint64_t e = m.ld_in + i;
+        const float g = grad_at<SRC>(a, e), mom = fmaf(a.mu, a.mom[e], g);
+        a.mom[e] = mom;
+        const double u = a.nesterov ? fmaf(a.mu, mom, g) : mom;
+        sum = fma(u, u, sum);
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) a.part[m.part + k] = sum;
+}
+
+// X0 and its transpose in two planes, zeros in the padding: one workgroup per
+// block of 64 x 64 of the matrix as it is stored.
+template <int SRC>
+__global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
+    const uint32_t q = find(t, blockIdx.x);
+    const NsMat &m = t.m[q];
+    const Sides d = sides(m);
+    double sum = 0.0;
+    const uint32_t end = q + 1 < t.n ? t.m[q + 1].part : t.parts;
+    for (uint32_t i = m.part + threadIdx.x; i < end; i += 256) sum += a.part[i];
+    sum = block_sum(sum);
+    const float scale = (float)((double)kXScale / (sqrt(sum) + (double)a.eps));
+    __shared__ float tile[64][65];
+    const uint32_t k = blockIdx.x - m.begin;
+    const uint32_t across = (d.tall ? d.S : d.L) / 64, r0 = k / across * 64, c0 = k % across * 64;
+    const uint32_t tc = threadIdx.x % 64;
+    for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
+        float v = 0.0f;
+        if (r0 + r < m.rows && c0 + tc < m.cols) v = entry<SRC>(a, m, r0 + r, c0 + tc) * scale;
+        tile[r][tc] = v;
+    }
+    __syncthreads();
+    // the block as stored goes to X (wide) or X^T (tall), its transpose to the other
+    char *straight = d.tall ? at_xt(a, m, d, 0) : at_x(a, m), *turned = d.tall ? at_x(a, m) : at_xt(a, m, d, 0);
+    const uint32_t w_straight = d.tall ? d.S : d.L, w_turned = d.tall ? d.L : d.S;
+    for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
+        _Float16 hi, lo;
+        split(tile[r][tc], hi, lo);
+        _Float16 *p = (_Float16 *)(straight + at_planes(r0 + r, c0 + tc, w_straight));
+        p[0] = hi;
+        p[32] = lo;
+        split(tile[tc][r], hi, lo);
+        p = (_Float16 *)(turned + at_planes(c0 + r, r0 + tc, w_turned));
+        p[0] = hi;
+        p[32] = lo;
+    }
+}
+
+// One tile of a product of a step.  OUT: the dtype of the result of the last
+// step's apply, or kNsMuonF32 for the update of the parameters.
+template <int PHASE, int OUT>
+__global__ __launch_bounds__(256) void ns_product_kernel(NsTable t, NsArgs a) {
+    constexpr uint32_t T = 64;
+    const NsMat &m = t.m[find(t, blockIdx.x)];
+    const Sides d = sides(m);
+    uint32_t k = blockIdx.x - m.begin, ti, tj;
+    if (PHASE == kNsApply) {
+        const uint32_t across = d.L / T;
+        ti = k / across;
+        tj = k % across;
+    } else {  // the lower triangle of a symmetric result
+        ti = (uint32_t)((sqrtf(8.0f * k + 1.0f) - 1.0f) * 0.5f);
+        while ((ti + 1) * (ti + 2) / 2 <= k) ti++;
+        while (ti * (ti + 1) / 2 > k) ti--;
+        tj = k - ti * (ti + 1) / 2;
+    }
+    const uint32_t K = PHASE == kNsGram ? d.L : d.S;  // the summed index
+    const char *left = PHASE == kNsGram ? at_x(a, m) : PHASE == kNsSquare ? at_a(a, m, d) : at_b(a, m, d);
+    const char *right = PHASE == kNsApply ? at_xt(a, m, d, a.turn) : left;
+    left += (uint64_t)ti * T * K * 4;
+    right += (uint64_t)tj * T * K * 4;
+
+    __shared__ __align__(16) char lds[2][T * 128];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / 2 * 32, wj = wave % 2 * 32;
+    f32x16 acc = {};
+    for (uint32_t kb = 0; kb < K; kb += 32) {
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < T * 8; c += 256) {
+            const uint32_t row = c / 8, ch = c % 8;
+            const uint64_t from = (uint64_t)row * K * 4 + (uint64_t)kb * 4 + ch * 16;
+            const uint32_t to = row * 128 + ((ch ^ (row & 7)) * 16);
+            *(u32x4 *)(lds[0] + to) = *(const u32x4 *)(left + from);
+            *(u32x4 *)(lds[1] + to) = *(const u32x4 *)(right + from);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t ks = 0; ks < 2; ks++) {
+            const uint32_t ri = wi + lane % 32, rj = wj + lane % 32, ch = ks * 2 + lane / 32;
+            const f16x8 ih = *(const f16x8 *)(lds[0] + ri * 128 + ((ch ^ (ri & 7)) * 16));
+            const f16x8 il = *(const f16x8 *)(lds[0] + ri * 128 + (((ch + 4) ^ (ri & 7)) * 16));
+            const f16x8 jh = *(const f16x8 *)(lds[1] + rj * 128 + ((ch ^ (rj & 7)) * 16));
+            const f16x8 jl = *(const f16x8 *)(lds[1] + rj * 128 + (((ch + 4) ^ (rj & 7)) * 16));
+            // the right factor's rows first: a lane then holds four consecutive columns of one row
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jh, il, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jl, ih, acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jh, ih, acc, 0, 0, 0);
+        }
+    }
+
+    const uint32_t i = ti * T + wi + lane % 32;
+#pragma unroll
+    for (uint32_t g = 0; g < 4; g++) {
+        const uint32_t j = tj * T + wj + 8 * g + 4 * (lane / 32);
+        float v[4];
+        f16x4 hi, lo;
+        if (PHASE == kNsGram) {
+            for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (kAScale / (kXScale * kXScale));
+        } else {
+            const char *old = (PHASE == kNsSquare ? at_a(a, m, d) : at_x(a, m)) + at_planes(i, j, PHASE == kNsSquare ? d.S : d.L);
+            hi = *(const f16x4 *)old;
+            lo = *(const f16x4 *)(old + 64);
+            for (int e = 0; e < 4; e++) {
+                const float o = (float)hi[e] + (float)lo[e];
+                v[e] = PHASE == kNsSquare ? fmaf(a.b, o, a.c * (acc[4 * g + e] * (1.0f / kAScale)))
+                                          : fmaf(a.a, o, acc[4 * g + e] * (1.0f / kAScale));
+            }
+        }
+        if (PHASE == kNsApply && a.last) {
+            for (int e = 0; e < 4; e++) {
+                if (i >= d.s || j + e >= d.l) continue;
+                const uint32_t row = d.tall ? j + e : i, col = d.tall ? i : j + e;
+                const float o = v[e] * (1.0f / kXScale);
+                if (OUT == kNsMuonF32) {
+                    float *x = a.x + m.ld_in + (uint64_t)row * m.cols + col;
+                    *x = fmaf(-m.unit, o, ((m.flags & 1) ? a.keep : 1.0f) * *x);
+                } else {
+                    const uint64_t at = (uint64_t)row * m.ld_out + col;
+                    if (OUT == kNsF32) ((float *)m.out)[at] = o;
+                    if (OUT == kNsFP16) ((_Float16 *)m.out)[at] = (_Float16)o;
+                    if (OUT == kNsBF16) ((__bf16 *)m.out)[at] = (__bf16)o;
+                }
+            }
+            continue;
+        }
+        for (int e = 0; e < 4; e++) {
+            _Float16 h, w;
+            split(v[e], h, w);
+            hi[e] = h;
+            lo[e] = w;
+        }
+        char *to = (PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_x(a, m)) +
+                   at_planes(i, j, PHASE == kNsApply ? d.L : d.S);
+        *(f16x4 *)to = hi;
+        *(f16x4 *)(to + 64) = lo;
+        if (PHASE == kNsApply || ti != tj) {  // X^T, or the upper triangle
+            char *base = PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_xt(a, m, d, 1 - a.turn);
+            for (int e = 0; e < 4; e++) {
+                _Float16 *p = (_Float16 *)(base + at_planes(j + e, i, d.S));
+                p[0] = hi[e];
+                p[32] = lo[e];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- launchers
+
+hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    switch (src) {
+        case kNsF32: ns_sum_kernel<kNsF32><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsFP16: ns_sum_kernel<kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsBF16: ns_sum_kernel<kNsBF16><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsMuonF32: muon_sum_kernel<kNsMuonF32><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsMuonFP16: muon_sum_kernel<kNsMuonFP16><<<groups, 256, 0, s>>>(t, a); break;
+        default: muon_sum_kernel<kNsMuonI8><<<groups, 256, 0, s>>>(t, a); break;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    switch (src) {
+        case kNsF32: ns_prepare_kernel<kNsF32><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsFP16: ns_prepare_kernel<kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsBF16: ns_prepare_kernel<kNsBF16><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsMuonF32: ns_prepare_kernel<kNsMuonF32><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsMuonFP16: ns_prepare_kernel<kNsMuonFP16><<<groups, 256, 0, s>>>(t, a); break;
+        default: ns_prepare_kernel<kNsMuonI8><<<groups, 256, 0, s>>>(t, a); break;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_ns_product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    if (phase == kNsGram) {
+        ns_product_kernel<kNsGram, kNsF32><<<groups, 256, 0, s>>>(t, a);
+    } else if (phase == kNsSquare) {
+        ns_product_kernel<kNsSquare, kNsF32><<<groups, 256, 0, s>>>(t, a);
+    } else {
+        switch (out) {
+            case kNsF32: ns_product_kernel<kNsApply, kNsF32><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16><<<groups, 256, 0, s>>>(t, a); break;
+            default: ns_product_kernel<kNsApply, kNsMuonF32><<<groups, 256, 0, s>>>(t, a); break;
+        }
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dedloc

@@ -73,6 +73,34 @@ def lars_cfg(lr=4.8, momentum=0.9, trust_coef=1e-3, weight_decay=1e-6,
     return dedloc_lars_cfg(lr, momentum, trust_coef, weight_decay, int(force_unit_trust))
 
 
+DEDLOC_DTYPE_F32 = 0
+DEDLOC_DTYPE_FP16 = 1
+DEDLOC_DTYPE_BF16 = 2
+
+
+class dedloc_ortho_cfg(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("eps", ctypes.c_float), ("steps", ctypes.c_uint32)]
+
+
+def ortho_cfg(a=3.4445, b=-4.7750, c=2.0315, eps=1e-7, steps=5) -> dedloc_ortho_cfg:
+    return dedloc_ortho_cfg(a, b, c, eps, steps)
+
+
+class dedloc_matrix(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("ld_in", ctypes.c_uint64),
+                ("ld_out", ctypes.c_uint64), ("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32)]
+
+
+class dedloc_muon_cfg(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("rms", ctypes.c_float), ("nesterov", ctypes.c_int32), ("ortho", dedloc_ortho_cfg)]
+
+
+def muon_cfg(lr=1e-3, momentum=0.95, weight_decay=0.01, rms=0.2, nesterov=True, ortho=None) -> dedloc_muon_cfg:
+    return dedloc_muon_cfg(lr, momentum, weight_decay, rms, int(nesterov), ortho if ortho is not None else ortho_cfg())
+
+
 class dedloc_local_peer(ctypes.Structure):
     _fields_ = [("index", ctypes.c_uint32), ("grad", ctypes.c_void_p)]
 
@@ -135,6 +163,14 @@ _SIGS = {
                            ctypes.c_void_p], ctypes.c_int),
     "dedloc_finalize": ([ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32, ctypes.c_uint32,
                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_orthogonalize_workspace_bytes": ([ctypes.c_void_p, ctypes.c_uint32], ctypes.c_size_t),
+    "dedloc_orthogonalize": ([ctypes.c_void_p, ctypes.c_uint32, ctypes.c_int32, ctypes.POINTER(dedloc_ortho_cfg),
+                              ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_muon_workspace_bytes": ([ctypes.c_void_p, ctypes.c_void_p, ctypes.c_uint32], ctypes.c_size_t),
+    "dedloc_muon_step": ([ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                          ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                          ctypes.c_void_p, ctypes.c_uint32, ctypes.POINTER(dedloc_muon_cfg), ctypes.c_void_p,
+                          ctypes.c_size_t, ctypes.c_void_p], ctypes.c_int),
     "dedloc_balance": ([ctypes.POINTER(dedloc_balance_problem), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
     "dedloc_group_size": ([ctypes.c_uint32, ctypes.c_double, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p],
@@ -610,6 +646,123 @@ def dedloc_finalize(acc, count: int, codec: int, block: int = DEDLOC_I8_BLOCK, c
                                   _dev(scales, _scale_bytes(codec, n, block), "scales"), int(reset),
                                   _stream(stream)))
     return codes, scales
+
+
+# --------------------------------------------- operators of the model's own step
+
+@functools.lru_cache(maxsize=None)
+def _dtypes():
+    import torch
+    return {torch.float32: DEDLOC_DTYPE_F32, torch.float16: DEDLOC_DTYPE_FP16, torch.bfloat16: DEDLOC_DTYPE_BF16}
+
+
+def _dtype(t, name: str) -> int:
+    try:
+        return _dtypes()[t.dtype]
+    except KeyError:
+        raise ValueError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}") from None
+
+
+def _rows(t, name: str):
+    """(address, row stride in elements) of a 2-D device tensor whose rows are
+    contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a device tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got {t.dim()} dimensions")
+    r, c = t.shape
+    if c > 1 and t.stride(1) != 1 or r > 1 and t.stride(0) < c:
+        raise ValueError(f"{name}: expected contiguous rows that do not overlap")
+    return t.data_ptr(), (t.stride(0) if r > 1 else max(c, 1))
+
+
+class OrthogonalizeCall:
+    """Pre-marshalled arguments of one dedloc_orthogonalize call: `mats` and
+    `out` are lists of 2-D tensors of one dtype with contiguous rows at any
+    stride (out None: in place).  Every call orthogonalises what `mats` then
+    hold."""
+
+    def __init__(self, mats: Sequence, out: Optional[Sequence] = None, cfg: Optional[dedloc_ortho_cfg] = None, ws=None):
+        import torch
+        out = mats if out is None else out
+        if not mats or len(out) != len(mats):
+            raise ValueError("mats and out must list the same number of matrices, at least one")
+        self.cfg = cfg if cfg is not None else ortho_cfg()
+        self.dtype = _dtype(mats[0], "mats[0]")
+        self.mats = (dedloc_matrix * len(mats))()
+        for k, (g, o) in enumerate(zip(mats, out)):
+            if g.dtype is not mats[0].dtype or o.dtype is not mats[0].dtype:
+                raise ValueError(f"matrix {k}: expected {mats[0].dtype}, got {g.dtype} and {o.dtype}")
+            if g.shape != o.shape:
+                raise ValueError(f"matrix {k}: {tuple(g.shape)} in, {tuple(o.shape)} out")
+            (gp, gl), (op, ol) = _rows(g, f"mats[{k}]"), _rows(o, f"out[{k}]")
+            self.mats[k] = dedloc_matrix(gp, op, gl, ol, *g.shape)
+        need = load().dedloc_orthogonalize_workspace_bytes(self.mats, len(mats))
+        if need == 0:
+            raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
+        self.ws = torch.empty(need, dtype=torch.uint8, device=mats[0].device) if ws is None else ws
+        self._ws = _dev(self.ws, name="ws")
+        self._ws_bytes = _nbytes(self.ws)
+        self._keep = (list(mats), list(out))
+        self._cfg = ctypes.byref(self.cfg)
+
+    def __call__(self, stream=None):
+        _check(load().dedloc_orthogonalize(self.mats, len(self.mats), self.dtype, self._cfg, self._ws, self._ws_bytes,
+                                           _stream(stream)))
+        return self._keep[1]
+
+
+def dedloc_orthogonalize(mats: Sequence, out: Optional[Sequence] = None, cfg: Optional[dedloc_ortho_cfg] = None,
+                         ws=None, stream=None) -> list:
+    """Orthogonalise a list of matrices (out None: into new tensors); returns
+    the results."""
+    import torch
+    if out is None:
+        out = [torch.empty(m.shape, dtype=m.dtype, device=m.device) for m in mats]
+    return OrthogonalizeCall(mats, out, cfg, ws)(stream)
+
+
+def make_muon_workspace(shapes, device="cuda"):
+    """A workspace for dedloc_muon_step over tensors of these (rows, cols)."""
+    import torch
+    r, c = (_host([s[k] for s in shapes], np.uint32) for k in (0, 1))
+    need = load().dedloc_muon_workspace_bytes(_ptr(r), _ptr(c), len(r))
+    if need == 0:
+        raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+class MuonCall:
+    """Pre-marshalled arguments of one dedloc_muon_step call.  shapes: (rows,
+    cols) per tensor, (0, 0) for one that is not a matrix and is left alone."""
+
+    def __init__(self, x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, grad_codec: int = DEDLOC_CODEC_F32,
+                 grad_scales=None, block: int = DEDLOC_I8_BLOCK, ws=None):
+        P = x.numel()
+        self.off = _host(offsets, np.uint64)
+        self.rows, self.cols = (_host([s[k] for s in shapes], np.uint32) for k in (0, 1))
+        self.fl = _host(flags, np.uint8)
+        if not len(self.off) - 1 == len(self.rows) == len(self.fl):
+            raise ValueError("offsets, shapes and flags describe different numbers of tensors")
+        self.cfg = cfg
+        self.ws = make_muon_workspace(shapes, x.device) if ws is None else ws
+        self._keep = (x, m, grad, grad_scales)
+        self.args = (_dev(x, 4 * P, "x", f32=True), _dev(m, 4 * P, "m", f32=True),
+                     _dev(grad, _code_bytes(grad_codec, P), "grad"),
+                     _dev(grad_scales, _scale_bytes(grad_codec, P, block), "grad_scales"), grad_codec, block, P)
+        self._ws = (_dev(self.ws, name="ws"), _nbytes(self.ws))
+
+    def __call__(self, stream=None):
+        _check(load().dedloc_muon_step(*self.args, _ptr(self.off), _ptr(self.rows), _ptr(self.cols), _ptr(self.fl),
+                                       len(self.fl), ctypes.byref(self.cfg), *self._ws, _stream(stream)))
+
+
+def dedloc_muon_step(x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, grad_codec: int = DEDLOC_CODEC_F32,
+                     grad_scales=None, block: int = DEDLOC_I8_BLOCK, ws=None, stream=None):
+    """One Muon step over the matrices of a flat vector; returns the workspace."""
+    call = MuonCall(x, m, grad, offsets, shapes, flags, cfg, grad_codec, grad_scales, block, ws)
+    call(stream)
+    return call.ws
 
 
 def dedloc_balance(s, d, u, B: float, P: float, t=None, can_aggregate=None, c_fixed=None):
