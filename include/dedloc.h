@@ -456,6 +456,40 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
                      const uint32_t *cols, const uint8_t *flags, uint32_t n_tensors,
                      const dedloc_muon_cfg *cfg, void *ws, size_t ws_bytes, void *stream);
 
+/* Embedding lookup with scaling:
+ *   out[i][c] = scale * table[ids[i]][c]   for 0 <= ids[i] < vocab
+ * computed in fp32 and rounded once.  An id outside the table (a masked
+ * position) names no row: it gives a row of zeros and has no gradient.
+ *   table  device, vocab rows of `width` elements of table_dtype (a
+ *          DEDLOC_DTYPE_*), ld_table >= width elements apart;
+ *   ids    device, n integers of id_bytes (4 or 8), signed;
+ *   out    device, n rows of out_dtype, ld_out elements apart, not overlapping
+ *          the table.
+ * n, vocab and width may be 0; n and vocab at most 2^30, width at most 2^20.
+ * Errors: a size above its limit, an unknown dtype, id_bytes other than 4 or
+ * 8, a NULL pointer to something that is not empty, a row stride less than
+ * the width -> INVALID_ARG; a pointer not aligned to its elements -> ALIGN. */
+int dedloc_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_t width,
+                 uint64_t ld_table, const void *ids, int32_t id_bytes, uint64_t n, float scale,
+                 void *out, int32_t out_dtype, uint64_t ld_out, void *stream);
+
+/* The lookup's gradient, added into a peer's accumulator like a micro-batch's
+ * gradients by dedloc_accumulate (grad: the table's part of it):
+ *   grad[v][c] = fma(scale * batch_samples, sum over i with ids[i] = v of
+ *                dy[i][c], grad[v][c])
+ * for every token v that ids hold; rows of other tokens are neither read nor
+ * written.  The sum is taken in fp32 in an order fixed by the ids (the positions of
+ * a token ascending, in groups), so equal calls give equal bits.
+ *   grad  device fp32, ld_grad >= width apart; dy: n rows of dy_dtype;
+ *   ws    dedloc_embed_workspace_bytes (0 for invalid sizes), 256-byte aligned,
+ *         contents arbitrary; calls that share it must not overlap in time.
+ * Errors as for dedloc_embed; ws NULL or too small -> WORKSPACE, not 256-byte
+ * aligned -> ALIGN. */
+size_t dedloc_embed_workspace_bytes(uint64_t n, uint64_t vocab, uint32_t width);
+int dedloc_embed_grad(float *grad, uint64_t vocab, uint32_t width, uint64_t ld_grad, const void *ids,
+                      int32_t id_bytes, uint64_t n, const void *dy, int32_t dy_dtype, uint64_t ld_dy,
+                      float scale, float batch_samples, void *ws, size_t ws_bytes, void *stream);
+
 /* Load balancer (Section 3.2, Appendix B): the relaxed linear program
  * (Eq. main_problem_appendix_relaxed) that maximises training steps per
  * second xi over the send rates a_ij (peer i -> reducer j), the return rates

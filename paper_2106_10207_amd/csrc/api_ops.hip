@@ -128,6 +128,55 @@ size_t batches_bytes(bool muon, uint32_t n, F sides) {
     return most;
 }
 
+// ------------------------------------------------ embedding and its gradient
+
+struct EmbedWs {
+    size_t pairs, counts, total;
+    uint32_t chunk;
+};
+EmbedWs embed_ws(uint64_t n, uint32_t width) {
+    EmbedWs w;
+    w.pairs = round_up((size_t)n * sizeof(uint2), 256);
+    const uint32_t tiles = std::max(1u, blocks(n, kSortTile));
+    w.chunk = (tiles + kSortChunks - 1) / kSortChunks * kSortTile;
+    w.counts = (size_t)blocks(n, w.chunk) * 256 * sizeof(uint32_t);
+    w.total = 2 * w.pairs + w.counts + round_up((size_t)blocks(n, kRunChunk) * 2 * width * sizeof(float), 256);
+    w.total = std::max(w.total, (size_t)256);
+    return w;
+}
+
+int check_embed_sizes(uint64_t n, uint64_t vocab, uint32_t width) {
+    if (n > kEmbedMaxTokens) return fail(DEDLOC_ERR_INVALID_ARG, "n must be at most 2^30 (got %llu)", (unsigned long long)n);
+    if (vocab > kEmbedMaxVocab) return fail(DEDLOC_ERR_INVALID_ARG, "vocab must be at most 2^30 (got %llu)", (unsigned long long)vocab);
+    if (width > kEmbedMaxWidth) return fail(DEDLOC_ERR_INVALID_ARG, "width must be at most 2^20 (got %u)", width);
+    return DEDLOC_OK;
+}
+
+int check_rows(const void *p, int32_t dtype, uint64_t rows, uint32_t width, uint64_t ld, const char *name) {
+    if (dtype != DEDLOC_DTYPE_F32 && dtype != DEDLOC_DTYPE_FP16 && dtype != DEDLOC_DTYPE_BF16)
+        return fail(DEDLOC_ERR_INVALID_ARG, "%s: unknown dtype %d", name, dtype);
+    if (rows == 0 || width == 0) return DEDLOC_OK;
+    if (!p) return fail(DEDLOC_ERR_INVALID_ARG, "%s must not be NULL", name);
+    if (!aligned(p, dtype == DEDLOC_DTYPE_F32 ? 4 : 2)) return fail(DEDLOC_ERR_ALIGN, "%s must be aligned to its elements", name);
+    if (ld < width) return fail(DEDLOC_ERR_INVALID_ARG, "%s: a row stride is less than the width", name);
+    return DEDLOC_OK;
+}
+
+int check_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_t width, uint64_t ld_table, const void *ids,
+                int32_t id_bytes, uint64_t n, const void *rows, int32_t rows_dtype, uint64_t ld_rows,
+                const char *table_name, const char *rows_name) {
+    int rc = check_embed_sizes(n, vocab, width);
+    if (rc) return rc;
+    if (id_bytes != 4 && id_bytes != 8) return fail(DEDLOC_ERR_INVALID_ARG, "id_bytes must be 4 or 8 (got %d)", id_bytes);
+    rc = check_rows(table, table_dtype, n ? vocab : 0, width, ld_table, table_name);
+    if (rc) return rc;
+    rc = check_rows(rows, rows_dtype, n, width, ld_rows, rows_name);
+    if (rc) return rc;
+    if (n && width && !ids) return fail(DEDLOC_ERR_INVALID_ARG, "ids must not be NULL");
+    if (!aligned(ids, (size_t)id_bytes)) return fail(DEDLOC_ERR_ALIGN, "ids must be aligned to their elements");
+    return DEDLOC_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -262,6 +311,52 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
         b.add(q);
     }
     return run_batch(b, src, kNsMuonF32, cfg->ortho, a, ws, (hipStream_t)stream);
+}
+
+int dedloc_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_t width, uint64_t ld_table,
+                 const void *ids, int32_t id_bytes, uint64_t n, float scale, void *out, int32_t out_dtype,
+                 uint64_t ld_out, void *stream) {
+    int rc = check_embed(table, table_dtype, vocab, width, ld_table, ids, id_bytes, n, out, out_dtype, ld_out, "table", "out");
+    if (rc) return rc;
+    if (n == 0 || width == 0) return DEDLOC_OK;
+    const EmbedArgs a = {table, ld_table, ids, out, ld_out, (uint32_t)vocab, width, (uint32_t)n, id_bytes == 8, scale};
+    hipStream_t s = (hipStream_t)stream;
+    const hipError_t e = timed(K_EMBED, s, [&] { return launch_embed(table_dtype, out_dtype, a, s); });
+    return e == hipSuccess ? DEDLOC_OK : hip_fail(e, "embed launch");
+}
+
+size_t dedloc_embed_workspace_bytes(uint64_t n, uint64_t vocab, uint32_t width) {
+    if (check_embed_sizes(n, vocab, width)) return 0;
+    return embed_ws(n, width).total;
+}
+
+int dedloc_embed_grad(float *grad, uint64_t vocab, uint32_t width, uint64_t ld_grad, const void *ids, int32_t id_bytes,
+                      uint64_t n, const void *dy, int32_t dy_dtype, uint64_t ld_dy, float scale, float batch_samples,
+                      void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_embed(grad, DEDLOC_DTYPE_F32, vocab, width, ld_grad, ids, id_bytes, n, dy, dy_dtype, ld_dy, "grad", "dy");
+    if (rc) return rc;
+    if (n == 0 || width == 0 || vocab == 0) return DEDLOC_OK;
+    const EmbedWs w = embed_ws(n, width);
+    rc = check_ws(ws, ws_bytes, w.total);
+    if (rc) return rc;
+    char *b = (char *)ws;
+    const EmbedGradArgs a = {grad, ld_grad, ids, dy, ld_dy, (uint32_t)vocab, width, (uint32_t)n, id_bytes == 8,
+                             scale * batch_samples, w.chunk, {(uint2 *)b, (uint2 *)(b + w.pairs)}, (uint32_t *)(b + 2 * w.pairs),
+                             (float *)(b + 2 * w.pairs + w.counts)};
+    hipStream_t s = (hipStream_t)stream;
+    int from = -1;
+    // digits of the tokens and of `vocab`, which stands for a masked position
+    for (uint32_t shift = 0; shift == 0 || vocab >> shift; shift += 8) {
+        hipError_t e = timed(K_EMBED_COUNT, s, [&] { return launch_embed_count(a, from, shift, s); });
+        if (e != hipSuccess) return hip_fail(e, "embed count launch");
+        e = timed(K_EMBED_SCATTER, s, [&] { return launch_embed_scatter(a, from, shift, s); });
+        if (e != hipSuccess) return hip_fail(e, "embed scatter launch");
+        from = from < 0 ? 0 : 1 - from;
+    }
+    hipError_t e = timed(K_EMBED_SUM, s, [&] { return launch_embed_sum(dy_dtype, a, from, s); });
+    if (e != hipSuccess) return hip_fail(e, "embed sum launch");
+    e = timed(K_EMBED_JOIN, s, [&] { return launch_embed_join(a, from, s); });
+    return e == hipSuccess ? DEDLOC_OK : hip_fail(e, "embed join launch");
 }
 
 }  // extern "C"

@@ -65,4 +65,49 @@ hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t gr
 hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
 hipError_t launch_ns_product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
 
+// ------------------------------------------------ embedding and its gradient
+
+constexpr uint32_t kEmbedMaxTokens = 1u << 30;
+constexpr uint32_t kEmbedMaxVocab = 1u << 30;
+constexpr uint32_t kEmbedMaxWidth = 1u << 20;
+// Positions are sorted in at most kSortChunks chunks of whole tiles, one
+// workgroup each: every workgroup reads the digit counts of all chunks.
+constexpr uint32_t kSortTile = 2048;
+constexpr uint32_t kSortChunks = 512;
+constexpr uint32_t kRunChunk = 32;     // sorted positions summed by one row of threads
+
+struct EmbedArgs {
+    const void *table;
+    uint64_t ld_table;
+    const void *ids;
+    void *out;
+    uint64_t ld_out;
+    uint32_t vocab, width, n;
+    int32_t wide_ids;  // 64-bit ids
+    float scale;
+};
+
+struct EmbedGradArgs {
+    float *grad;
+    uint64_t ld_grad;
+    const void *ids;
+    const void *dy;
+    uint64_t ld_dy;
+    uint32_t vocab, width, n;
+    int32_t wide_ids;
+    float factor;    // scale * batch_samples
+    uint32_t chunk;  // positions of a chunk of the sort
+    // workspace: (token, position) pairs sorted in turn between two buffers,
+    // digit counts per chunk, and the sums of runs cut by a chunk's edge
+    uint2 *pairs[2];
+    uint32_t *counts;
+    float *cut;  // [chunks][2][width]
+};
+
+hipError_t launch_embed(int table, int out, const EmbedArgs &a, hipStream_t s);
+hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
+hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
+hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStream_t s);
+hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s);
+
 }  // namespace dedloc

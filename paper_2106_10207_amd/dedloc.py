@@ -171,6 +171,14 @@ _SIGS = {
                           ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                           ctypes.c_void_p, ctypes.c_uint32, ctypes.POINTER(dedloc_muon_cfg), ctypes.c_void_p,
                           ctypes.c_size_t, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_embed": ([ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint64,
+                      ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float, ctypes.c_void_p,
+                      ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_embed_workspace_bytes": ([ctypes.c_uint64, ctypes.c_uint64, ctypes.c_uint32], ctypes.c_size_t),
+    "dedloc_embed_grad": ([ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_void_p,
+                           ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64,
+                           ctypes.c_float, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+                          ctypes.c_int),
     "dedloc_balance": ([ctypes.POINTER(dedloc_balance_problem), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
     "dedloc_group_size": ([ctypes.c_uint32, ctypes.c_double, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p],
@@ -763,6 +771,56 @@ def dedloc_muon_step(x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, g
     call = MuonCall(x, m, grad, offsets, shapes, flags, cfg, grad_codec, grad_scales, block, ws)
     call(stream)
     return call.ws
+
+
+def _ids(ids):
+    """(address, bytes of an id, count) of a tensor of int32 or int64 ids of any shape."""
+    size = ids.element_size()
+    if ids.is_floating_point() or size not in (4, 8):
+        raise ValueError(f"ids: expected int32 or int64, got {ids.dtype}")
+    return _dev(ids, name="ids"), size, ids.numel()
+
+
+def dedloc_embed(table, ids, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+    """scale * table[ids], rows of zeros where an id names no row; `out` has a
+    row per id (ids.numel() of them) at any stride."""
+    import torch
+    p, size, n = _ids(ids)
+    tp, tl = _rows(table, "table")
+    if out is None:
+        out = torch.empty(n, table.shape[1], dtype=out_dtype or table.dtype, device=table.device)
+    op, ol = _rows(out, "out")
+    if tuple(out.shape) != (n, table.shape[1]):
+        raise ValueError(f"out: expected {n} rows of {table.shape[1]}, got {tuple(out.shape)}")
+    _check(load().dedloc_embed(tp, _dtype(table, "table"), table.shape[0], table.shape[1], tl, p, size, n, scale, op,
+                               _dtype(out, "out"), ol, _stream(stream)))
+    return out
+
+
+def make_embed_workspace(n: int, vocab: int, width: int, device="cuda"):
+    """A workspace for dedloc_embed_grad of up to n ids."""
+    import torch
+    need = load().dedloc_embed_workspace_bytes(n, vocab, width)
+    if need == 0:
+        raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def dedloc_embed_grad(grad, ids, dy, scale: float = 1.0, batch_samples: float = 1.0, ws=None, stream=None):
+    """grad[ids[i]] += scale * batch_samples * dy[i] for every id that names a
+    row of the fp32 accumulator `grad`; returns it."""
+    p, size, n = _ids(ids)
+    gp, gl = _rows(grad, "grad")
+    dp, dl = _rows(dy, "dy")
+    if grad.dtype is not _float32():
+        raise ValueError(f"grad: expected float32, got {grad.dtype}")
+    if tuple(dy.shape) != (n, grad.shape[1]):
+        raise ValueError(f"dy: expected {n} rows of {grad.shape[1]}, got {tuple(dy.shape)}")
+    if ws is None:
+        ws = make_embed_workspace(n, *grad.shape, grad.device)
+    _check(load().dedloc_embed_grad(gp, *grad.shape, gl, p, size, n, dp, _dtype(dy, "dy"), dl, scale, batch_samples,
+                                    _dev(ws, name="ws"), _nbytes(ws), _stream(stream)))
+    return grad
 
 
 def dedloc_balance(s, d, u, B: float, P: float, t=None, can_aggregate=None, c_fixed=None):
