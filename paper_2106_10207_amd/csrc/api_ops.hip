@@ -17,6 +17,11 @@ static_assert(kNsMaxShort == DEDLOC_ORTHO_MAX_SHORT && kNsMaxLong == DEDLOC_ORTH
 
 namespace {
 
+#ifndef NS_FEW
+#define NS_FEW 256
+#endif
+constexpr uint32_t kNsFewTiles = NS_FEW;
+
 uint32_t blocks(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 1) / per); }
 
 int check_sides(uint32_t k, uint32_t rows, uint32_t cols) {
@@ -85,21 +90,26 @@ int run_batch(Batch &b, int src, int out, const dedloc_ortho_cfg &c, NsArgs a, v
     g = b.spread([&](const NsMat &m) { return blocks(m.rows, kNsPad) * blocks(m.cols, kNsPad); });
     e = timed(K_NS_PREPARE, s, [&] { return launch_ns_prepare(src, b.t, a, g, s); });
     if (e != hipSuccess) return hip_fail(e, "prepare launch");
-    auto triangle = [](const NsMat &m) {
-        const uint32_t T = Batch::S(m) / 64;
-        return T * (T + 1) / 2;
+    // workgroups of a phase in tiles of 128 x 256, or of 64 x 64
+    auto tiles = [&](int phase, bool wide) {
+        return b.spread([&](const NsMat &m) {
+            const uint32_t down = blocks(Batch::S(m), wide ? 128 : 64);
+            if (phase == kNsApply) return down * blocks(Batch::L(m), wide ? 256 : 64);
+            const uint32_t R = wide ? 2 : 1, u = down / R;  // R tile rows have the same number of tiles
+            return R * u * (u + 1) / 2 + (down % R) * (u + 1);
+        });
     };
+    static const int kinds[] = {K_NS_GRAM, K_NS_SQUARE, K_NS_APPLY};
     for (uint32_t k = 0; k < c.steps; k++) {
         a.turn = k % 2;
         a.last = k + 1 == c.steps;
-        g = b.spread(triangle);
-        e = timed(K_NS_GRAM, s, [&] { return launch_ns_product(kNsGram, out, b.t, a, g, s); });
-        if (e != hipSuccess) return hip_fail(e, "gram launch");
-        e = timed(K_NS_SQUARE, s, [&] { return launch_ns_product(kNsSquare, out, b.t, a, g, s); });
-        if (e != hipSuccess) return hip_fail(e, "square launch");
-        g = b.spread([](const NsMat &m) { return (Batch::S(m) / 64) * (Batch::L(m) / 64); });
-        e = timed(K_NS_APPLY, s, [&] { return launch_ns_product(kNsApply, out, b.t, a, g, s); });
-        if (e != hipSuccess) return hip_fail(e, "apply launch");
+        for (int phase = kNsGram; phase <= kNsApply; phase++) {
+            bool wide = true;
+            g = tiles(phase, wide);
+            if (g < kNsFewTiles) g = tiles(phase, wide = false);
+            e = timed(kinds[phase], s, [&] { return launch_ns_product(phase, out, wide, b.t, a, g, s); });
+            if (e != hipSuccess) return hip_fail(e, "product launch");
+        }
     }
     return DEDLOC_OK;
 }

@@ -63,7 +63,7 @@ enum NsPhase : int { kNsGram = 0, kNsSquare = 1, kNsApply = 2 };
 
 hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
 hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
-hipError_t launch_ns_product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
+hipError_t launch_ns_product(int phase, int out, bool wide, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
 
 // ------------------------------------------------ embedding and its gradient
 

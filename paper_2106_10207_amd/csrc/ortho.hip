@@ -15,8 +15,11 @@
 // are at most about 1.3 and 3, and the low planes of entries of the usual
 // size (1 / sqrt(s l)) then stay in fp16's normal range.
 //
-// Layout of a two-plane matrix: 32 columns of a row are 128 bytes, 64 of hi then
-// 64 of lo, so 128 bytes of a row are what one step of a product's loop reads.
+// Layout of a two-plane matrix: panels of 32 columns, in a panel the rows one after
+// the other, 128 bytes each, 64 of hi then 64 of lo.  A turn of a product's loop
+// reads a tile's rows of one panel, one piece of memory.  (Row by row, the rows
+// of a tile would lie 4 l bytes apart, for most matrices a power of two, and so
+// on one of the L2's channels.)
 // Both factors of every product have the summed index along their rows (A and
 // B are symmetric; X^T is kept beside X).
 #include "ops_internal.h"
@@ -58,9 +61,9 @@ __device__ inline char *at_a(const NsArgs &a, const NsMat &m, const Sides &d) {
 __device__ inline char *at_b(const NsArgs &a, const NsMat &m, const Sides &d) {
     return at_a(a, m, d) + (uint64_t)d.S * d.S * 4;
 }
-// Byte offset of element (i, j) of a matrix of `width` columns: its hi; lo is 64 bytes on.
-__device__ inline uint64_t at_planes(uint32_t i, uint32_t j, uint32_t width) {
-    return ((uint64_t)i * width + (j & ~31u)) * 4 + (j & 31u) * 2;
+// Byte offset of element (i, j) of a matrix of `rows` rows: its hi; lo is 64 bytes on.
+__device__ inline uint64_t at_planes(uint32_t i, uint32_t j, uint32_t rows) {
+    return ((uint64_t)(j / 32) * rows + i) * 128 + (j % 32) * 2;
 }
 
 __device__ inline void split(float v, _Float16 &hi, _Float16 &lo) {
@@ -167,81 +170,34 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
     __syncthreads();
     // the block as stored goes to X (wide) or X^T (tall), its transpose to the other
     char *straight = d.tall ? at_xt(a, m, d, 0) : at_x(a, m), *turned = d.tall ? at_x(a, m) : at_xt(a, m, d, 0);
-    const uint32_t w_straight = d.tall ? d.S : d.L, w_turned = d.tall ? d.L : d.S;
+    const uint32_t h_straight = d.tall ? d.L : d.S, h_turned = d.tall ? d.S : d.L;
     for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
         _Float16 hi, lo;
         split(tile[r][tc], hi, lo);
-        _Float16 *p = (_Float16 *)(straight + at_planes(r0 + r, c0 + tc, w_straight));
+        _Float16 *p = (_Float16 *)(straight + at_planes(r0 + r, c0 + tc, h_straight));
         p[0] = hi;
         p[32] = lo;
         split(tile[tc][r], hi, lo);
-        p = (_Float16 *)(turned + at_planes(c0 + r, r0 + tc, w_turned));
+        p = (_Float16 *)(turned + at_planes(c0 + r, r0 + tc, h_turned));
         p[0] = hi;
         p[32] = lo;
     }
 }
 
-// One tile of a product of a step.  OUT: the dtype of the result of the last
-// step's apply, or kNsMuonF32 for the update of the parameters.
+// A block's results: row i, columns j0 + 8 g + (0 to 3) are acc[4 g] to
+// acc[4 g + 3].  diagonal: the block lies on a symmetric result's diagonal.
 template <int PHASE, int OUT>
-__global__ __launch_bounds__(256) void ns_product_kernel(NsTable t, NsArgs a) {
-    constexpr uint32_t T = 64;
-    const NsMat &m = t.m[find(t, blockIdx.x)];
-    const Sides d = sides(m);
-    uint32_t k = blockIdx.x - m.begin, ti, tj;
-    if (PHASE == kNsApply) {
-        const uint32_t across = d.L / T;
-        ti = k / across;
-        tj = k % across;
-    } else {  // the lower triangle of a symmetric result
-        ti = (uint32_t)((sqrtf(8.0f * k + 1.0f) - 1.0f) * 0.5f);
-        while ((ti + 1) * (ti + 2) / 2 <= k) ti++;
-        while (ti * (ti + 1) / 2 > k) ti--;
-        tj = k - ti * (ti + 1) / 2;
-    }
-    const uint32_t K = PHASE == kNsGram ? d.L : d.S;  // the summed index
-    const char *left = PHASE == kNsGram ? at_x(a, m) : PHASE == kNsSquare ? at_a(a, m, d) : at_b(a, m, d);
-    const char *right = PHASE == kNsApply ? at_xt(a, m, d, a.turn) : left;
-    left += (uint64_t)ti * T * K * 4;
-    right += (uint64_t)tj * T * K * 4;
-
-    __shared__ __align__(16) char lds[2][T * 128];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / 2 * 32, wj = wave % 2 * 32;
-    f32x16 acc = {};
-    for (uint32_t kb = 0; kb < K; kb += 32) {
-        __syncthreads();
-        for (uint32_t c = threadIdx.x; c < T * 8; c += 256) {
-            const uint32_t row = c / 8, ch = c % 8;
-            const uint64_t from = (uint64_t)row * K * 4 + (uint64_t)kb * 4 + ch * 16;
-            const uint32_t to = row * 128 + ((ch ^ (row & 7)) * 16);
-            *(u32x4 *)(lds[0] + to) = *(const u32x4 *)(left + from);
-            *(u32x4 *)(lds[1] + to) = *(const u32x4 *)(right + from);
-        }
-        __syncthreads();
-#pragma unroll
-        for (uint32_t ks = 0; ks < 2; ks++) {
-            const uint32_t ri = wi + lane % 32, rj = wj + lane % 32, ch = ks * 2 + lane / 32;
-            const f16x8 ih = *(const f16x8 *)(lds[0] + ri * 128 + ((ch ^ (ri & 7)) * 16));
-            const f16x8 il = *(const f16x8 *)(lds[0] + ri * 128 + (((ch + 4) ^ (ri & 7)) * 16));
-            const f16x8 jh = *(const f16x8 *)(lds[1] + rj * 128 + ((ch ^ (rj & 7)) * 16));
-            const f16x8 jl = *(const f16x8 *)(lds[1] + rj * 128 + (((ch + 4) ^ (rj & 7)) * 16));
-            // the right factor's rows first: a lane then holds four consecutive columns of one row
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jh, il, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jl, ih, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(jh, ih, acc, 0, 0, 0);
-        }
-    }
-
-    const uint32_t i = ti * T + wi + lane % 32;
+__device__ inline void ns_finish(const NsMat &m, const Sides &d, const NsArgs &a, uint32_t i, uint32_t j0, bool diagonal,
+                                 const f32x16 &acc) {
 #pragma unroll
     for (uint32_t g = 0; g < 4; g++) {
-        const uint32_t j = tj * T + wj + 8 * g + 4 * (lane / 32);
+        const uint32_t j = j0 + 8 * g;
         float v[4];
         f16x4 hi, lo;
         if (PHASE == kNsGram) {
             for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (kAScale / (kXScale * kXScale));
         } else {
-            const char *old = (PHASE == kNsSquare ? at_a(a, m, d) : at_x(a, m)) + at_planes(i, j, PHASE == kNsSquare ? d.S : d.L);
+            const char *old = (PHASE == kNsSquare ? at_a(a, m, d) : at_x(a, m)) + at_planes(i, j, d.S);
             hi = *(const f16x4 *)old;
             lo = *(const f16x4 *)(old + 64);
             for (int e = 0; e < 4; e++) {
@@ -274,18 +230,125 @@ __global__ __launch_bounds__(256) void ns_product_kernel(NsTable t, NsArgs a) {
             lo[e] = w;
         }
         char *to = (PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_x(a, m)) +
-                   at_planes(i, j, PHASE == kNsApply ? d.L : d.S);
+                   at_planes(i, j, d.S);
         *(f16x4 *)to = hi;
         *(f16x4 *)(to + 64) = lo;
-        if (PHASE == kNsApply || ti != tj) {  // X^T, or the upper triangle
+        if (!diagonal) {  // X^T, or the upper triangle
             char *base = PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_xt(a, m, d, 1 - a.turn);
             for (int e = 0; e < 4; e++) {
-                _Float16 *p = (_Float16 *)(base + at_planes(j + e, i, d.S));
+                _Float16 *p = (_Float16 *)(base + at_planes(j + e, i, PHASE == kNsApply ? d.L : d.S));
                 p[0] = hi[e];
                 p[32] = lo[e];
             }
         }
     }
+}
+
+typedef __attribute__((address_space(1))) const void *GlobalPtr;
+typedef __attribute__((address_space(3))) void *LdsPtr;
+
+constexpr int kAllLoaded = 0x0f70;  // s_waitcnt vmcnt(0)
+
+// One tile of a product of a step: 64 WI rows and 64 WJ columns, a quarter per
+// wave, WI x WJ blocks of 32 x 32.  OUT: the dtype of the result of the last step's
+// apply, or kNsMuonF32 for the update of the parameters.
+//
+// A turn of the loop takes 32 of the summed index, 128 bytes of a row of either
+// factor.  They go from memory into LDS without passing registers, in flight
+// while the matrix cores work on the turn before, whose operands wait in
+// registers; other workgroups of the CU fill the rest of the latency.  16-byte
+// piece c of row r lies at place c ^ (r / 2 % 8) of its row, so that 16 lanes of a
+// read, one row each, meet all 64 banks (with r % 8 two rows met in a bank and
+// every read took 8 cycles instead of 4); the DMA writes lanes in order, so the
+// lane picks its source piece instead.
+template <int PHASE, int OUT, int WI, int WJ>
+__global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a) {
+    constexpr uint32_t TI = 64 * WI, TJ = 64 * WJ, R = WJ / WI;
+    // workgroups go round the 8 XCDs: give each a contiguous range of tiles
+    const uint32_t per = gridDim.x / 8, odd = gridDim.x % 8, xcd = blockIdx.x % 8;
+    const uint32_t wg = xcd * per + min(xcd, odd) + blockIdx.x / 8;
+    const NsMat &m = t.m[find(t, wg)];
+    const Sides d = sides(m);
+    uint32_t k = wg - m.begin, ti, tj;
+    if (PHASE == kNsApply) {
+        // bands of 8 tile rows, column by column: a tile's neighbours in time share its factors
+        const uint32_t across = (d.L + TJ - 1) / TJ, down = (d.S + TI - 1) / TI;
+        const uint32_t band = k / (8 * across), high = min(8u, down - band * 8);
+        k -= band * 8 * across;
+        ti = band * 8 + k % high;
+        tj = k / high;
+    } else {  // the lower triangle of a symmetric result: tile rows R u to R u + R - 1 have u + 1 tiles
+        uint32_t u = (uint32_t)((sqrtf(8.0f / R * k + 1.0f) - 1.0f) * 0.5f);
+        while (R * (u + 1) * (u + 2) / 2 <= k) u++;
+        while (R * u * (u + 1) / 2 > k) u--;
+        k -= R * u * (u + 1) / 2;
+        ti = R * u + k / (u + 1);
+        tj = k % (u + 1);
+    }
+    const uint32_t K = PHASE == kNsGram ? d.L : d.S;  // the summed index
+    const char *left = PHASE == kNsGram ? at_x(a, m) : PHASE == kNsSquare ? at_a(a, m, d) : at_b(a, m, d);
+    const char *right = PHASE == kNsApply ? at_xt(a, m, d, a.turn) : left;
+    const uint32_t left_rows = d.S, right_rows = PHASE == kNsApply ? d.L : d.S;
+
+    __shared__ __align__(1024) char lds[(TI + TJ) * 128];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wi = wave / 2 * (32 * WI), wj = wave % 2 * (32 * WJ);
+    // a load of a wave: 8 rows; rows past the end (padded to 64, so all 8 or none) repeat the last
+    const uint32_t from = (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
+    const char *src[2 * (WI + WJ)];
+#pragma unroll
+    for (uint32_t q = 0; q < 2 * (WI + WJ); q++) {
+        const uint32_t row = q * 32 + wave * 8;
+        src[q] = q < 2 * WI ? left + (uint64_t)min(ti * TI + row, left_rows - 8) * 128
+                            : right + (uint64_t)min(tj * TJ + row - TI, right_rows - 8) * 128;
+    }
+    auto fetch = [&](uint32_t panel) {
+#pragma unroll
+        for (uint32_t q = 0; q < 2 * (WI + WJ); q++)
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(src[q] + (uint64_t)panel * (q < 2 * WI ? left_rows : right_rows) * 128 + from),
+                                             (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16, 0, 0);
+    };
+    f32x16 acc[WI][WJ] = {};
+    fetch(0);
+    for (uint32_t panel = 0; panel < K / 32; panel++) {
+        f16x8 l[WI][2][2], r[WJ][2][2];  // [block][half of the turn][plane]
+        __builtin_amdgcn_s_waitcnt(kAllLoaded);  // this wave's part is in LDS: a barrier alone does not wait for it
+        __syncthreads();
+        auto read = [&](uint32_t row, uint32_t h, uint32_t p) {
+            const uint32_t c = p * 4 + h * 2 + lane / 32;
+            return *(const f16x8 *)(lds + row * 128 + ((c ^ (row / 2 % 8)) * 16));
+        };
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++)
+#pragma unroll
+            for (uint32_t p = 0; p < 2; p++) {
+#pragma unroll
+                for (uint32_t b = 0; b < WI; b++) l[b][h][p] = read(wi + b * 32 + lane % 32, h, p);
+#pragma unroll
+                for (uint32_t b = 0; b < WJ; b++) r[b][h][p] = read(TI + wj + b * 32 + lane % 32, h, p);
+            }
+        __syncthreads();
+        if (panel + 1 < K / 32) fetch(panel + 1);
+#pragma unroll
+        for (uint32_t h = 0; h < 2; h++)
+#pragma unroll
+            for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
+#pragma unroll
+                for (uint32_t i = 0; i < WI; i++)
+#pragma unroll
+                    for (uint32_t j = 0; j < WJ; j++)
+                        // the right factor's rows first: a lane then holds four consecutive columns of one row
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[j][h][p == 1], l[i][h][p == 0], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (uint32_t bi = 0; bi < WI; bi++)
+#pragma unroll
+        for (uint32_t bj = 0; bj < WJ; bj++) {
+            const uint32_t i0 = ti * TI + wi + bi * 32, j0 = tj * TJ + wj + bj * 32;
+            // of a symmetric result the blocks above the diagonal are written as the mirror of those below
+            if (i0 < left_rows && j0 < right_rows && (PHASE == kNsApply || j0 <= i0))
+                ns_finish<PHASE, OUT>(m, d, a, i0 + lane % 32, j0 + 4 * (lane / 32), PHASE != kNsApply && i0 == j0, acc[bi][bj]);
+        }
 }
 
 // ---------------------------------------------------------------- launchers
@@ -314,19 +377,28 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
     return hipGetLastError();
 }
 
-hipError_t launch_ns_product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+namespace {
+template <int WI, int WJ>
+void product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
     if (phase == kNsGram) {
-        ns_product_kernel<kNsGram, kNsF32><<<groups, 256, 0, s>>>(t, a);
+        ns_product_kernel<kNsGram, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a);
     } else if (phase == kNsSquare) {
-        ns_product_kernel<kNsSquare, kNsF32><<<groups, 256, 0, s>>>(t, a);
+        ns_product_kernel<kNsSquare, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a);
     } else {
         switch (out) {
-            case kNsF32: ns_product_kernel<kNsApply, kNsF32><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16><<<groups, 256, 0, s>>>(t, a); break;
-            default: ns_product_kernel<kNsApply, kNsMuonF32><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsF32: ns_product_kernel<kNsApply, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
+            default: ns_product_kernel<kNsApply, kNsMuonF32, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
         }
     }
+}
+}  // namespace
+
+// wide: tiles of 128 x 256, else of 64 x 64 (what `groups` and the table count)
+hipError_t launch_ns_product(int phase, int out, bool wide, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    if (wide) product<2, 4>(phase, out, t, a, groups, s);
+    else product<1, 1>(phase, out, t, a, groups, s);
     return hipGetLastError();
 }
 
