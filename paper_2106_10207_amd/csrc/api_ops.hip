@@ -17,6 +17,10 @@ static_assert(kNsMaxShort == DEDLOC_ORTHO_MAX_SHORT && kNsMaxLong == DEDLOC_ORTH
 
 namespace {
 
+#ifndef NS_TI
+#define NS_TI 128
+#define NS_TJ 256
+#endif
 #ifndef NS_FEW
 #define NS_FEW 256
 #endif
@@ -93,9 +97,9 @@ int run_batch(Batch &b, int src, int out, const dedloc_ortho_cfg &c, NsArgs a, v
     // workgroups of a phase in tiles of 128 x 256, or of 64 x 64
     auto tiles = [&](int phase, bool wide) {
         return b.spread([&](const NsMat &m) {
-            const uint32_t down = blocks(Batch::S(m), wide ? 128 : 64);
-            if (phase == kNsApply) return down * blocks(Batch::L(m), wide ? 256 : 64);
-            const uint32_t R = wide ? 2 : 1, u = down / R;  // R tile rows have the same number of tiles
+            const uint32_t down = blocks(Batch::S(m), wide ? NS_TI : 64);
+            if (phase == kNsApply) return down * blocks(Batch::L(m), wide ? NS_TJ : 64);
+            const uint32_t R = wide ? NS_TJ / NS_TI : 1, u = down / R;  // R tile rows have the same number of tiles
             return R * u * (u + 1) / 2 + (down % R) * (u + 1);
         });
     };

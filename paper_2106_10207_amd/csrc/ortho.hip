@@ -22,8 +22,16 @@
 // on one of the L2's channels.)
 // Both factors of every product have the summed index along their rows (A and
 // B are symmetric; X^T is kept beside X).
+#include <type_traits>
+
 #include "ops_internal.h"
 
+#ifndef NS_WIDE
+#define NS_WIDE 2, 4, 2
+#endif
+#ifndef NS_SMALL
+#define NS_SMALL 1, 1, 4
+#endif
 namespace dedloc {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -244,24 +252,39 @@ __device__ inline void ns_finish(const NsMat &m, const Sides &d, const NsArgs &a
     }
 }
 
-typedef __attribute__((address_space(1))) const void *GlobalPtr;
+#ifndef NS_WIDE
+#define NS_WIDE 2, 4, 1
+#endif
+#ifndef NS_SMALL
+#define NS_SMALL 1, 1, 4
+#endif
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
-constexpr int kAllLoaded = 0x0f70;  // s_waitcnt vmcnt(0)
+// Waits until at most N of this wave's loads are in flight and its LDS reads are done, then for the workgroup's other
+// waves.  (A fence would wait for LDS alone, __syncthreads for every load.)
+template <int N>
+__device__ inline void arrived() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x70);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+constexpr int kRawBuffer = 0x00020000;  // descriptor of untyped bytes
+constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // classes of sched_group_barrier
 
 // One tile of a product of a step: 64 WI rows and 64 WJ columns, a quarter per
 // wave, WI x WJ blocks of 32 x 32.  OUT: the dtype of the result of the last step's
 // apply, or kNsMuonF32 for the update of the parameters.
 //
 // A turn of the loop takes 32 of the summed index, 128 bytes of a row of either
-// factor.  They go from memory into LDS without passing registers, in flight
-// while the matrix cores work on the turn before, whose operands wait in
-// registers; other workgroups of the CU fill the rest of the latency.  16-byte
-// piece c of row r lies at place c ^ (r / 2 % 8) of its row, so that 16 lanes of a
-// read, one row each, meet all 64 banks (with r % 8 two rows met in a bank and
-// every read took 8 cycles instead of 4); the DMA writes lanes in order, so the
-// lane picks its source piece instead.
-template <int PHASE, int OUT, int WI, int WJ>
+// factor.  They go from memory into one of NS stages of LDS without passing
+// registers, NS - 1 turns ahead, and from there into registers half a turn ahead, so that
+// the matrix cores find their operands; loads and reads are dealt out between the products.
+// 16-byte piece c of row r lies at place c ^ (r / 2 % 8) of its row, so that 16
+// lanes of a read, one row each, meet all 64 banks (with r % 8 two rows met in a bank
+// and every read took 8 cycles instead of 4); the load writes lanes in order, so
+// the lane picks its source piece instead.
+template <int PHASE, int OUT, int WI, int WJ, int NS>
 __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a) {
     constexpr uint32_t TI = 64 * WI, TJ = 64 * WJ, R = WJ / WI;
     // workgroups go round the 8 XCDs: give each a contiguous range of tiles
@@ -290,56 +313,89 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a)
     const char *right = PHASE == kNsApply ? at_xt(a, m, d, a.turn) : left;
     const uint32_t left_rows = d.S, right_rows = PHASE == kNsApply ? d.L : d.S;
 
-    __shared__ __align__(1024) char lds[(TI + TJ) * 128];
+    constexpr uint32_t kStage = (TI + TJ) * 128;
+    // one array per stage: the compiler then knows which loads a read has to wait for
+    __shared__ __align__(1024) char lds0[kStage], lds1[NS > 1 ? kStage : 16], lds2[NS > 2 ? kStage : 16],
+        lds3[NS > 3 ? kStage : 16];
+    auto stage = [&](uint32_t k) { return k == 0 ? lds0 : k == 1 ? lds1 : k == 2 ? lds2 : lds3; };
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wi = wave / 2 * (32 * WI), wj = wave % 2 * (32 * WJ);
-    // a load of a wave: 8 rows; rows past the end (padded to 64, so all 8 or none) repeat the last
-    const uint32_t from = (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
-    const char *src[2 * (WI + WJ)];
+    // A load of a wave takes 8 rows.  The panels' rows past the matrix' end lie beyond the descriptor's end and read as 0.
+    constexpr uint32_t kLoads = 2 * (WI + WJ);
+    const uint32_t from = wave * 1024 + (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
+    const uint64_t left_panel = (uint64_t)left_rows * 128, right_panel = (uint64_t)right_rows * 128;
+    const uint32_t left_end = (left_rows - ti * TI) * 128, right_end = (right_rows - tj * TJ) * 128;
+    left += (uint64_t)ti * TI * 128;
+    right += (uint64_t)tj * TJ * 128;
+    const uint32_t panels = K / 32;
+    auto fetch = [&](char *lds, uint32_t panel) {
+        const uint64_t p = min(panel, panels - 1);  // past the end the last once more: the loop then counts its loads
+        const auto lrows = __builtin_amdgcn_make_buffer_rsrc((void *)(left + p * left_panel), 0, left_end, kRawBuffer);
+        const auto rrows = __builtin_amdgcn_make_buffer_rsrc((void *)(right + p * right_panel), 0, right_end, kRawBuffer);
 #pragma unroll
-    for (uint32_t q = 0; q < 2 * (WI + WJ); q++) {
-        const uint32_t row = q * 32 + wave * 8;
-        src[q] = q < 2 * WI ? left + (uint64_t)min(ti * TI + row, left_rows - 8) * 128
-                            : right + (uint64_t)min(tj * TJ + row - TI, right_rows - 8) * 128;
-    }
-    auto fetch = [&](uint32_t panel) {
-#pragma unroll
-        for (uint32_t q = 0; q < 2 * (WI + WJ); q++)
-            __builtin_amdgcn_global_load_lds((GlobalPtr)(src[q] + (uint64_t)panel * (q < 2 * WI ? left_rows : right_rows) * 128 + from),
-                                             (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16, 0, 0);
+        for (uint32_t q = 0; q < kLoads; q++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(q < 2 * WI ? lrows : rrows, (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16,
+                                                     from, (q < 2 * WI ? q : q - 2 * WI) * 4096, 0, 0);
     };
     f32x16 acc[WI][WJ] = {};
-    fetch(0);
-    for (uint32_t panel = 0; panel < K / 32; panel++) {
-        f16x8 l[WI][2][2], r[WJ][2][2];  // [block][half of the turn][plane]
-        __builtin_amdgcn_s_waitcnt(kAllLoaded);  // this wave's part is in LDS: a barrier alone does not wait for it
-        __syncthreads();
-        auto read = [&](uint32_t row, uint32_t h, uint32_t p) {
+    f16x8 l[2][WI][2], r[2][WJ][2];  // [half of the turn][block][plane]
+    auto read = [&](const char *lds, uint32_t h) {
+        auto one = [&](uint32_t row, uint32_t p) {
             const uint32_t c = p * 4 + h * 2 + lane / 32;
             return *(const f16x8 *)(lds + row * 128 + ((c ^ (row / 2 % 8)) * 16));
         };
 #pragma unroll
-        for (uint32_t h = 0; h < 2; h++)
+        for (uint32_t p = 0; p < 2; p++) {
 #pragma unroll
-            for (uint32_t p = 0; p < 2; p++) {
+            for (uint32_t b = 0; b < WI; b++) l[h][b][p] = one(wi + b * 32 + lane % 32, p);
 #pragma unroll
-                for (uint32_t b = 0; b < WI; b++) l[b][h][p] = read(wi + b * 32 + lane % 32, h, p);
+            for (uint32_t b = 0; b < WJ; b++) r[h][b][p] = one(TI + wj + b * 32 + lane % 32, p);
+        }
+    };
+    auto multiply = [&](uint32_t h) {
 #pragma unroll
-                for (uint32_t b = 0; b < WJ; b++) r[b][h][p] = read(TI + wj + b * 32 + lane % 32, h, p);
-            }
-        __syncthreads();
-        if (panel + 1 < K / 32) fetch(panel + 1);
+        for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
 #pragma unroll
-        for (uint32_t h = 0; h < 2; h++)
+            for (uint32_t i = 0; i < WI; i++)
 #pragma unroll
-            for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
+                for (uint32_t j = 0; j < WJ; j++)
+                    // the right factor's rows first: a lane then holds four consecutive columns of one row
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[h][j][p == 1], l[h][i][p == 0], acc[i][j], 0, 0, 0);
+    };
 #pragma unroll
-                for (uint32_t i = 0; i < WI; i++)
+    for (uint32_t k = 0; k < NS; k++) fetch(stage(k), k);
+    arrived<(NS - 1) * kLoads>();
+    read(stage(0), 0);
+    auto turn = [&](uint32_t k, uint32_t panel) {
+        read(stage(k), 1);
+        multiply(0);
 #pragma unroll
-                    for (uint32_t j = 0; j < WJ; j++)
-                        // the right factor's rows first: a lane then holds four consecutive columns of one row
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[j][h][p == 1], l[i][h][p == 0], acc[i][j], 0, 0, 0);
-    }
+        for (uint32_t q = 0; q < kLoads; q++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * WI * WJ / kLoads, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
+        }
+        // the next stage is there, and all have read this one, which the next loads fill
+        __builtin_amdgcn_sched_barrier(0);
+        arrived<(NS - 2) * kLoads>();
+        __builtin_amdgcn_sched_barrier(0);
+        read(stage((k + 1) % NS), 0);
+        fetch(stage(k), panel + NS);
+        multiply(1);
+#pragma unroll
+        for (uint32_t q = 0; q < kLoads; q++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * WI * WJ / kLoads, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedLoad, 1, 0);
+        }
+    };
+    uint32_t panel = 0;
+    for (; panel + NS <= panels; panel += NS)  // whole rounds of the stages, without a way out: the compiler counts the loads
+#pragma unroll
+        for (uint32_t k = 0; k < NS; k++) turn(k, panel + k);
+#pragma unroll
+    for (uint32_t k = 0; k + 1 < NS; k++)
+        if (panel + k < panels) turn(k, panel + k);
+    arrived<0>();  // no load may arrive in LDS that another workgroup has by then
 #pragma unroll
     for (uint32_t bi = 0; bi < WI; bi++)
 #pragma unroll
@@ -378,18 +434,18 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
 }
 
 namespace {
-template <int WI, int WJ>
+template <int WI, int WJ, int NS>
 void product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
     if (phase == kNsGram) {
-        ns_product_kernel<kNsGram, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a);
+        ns_product_kernel<kNsGram, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a);
     } else if (phase == kNsSquare) {
-        ns_product_kernel<kNsSquare, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a);
+        ns_product_kernel<kNsSquare, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a);
     } else {
         switch (out) {
-            case kNsF32: ns_product_kernel<kNsApply, kNsF32, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
-            default: ns_product_kernel<kNsApply, kNsMuonF32, WI, WJ><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsF32: ns_product_kernel<kNsApply, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
+            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
+            default: ns_product_kernel<kNsApply, kNsMuonF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
         }
     }
 }
@@ -397,8 +453,8 @@ void product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t gro
 
 // wide: tiles of 128 x 256, else of 64 x 64 (what `groups` and the table count)
 hipError_t launch_ns_product(int phase, int out, bool wide, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
-    if (wide) product<2, 4>(phase, out, t, a, groups, s);
-    else product<1, 1>(phase, out, t, a, groups, s);
+    if (wide) product<NS_WIDE>(phase, out, t, a, groups, s);
+    else product<NS_SMALL>(phase, out, t, a, groups, s);
     return hipGetLastError();
 }
 
