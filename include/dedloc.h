@@ -405,7 +405,8 @@ typedef struct {
  * are rounded once, at the end.  The arithmetic takes |X|, |A| and |B| up to 15,
  * 63 and 63: coefficients that leave that range give infinities or NaN.  A zero
  * matrix gives zeros; one that holds an infinity or NaN gives NaN throughout.
- * Results are the same bits for the same call, whatever the other matrices.
+ * Equal calls give equal bits; beside other matrices a matrix' sums may be
+ * taken in other pieces, and so differ in their last bits.
  * ws: dedloc_orthogonalize_workspace_bytes (0 for invalid arguments; it looks
  * at the sides and their limits only), 256-byte aligned, contents arbitrary.
  * About 12 bytes an element and 8 a square of the shorter side; calls that

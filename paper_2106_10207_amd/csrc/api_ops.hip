@@ -17,15 +17,6 @@ static_assert(kNsMaxShort == DEDLOC_ORTHO_MAX_SHORT && kNsMaxLong == DEDLOC_ORTH
 
 namespace {
 
-#ifndef NS_TI
-#define NS_TI 128
-#define NS_TJ 256
-#endif
-#ifndef NS_FEW
-#define NS_FEW 256
-#endif
-constexpr uint32_t kNsFewTiles = NS_FEW;
-
 uint32_t blocks(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 1) / per); }
 
 int check_sides(uint32_t k, uint32_t rows, uint32_t cols) {
@@ -40,32 +31,107 @@ int check_ortho(const dedloc_ortho_cfg &c) {
     return DEDLOC_OK;
 }
 
-// Matrices are worked on in batches of kNsMats, one after the other on the
-// same workspace.  A batch is built by add() until it is full.
+uint32_t padded(uint32_t n) { return blocks(n, kNsPad) * kNsPad; }
+
+// Steps of the block that starts `done` steps into `steps`: how many are taken
+// on the s x s side before X is touched again.  An error of A grows by a^2 in each, so a
+// block from X0 takes at most three (a = 3.4445: 141 times) and a later one, whose A is no longer
+// small, two; with a beyond 3.5 fewer.
+uint32_t block_steps(const dedloc_ortho_cfg &c, bool blocked, uint32_t done) {
+    if (!blocked) return 1;
+    const double grow = (double)c.a * c.a;
+    uint32_t n = 1;
+    for (double g = grow; g <= 150.0 && n < 3; g *= grow) n++;
+    return std::min(done == 0 ? n : std::min(n, 2u), c.steps - done);
+}
+
+// The products of a call on one matrix, in order: at most two at a launch.
+struct Program {
+    uint32_t op[3 * DEDLOC_ORTHO_MAX_STEPS + 64][2];
+    uint32_t n = 0;
+};
+uint32_t op_of(int kind, uint32_t left, uint32_t right, uint32_t out) { return kind | left << 4 | right << 8 | out << 12; }
+
+void make_program(const dedloc_ortho_cfg &c, bool blocked, Program &p) {
+    constexpr uint32_t none = ~0u, A0 = kNsSmall, M0 = A0 + 1, A1 = A0 + 2, M1 = A0 + 3, C = A0 + 4, Q = A0 + 5;
+    p.n = 0;
+    auto add = [&](uint32_t first, uint32_t second = none) {
+        p.op[p.n][0] = first;
+        p.op[p.n++][1] = second;
+    };
+    uint32_t turn = 1;  // which X^T is read
+    for (uint32_t done = 0; done < c.steps;) {
+        const uint32_t n = block_steps(c, blocked, done);
+        uint32_t q = M0;
+        add(op_of(kNsGram, 0, 0, A0));
+        add(op_of(kNsSquare, A0, A0, M0));
+        if (n > 1) {
+            add(op_of(kNsMul, M0, M0, C));
+            add(op_of(kNsMul, C, A0, A1));  // M A M
+            add(op_of(kNsSquare, A1, A1, M1));
+            if (n == 2) {
+                add(op_of(kNsMul, M1, M0, Q));
+                q = Q;
+            } else {
+                add(op_of(kNsMul, M1, M1, C), op_of(kNsMul, M1, M0, Q));
+                add(op_of(kNsMul, C, A1, A0));
+                add(op_of(kNsSquare, A0, A0, M0));
+                add(op_of(kNsMul, M0, Q, M1));
+                q = M1;
+            }
+        }
+        done += n;
+        add(op_of(done == c.steps ? kNsResult : kNsApply, q, turn, 3 - turn));
+        turn = 3 - turn;
+    }
+}
+
+#ifndef NS_BLOCKED
+#define NS_BLOCKED (1ull << 28)
+#endif
+constexpr uint64_t kNsBlocked = NS_BLOCKED;
+
+// Whether a matrix is worked on in blocks of steps.  Five steps as blocks of three and two
+// are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15.
+bool blocked(uint32_t rows, uint32_t cols) {
+    const uint64_t s = std::min(rows, cols), l = std::max(rows, cols);
+    return s * s * (l - s) >= kNsBlocked;
+}
+
+// Matrices are worked on in batches, one after the other on the same workspace:
+// as many as two works each of the blocked ones, one of the others, fit a launch.
 struct Batch {
     NsTable t;
-    uint64_t regions = 0;
+    NsWork w[kNsWorks];  // per matrix: the fields that do not change
+    bool blocked_[kNsWorks];
+    uint32_t works;
+    uint64_t regions;
     bool muon;
     explicit Batch(bool muon_) : muon(muon_) { clear(); }
     void clear() {
         memset(&t, 0, sizeof t);
+        works = 0;
         regions = 0;
     }
-    bool full() const { return t.n == (uint32_t)kNsMats; }
-    static uint32_t S(const NsMat &m) { return blocks(std::min(m.rows, m.cols), kNsPad) * kNsPad; }
-    static uint32_t L(const NsMat &m) { return blocks(std::max(m.rows, m.cols), kNsPad) * kNsPad; }
+    bool fits(uint32_t rows, uint32_t cols) const { return works + 1 + blocked(rows, cols) <= (uint32_t)kNsWorks; }
     uint32_t sums(const NsMat &m) const {
         return muon ? blocks((uint64_t)m.rows * m.cols, kSumChunk) : blocks(m.rows, kNsTile) * blocks(m.cols, kNsTile);
     }
-    void add(NsMat m) {
-        m.base = regions;
-        m.part = t.parts;
-        const uint64_t s = S(m), l = L(m);
-        regions += round_up((size_t)(3 * s * l + 2 * s * s) * 4, 256);
+    void add(const void *in, uint64_t ld_in, void *out, uint64_t ld_out, uint32_t rows, uint32_t cols, uint32_t flags, float unit) {
+        const uint64_t s = padded(std::min(rows, cols)), l = padded(std::max(rows, cols));
+        const bool b = blocked(rows, cols);
+        NsMat &m = t.m[t.n];
+        m = {regions, in, ld_in, rows, cols, t.parts, 0};
         t.parts += sums(m);
-        t.m[t.n++] = m;
+        w[t.n] = {regions, out, ld_out, rows, cols, 0, 0, (flags & DEDLOC_TENSOR_DECAY) << 16, unit};
+        blocked_[t.n++] = b;
+        works += 1 + b;
+        regions += round_up((size_t)(kNsSmall * s * l + (b ? kNsSmalls : 2) * s * s) * 4, 256);
     }
-    size_t bytes() const { return (size_t)regions + round_up((size_t)t.parts * sizeof(double), 256); }
+    size_t part_bytes() const { return round_up((size_t)t.parts * sizeof(double), 256); }
+    // room for the sums of cut items: what a launch cuts stays below it
+    size_t piece_bytes() const { return round_up(std::max((size_t)regions / 2, (size_t)4 << 20), 256); }
+    size_t bytes() const { return (size_t)regions + part_bytes() + piece_bytes(); }
     // Workgroups of a launch in which matrix m takes count(m).
     template <typename F>
     uint32_t spread(F count) {
@@ -77,45 +143,140 @@ struct Batch {
         return g;
     }
 };
+static_assert(DEDLOC_TENSOR_DECAY == 1u, "the flag's bit moves into a work's op");
+
+uint32_t tiles_of(const NsWork &w, uint32_t edge) {
+    const uint32_t down = blocks(padded(std::min(w.rows, w.cols)), edge);
+    return (w.op & 15) >= kNsApply ? down * blocks(padded(std::max(w.rows, w.cols)), edge) : down * (down + 1) / 2;
+}
+uint32_t panels_of(const NsWork &w) {
+    return padded((w.op & 15) == kNsGram ? std::max(w.rows, w.cols) : std::min(w.rows, w.cols)) / 32;
+}
+uint32_t pieces_of(uint32_t panels, uint32_t most) { return panels > most + most / 2 ? blocks(panels, most) : 1; }
+
+#ifndef NS_FORCE_EDGE
+#define NS_FORCE_EDGE 0
+#endif
+#ifndef NS_FORCE_CUT
+#define NS_FORCE_CUT 0
+#endif
+
+// How a launch's products are cut: the edge of the tiles, and pieces of at most
+// `most` panels of the summed index.
+struct Cut {
+    uint32_t edge, most;
+};
+
+// Estimated time of a launch in ns, below 0 if the sums of its cut items take more than `room` bytes.
+double cost_of(const NsWorks &t, Cut c, size_t room) {
+    const double busy = c.edge == 128 ? 575 : 165, alone = c.edge == 128 ? 750 : 230, once = c.edge == 128 ? 3000 : 2000;
+    double turns = 0, cut = 0;
+    uint32_t longest = 0;
+    for (uint32_t k = 0; k < t.n; k++) {
+        const uint32_t P = panels_of(t.w[k]), z = pieces_of(P, c.most), len = blocks(P, z);
+        const double tiles = tiles_of(t.w[k], c.edge);
+        turns += tiles * (P + z * (once / busy));
+        longest = std::max(longest, len);
+        if (z > 1) cut += tiles * z * c.edge * c.edge * sizeof(float);
+    }
+    if (cut > (double)room) return -1.0;
+    return std::max(turns / 256 * busy + 0.5 * longest * busy, longest * alone + once) + (cut > 0 ? 4000 + cut / 2000 : 0);
+}
+
+Cut choose_cut(const NsWorks &t, size_t room) {
+    Cut best = {};
+    double cost = 0;
+    for (uint32_t edge : {128u, 64u})
+        for (uint32_t most : {1u << 30, 512u, 256u, 128u, 64u, 32u, 16u, 8u}) {
+            if (NS_FORCE_EDGE && edge != NS_FORCE_EDGE) continue;
+            if (NS_FORCE_CUT && most != NS_FORCE_CUT && most != 1u << 30) continue;
+            const double c = cost_of(t, {edge, most}, room);
+            if (c >= 0 && (best.edge == 0 || c < cost || (NS_FORCE_CUT && most == NS_FORCE_CUT))) {
+                cost = c;
+                best = {edge, most};
+            }
+        }
+    return best;
+}
+
+// The works of a batch's launch `k`; those with the longest sums first.
+void works_of(const Batch &b, const Program p[2], uint32_t k, NsWorks &t) {
+    t.n = 0;
+    for (uint32_t m = 0; m < b.t.n; m++) {
+        const Program &q = p[b.blocked_[m]];
+        for (uint32_t i = 0; i < 2 && k < q.n; i++)
+            if (q.op[k][i] != ~0u) {
+                t.w[t.n] = b.w[m];
+                t.w[t.n++].op |= q.op[k][i];
+            }
+    }
+    std::sort(t.w, t.w + t.n, [](const NsWork &x, const NsWork &y) { return panels_of(x) > panels_of(y); });
+}
+
+// Sets every work's pieces and first item: the launch's items, the tiles that are cut and the items that these have.
+struct Items {
+    uint32_t all, cut_tiles, cut_items;
+};
+Items cut_works(NsWorks &t, Cut c) {
+    Items n = {};
+    for (uint32_t k = 0; k < t.n; k++) {
+        NsWork &w = t.w[k];
+        const uint32_t tiles = tiles_of(w, c.edge);
+        w.pieces = pieces_of(panels_of(w), c.most);
+        w.begin = n.all;
+        n.all += tiles * w.pieces;
+        if (w.pieces > 1) {
+            n.cut_tiles += tiles;
+            n.cut_items = n.all;
+        }
+    }
+    return n;
+}
 
 // The steps on a batch.  src: where the matrices come from; out: where the
 // results go (a dtype, or kNsMuonF32).
-int run_batch(Batch &b, int src, int out, const dedloc_ortho_cfg &c, NsArgs a, void *ws, hipStream_t s) {
-    if (b.t.n == 0) return DEDLOC_OK;
+int run_batch(Batch &b, const Program p[2], int src, int out, NsArgs a, void *ws, hipStream_t s) {
     a.ws = (char *)ws;
     a.part = (double *)((char *)ws + b.regions);
-    a.a = c.a;
-    a.b = c.b;
-    a.c = c.c;
-    a.eps = c.eps;
+    a.pieces = (float *)((char *)ws + b.regions + b.part_bytes());
     uint32_t g = b.spread([&](const NsMat &m) { return b.sums(m); });
     hipError_t e = timed(b.muon ? K_MUON_SUM : K_NS_SUM, s, [&] { return launch_ns_sum(src, b.t, a, g, s); });
     if (e != hipSuccess) return hip_fail(e, "norm launch");
     g = b.spread([&](const NsMat &m) { return blocks(m.rows, kNsPad) * blocks(m.cols, kNsPad); });
     e = timed(K_NS_PREPARE, s, [&] { return launch_ns_prepare(src, b.t, a, g, s); });
     if (e != hipSuccess) return hip_fail(e, "prepare launch");
-    // workgroups of a phase in tiles of 128 x 256, or of 64 x 64
-    auto tiles = [&](int phase, bool wide) {
-        return b.spread([&](const NsMat &m) {
-            const uint32_t down = blocks(Batch::S(m), wide ? NS_TI : 64);
-            if (phase == kNsApply) return down * blocks(Batch::L(m), wide ? NS_TJ : 64);
-            const uint32_t R = wide ? NS_TJ / NS_TI : 1, u = down / R;  // R tile rows have the same number of tiles
-            return R * u * (u + 1) / 2 + (down % R) * (u + 1);
-        });
-    };
-    static const int kinds[] = {K_NS_GRAM, K_NS_SQUARE, K_NS_APPLY};
-    for (uint32_t k = 0; k < c.steps; k++) {
-        a.turn = k % 2;
-        a.last = k + 1 == c.steps;
-        for (int phase = kNsGram; phase <= kNsApply; phase++) {
-            bool wide = true;
-            g = tiles(phase, wide);
-            if (g < kNsFewTiles) g = tiles(phase, wide = false);
-            e = timed(kinds[phase], s, [&] { return launch_ns_product(phase, out, wide, b.t, a, g, s); });
-            if (e != hipSuccess) return hip_fail(e, "product launch");
-        }
+    NsWorks t;
+    for (uint32_t k = 0; k < std::max(p[0].n, p[1].n); k++) {
+        works_of(b, p, k, t);
+        if (t.n == 0) break;
+        const Cut c = choose_cut(t, b.piece_bytes());
+        const Items n = cut_works(t, c);
+        e = timed(K_NS_PRODUCT, s, [&] { return launch_ns_product(out, c.edge, t, a, n.all, s); });
+        if (e != hipSuccess) return hip_fail(e, "product launch");
+        if (n.cut_tiles == 0) continue;
+        e = timed(K_NS_JOIN, s, [&] { return launch_ns_join(out, c.edge, t, a, n.cut_tiles, s); });
+        if (e != hipSuccess) return hip_fail(e, "join launch");
     }
     return DEDLOC_OK;
+}
+
+// Calls run(batch) on the matrices of a call in batches.  next(k, batch) adds
+// matrix k; sides(k, rows, cols) gives its sides.
+template <typename S, typename N, typename R>
+int in_batches(bool muon, uint32_t n, S sides, N next, R run) {
+    Batch b(muon);
+    for (uint32_t k = 0; k < n; k++) {
+        uint32_t rows = 0, cols = 0;
+        sides(k, rows, cols);
+        if (rows == 0 || cols == 0) continue;
+        if (!b.fits(rows, cols)) {
+            const int rc = run(b);
+            if (rc) return rc;
+            b.clear();
+        }
+        next(k, b);
+    }
+    return b.t.n ? run(b) : DEDLOC_OK;
 }
 
 int check_ws(const void *ws, size_t have, size_t need) {
@@ -126,19 +287,24 @@ int check_ws(const void *ws, size_t have, size_t need) {
 }
 
 // Workspace of matrices given by their sides: the largest batch's.
-template <typename F>
-size_t batches_bytes(bool muon, uint32_t n, F sides) {
-    Batch b(muon);
-    size_t most = 256;
+template <typename S>
+size_t batches_bytes(bool muon, uint32_t n, S sides) {
     for (uint32_t k = 0; k < n; k++) {
-        NsMat m = {};
-        sides(k, m.rows, m.cols);
-        if (m.rows == 0 || m.cols == 0) continue;
-        if (check_sides(k, m.rows, m.cols)) return 0;
-        if (b.full()) b.clear();
-        b.add(m);
-        most = std::max(most, b.bytes());
+        uint32_t rows = 0, cols = 0;
+        sides(k, rows, cols);
+        if (check_sides(k, rows, cols)) return 0;
     }
+    size_t most = 256;
+    in_batches(muon, n, sides,
+               [&](uint32_t k, Batch &b) {
+                   uint32_t rows = 0, cols = 0;
+                   sides(k, rows, cols);
+                   b.add(nullptr, 0, nullptr, 0, rows, cols, 0, 0.0f);
+               },
+               [&](Batch &b) {
+                   most = std::max(most, b.bytes());
+                   return DEDLOC_OK;
+               });
     return most;
 }
 
@@ -230,26 +396,25 @@ int dedloc_orthogonalize(const dedloc_matrix *mats, uint32_t n, int32_t dtype, c
     if (need == 0) return DEDLOC_ERR_INVALID_ARG;
     rc = check_ws(ws, ws_bytes, need);
     if (rc) return rc;
-    Batch b(false);
+    Program p[2];
+    make_program(*cfg, false, p[0]);
+    make_program(*cfg, true, p[1]);
     NsArgs a = {};
-    for (uint32_t k = 0; k < n; k++) {
-        const dedloc_matrix &q = mats[k];
-        if (q.rows == 0 || q.cols == 0) continue;
-        if (b.full()) {
-            rc = run_batch(b, dtype, dtype, *cfg, a, ws, (hipStream_t)stream);
-            if (rc) return rc;
-            b.clear();
-        }
-        NsMat m = {};
-        m.in = q.in;
-        m.out = q.out;
-        m.ld_in = q.ld_in;
-        m.ld_out = q.ld_out;
-        m.rows = q.rows;
-        m.cols = q.cols;
-        b.add(m);
-    }
-    return run_batch(b, dtype, dtype, *cfg, a, ws, (hipStream_t)stream);
+    a.a = cfg->a;
+    a.b = cfg->b;
+    a.c = cfg->c;
+    a.eps = cfg->eps;
+    return in_batches(
+        false, n,
+        [&](uint32_t k, uint32_t &rows, uint32_t &cols) {
+            rows = mats[k].rows;
+            cols = mats[k].cols;
+        },
+        [&](uint32_t k, Batch &b) {
+            const dedloc_matrix &m = mats[k];
+            b.add(m.in, m.ld_in, m.out, m.ld_out, m.rows, m.cols, 0, 0.0f);
+        },
+        [&](Batch &b) { return run_batch(b, p, dtype, dtype, a, ws, (hipStream_t)stream); });
 }
 
 size_t dedloc_muon_workspace_bytes(const uint32_t *rows, const uint32_t *cols, uint32_t n_tensors) {
@@ -299,8 +464,14 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
     rc = check_ws(ws, ws_bytes, need);
     if (rc) return rc;
     const int src = grad_codec == DEDLOC_CODEC_F32 ? kNsMuonF32 : grad_codec == DEDLOC_CODEC_FP16 ? kNsMuonFP16 : kNsMuonI8;
-    Batch b(true);
+    Program p[2];
+    make_program(cfg->ortho, false, p[0]);
+    make_program(cfg->ortho, true, p[1]);
     NsArgs a = {};
+    a.a = cfg->ortho.a;
+    a.b = cfg->ortho.b;
+    a.c = cfg->ortho.c;
+    a.eps = cfg->ortho.eps;
     a.x = x;
     a.mom = m;
     a.grad = grad;
@@ -308,23 +479,18 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
     a.mu = cfg->momentum;
     a.keep = (float)(1.0 - (double)cfg->lr * (double)cfg->weight_decay);
     a.nesterov = cfg->nesterov;
-    for (uint32_t k = 0; k < n_tensors; k++) {
-        if (rows[k] == 0 || cols[k] == 0) continue;
-        if (b.full()) {
-            rc = run_batch(b, src, kNsMuonF32, cfg->ortho, a, ws, (hipStream_t)stream);
-            if (rc) return rc;
-            b.clear();
-        }
-        NsMat q = {};
-        q.ld_in = offsets[k];
-        q.rows = rows[k];
-        q.cols = cols[k];
-        q.flags = flags[k];
-        const double ratio = flags[k] & DEDLOC_TENSOR_ADAPT ? (double)cfg->rms * sqrt((double)std::max(rows[k], cols[k])) : 1.0;
-        q.unit = (float)((double)cfg->lr * ratio);
-        b.add(q);
-    }
-    return run_batch(b, src, kNsMuonF32, cfg->ortho, a, ws, (hipStream_t)stream);
+    return in_batches(
+        true, n_tensors,
+        [&](uint32_t k, uint32_t &r, uint32_t &c) {
+            r = rows[k];
+            c = cols[k];
+        },
+        [&](uint32_t k, Batch &b) {
+            const double ratio =
+                flags[k] & DEDLOC_TENSOR_ADAPT ? (double)cfg->rms * sqrt((double)std::max(rows[k], cols[k])) : 1.0;
+            b.add(nullptr, offsets[k], nullptr, offsets[k], rows[k], cols[k], flags[k], (float)((double)cfg->lr * ratio));
+        },
+        [&](Batch &b) { return run_batch(b, p, src, kNsMuonF32, a, ws, (hipStream_t)stream); });
 }
 
 int dedloc_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_t width, uint64_t ld_table,

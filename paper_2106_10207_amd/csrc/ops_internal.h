@@ -13,57 +13,83 @@ namespace dedloc {
 // Element types, as the DEDLOC_DTYPE_* ids.
 enum Dtype : int { kF32 = 0, kFP16 = 1, kBF16 = 2 };
 
-// A launch describes at most kNsMats matrices in its arguments (56 of 64
-// bytes: 3.5 KB of the 4 KB that kernel arguments may take).
-constexpr int kNsMats = 56;
-constexpr uint32_t kNsPad = 64;      // both sides of a matrix are padded with zeros to this in the workspace
-constexpr uint32_t kNsTile = 64;     // edge of a block of the elementwise passes
+// A launch describes at most kNsWorks products in its arguments (48 bytes each,
+// 3.4 KB of the 4 KB that kernel arguments may take).
+constexpr int kNsWorks = 72;
+constexpr uint32_t kNsPad = 64;   // both sides of a matrix are padded with zeros to this in the workspace
+constexpr uint32_t kNsTile = 64;  // edge of a block of the elementwise passes
 constexpr uint32_t kNsMaxShort = 32768;
 constexpr uint32_t kNsMaxLong = 1u << 26;
 constexpr uint32_t kSumChunk = 8192;  // flat elements summed by one workgroup of the momentum pass
 
-// One matrix of a launch.  s is its shorter side, l the longer; S and L are s
-// and l rounded up to kNsPad.  Its region of the workspace, at `base` bytes:
-//   X [S][L], X^T [L][S] twice (read and written in turn), A [S][S], B [S][S]
-// in two planes (4 bytes an element).
+// A matrix has a region of the workspace.  s is its shorter side, l the longer; S
+// and L are s and l rounded up to kNsPad.  The region holds, 4 bytes an element,
+//   buffer 0: X [S][L],  1 and 2: X^T [L][S], read and written in turn,
+//   buffers 3 on: symmetric [S][S].
+constexpr uint32_t kNsSmall = 3;   // the first symmetric buffer
+constexpr uint32_t kNsSmalls = 6;  // of a matrix that is worked on in blocks of steps; 2 otherwise
+
+// The two passes before the products.
 struct NsMat {
-    uint64_t base;
-    const void *in;         // orthogonalize: the matrix
-    void *out;
-    uint64_t ld_in, ld_out;  // Muon: ld_in is the matrix' first element in the flat vector
+    uint64_t base;     // its region
+    const void *in;    // orthogonalize: the matrix
+    uint64_t ld_in;    // Muon: its first element in the flat vector
     uint32_t rows, cols;
-    uint32_t part;          // its first partial sum; the next matrix' is the end
-    uint32_t begin;         // its first workgroup in this launch
-    uint32_t flags;
-    float unit;             // Muon: lr * s_t
+    uint32_t part;     // its first partial sum; the next matrix' is the end
+    uint32_t begin;    // its first workgroup in this launch
 };
 struct NsTable {
-    NsMat m[kNsMats];
+    NsMat m[kNsWorks];
     uint32_t n;
     uint32_t parts;  // partial sums of all matrices
+};
+
+// One product of a launch, left right^T, and what becomes of it:
+enum NsKind : int {
+    kNsGram = 0,    // X X^T, symmetric
+    kNsSquare = 1,  // a I + b A + c A A, symmetric
+    kNsMul = 2,     // of two commuting symmetric matrices
+    kNsApply = 3,   // Q X: the next X and X^T
+    kNsResult = 4   // Q X: the call's result
+};
+struct NsWork {
+    uint64_t base;
+    void *out;        // kNsResult: orthogonalize's matrix
+    uint64_t ld_out;  // Muon: its first element in the flat vector
+    uint32_t rows, cols;
+    uint32_t begin;   // its first work item in this launch
+    uint32_t pieces;  // that the summed index is cut into
+    uint32_t op;      // kind | left << 4 | right << 8 | out << 12 (buffers) | decay << 16
+    float unit;       // Muon: lr * s_t
+};
+struct NsWorks {
+    NsWork w[kNsWorks];
+    uint32_t n;
 };
 
 struct NsArgs {
     char *ws;        // the regions
     double *part;    // partial sums of squares
+    float *pieces;   // sums of the items whose summed index is cut, a tile each
     float *x, *mom;  // Muon: the flat vector and the momentum
     const void *grad;
     const float *scales;
     float a, b, c, eps;
     float mu, keep;  // momentum; 1 - lr * weight_decay
     int32_t nesterov;
-    int32_t turn;    // which X^T is read (the other is written)
-    int32_t last;    // the last step: the result goes out instead of into the workspace
 };
 
 // Where prepare takes its matrix from: a dtype of orthogonalize, or the Muon
 // step's update formed from the momentum and a gradient of this codec.
 enum NsSrc : int { kNsF32 = 0, kNsFP16 = 1, kNsBF16 = 2, kNsMuonF32 = 3, kNsMuonFP16 = 4, kNsMuonI8 = 5 };
-enum NsPhase : int { kNsGram = 0, kNsSquare = 1, kNsApply = 2 };
 
 hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
 hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
-hipError_t launch_ns_product(int phase, int out, bool wide, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s);
+// out: the dtype of results, kNsMuonF32 for the update of the parameters.  edge: of
+// the tiles, 64 or 128.  The works whose summed index is cut come first in the
+// table; join takes their number of tiles.
+hipError_t launch_ns_product(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t items, hipStream_t s);
+hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s);
 
 // ------------------------------------------------ embedding and its gradient
 

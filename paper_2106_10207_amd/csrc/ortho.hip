@@ -3,71 +3,67 @@
 //
 // With s the shorter side of a matrix and l the longer, X [s][l] is taken
 // towards the nearest matrix with orthogonal rows by
-//   X0 = G / (|G|_F + eps),   A = X X^T,   B = b A + c A^2,   X <- a X + B X,
-// three products a step on the matrix cores.  A singular value far below 1
-// grows by a (3.4) in a step, and a rounding error of X with it, so five
-// steps multiply it by up to a^5 = 485: operands of 11 bits (fp16) lose 1e-2 of
-// the result of an ill-conditioned gradient, 8 bits (bf16) 1e-1.  So every
-// operand is held in two fp16 planes, hi + lo, 22 bits, and a product takes
-// three of them,
+//   X0 = G / (|G|_F + eps),   A = X X^T,   M = a I + b A + c A^2,   X <- M X.
+// Everything that multiplies X is a polynomial of A, symmetric, and commutes, so
+// n steps can be taken on the s x s side, A <- M A M, with one Gram matrix before
+// them and one product Q X, Q = M_n ... M_1, after: 3 s^2 l + (4 n - 3) s^3 multiply-adds
+// for n (3 s^2 l + s^3), symmetric products counted half.
+//
+// Precision.  A singular value far below 1 grows by a (3.4) in a step, and a
+// rounding error of X with it, so five steps multiply it by up to a^5 = 485:
+// operands of 11 bits (fp16) lose 1e-2 of the result of an ill-conditioned
+// gradient, 8 bits (bf16) 1e-1.  So every operand is held in two fp16 planes,
+// hi + lo, 22 bits, and a product takes three of them,
 //   hi hi' + hi lo' + lo hi'
-// in fp32 accumulators.  X is stored times 2^12, A and B times 2^10: their entries
-// are at most about 1.3 and 3, and the low planes of entries of the usual
-// size (1 / sqrt(s l)) then stay in fp16's normal range.
+// in fp32 accumulators, which leaves errors of 5e-7 to 2e-6 of the result (fp32 products:
+// 1e-6 to 4e-6).  An error of A grows by a^2 in a step on the s x s side: three
+// steps from X0 and two from later X keep that; five lose it altogether.
+// X is stored times 2^12, the symmetric matrices times 2^8: |X| stays below 1.3 and
+// |Q| below a^3 = 41, and the low planes of entries of the usual size (1 / sqrt(s l))
+// stay in fp16's normal range.
 //
 // Layout of a two-plane matrix: panels of 32 columns, in a panel the rows one after
 // the other, 128 bytes each, 64 of hi then 64 of lo.  A turn of a product's loop
 // reads a tile's rows of one panel, one piece of memory.  (Row by row, the rows
 // of a tile would lie 4 l bytes apart, for most matrices a power of two, and so
 // on one of the L2's channels.)
-// Both factors of every product have the summed index along their rows (A and
-// B are symmetric; X^T is kept beside X).
+// Both factors of every product have the summed index along their rows: the
+// small matrices are symmetric, and X^T is kept beside X.
 #include <type_traits>
 
 #include "ops_internal.h"
 
-#ifndef NS_WIDE
-#define NS_WIDE 2, 4, 2
-#endif
-#ifndef NS_SMALL
-#define NS_SMALL 1, 1, 4
-#endif
 namespace dedloc {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
 constexpr float kXScale = 4096.0f;  // of X
-constexpr float kAScale = 1024.0f;  // of A and B
+constexpr float kAScale = 256.0f;   // of the symmetric matrices
 
 struct Sides {
     uint32_t s, l, S, L;
     bool tall;  // rows > cols: X is the transpose
 };
-__host__ __device__ inline Sides sides(const NsMat &m) {
+__device__ inline Sides sides(uint32_t rows, uint32_t cols) {
     Sides d;
-    d.tall = m.rows > m.cols;
-    d.s = d.tall ? m.cols : m.rows;
-    d.l = d.tall ? m.rows : m.cols;
+    d.tall = rows > cols;
+    d.s = d.tall ? cols : rows;
+    d.l = d.tall ? rows : cols;
     d.S = (d.s + kNsPad - 1) / kNsPad * kNsPad;
     d.L = (d.l + kNsPad - 1) / kNsPad * kNsPad;
     return d;
 }
 
-// The parts of a matrix' region.
-__device__ inline char *at_x(const NsArgs &a, const NsMat &m) { return a.ws + m.base; }
-__device__ inline char *at_xt(const NsArgs &a, const NsMat &m, const Sides &d, int k) {
-    return a.ws + m.base + (uint64_t)(1 + k) * d.S * d.L * 4;
-}
-__device__ inline char *at_a(const NsArgs &a, const NsMat &m, const Sides &d) {
-    return a.ws + m.base + (uint64_t)3 * d.S * d.L * 4;
-}
-__device__ inline char *at_b(const NsArgs &a, const NsMat &m, const Sides &d) {
-    return at_a(a, m, d) + (uint64_t)d.S * d.S * 4;
+// A buffer of a matrix' region.
+__device__ inline char *buffer(const NsArgs &a, uint64_t base, const Sides &d, uint32_t k) {
+    const uint64_t big = (uint64_t)d.S * d.L * 4, small = (uint64_t)d.S * d.S * 4;
+    return a.ws + base + (k < kNsSmall ? k * big : kNsSmall * big + (k - kNsSmall) * small);
 }
 // Byte offset of element (i, j) of a matrix of `rows` rows: its hi; lo is 64 bytes on.
 __device__ inline uint64_t at_planes(uint32_t i, uint32_t j, uint32_t rows) {
@@ -79,10 +75,11 @@ __device__ inline void split(float v, _Float16 &hi, _Float16 &lo) {
     lo = (_Float16)(v - (float)hi);
 }
 
-// The matrix that workgroup `wg` belongs to.
-__device__ inline uint32_t find(const NsTable &t, uint32_t wg) {
+// The entry of a table that workgroup `wg` belongs to.
+template <typename T>
+__device__ inline uint32_t find(const T *m, uint32_t n, uint32_t wg) {
     uint32_t k = 0;
-    while (k + 1 < t.n && t.m[k + 1].begin <= wg) k++;
+    while (k + 1 < n && m[k + 1].begin <= wg) k++;
     return k;
 }
 
@@ -122,7 +119,7 @@ __device__ inline double block_sum(double v) {
 // Sums of squares in 64 bits, one per block of kNsTile rows and columns.
 template <int SRC>
 __global__ __launch_bounds__(256) void ns_sum_kernel(NsTable t, NsArgs a) {
-    const NsMat &m = t.m[find(t, blockIdx.x)];
+    const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin, across = (m.cols + kNsTile - 1) / kNsTile;
     const uint32_t r0 = k / across * kNsTile, col = k % across * kNsTile + threadIdx.x % kNsTile;
     double sum = 0.0;
@@ -139,7 +136,7 @@ __global__ __launch_bounds__(256) void ns_sum_kernel(NsTable t, NsArgs a) {
 // kSumChunk elements.
 template <int SRC>
 __global__ __launch_bounds__(256) void muon_sum_kernel(NsTable t, NsArgs a) {
-    const NsMat &m = t.m[find(t, blockIdx.x)];
+    const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin;
     const uint64_t n = (uint64_t)m.rows * m.cols, end = (uint64_t)(k + 1) * kSumChunk < n ? (uint64_t)(k + 1) * kSumChunk : n;
     double sum = 0.0;
@@ -158,9 +155,9 @@ __global__ __launch_bounds__(256) void muon_sum_kernel(NsTable t, NsArgs a) {
 // block of 64 x 64 of the matrix as it is stored.
 template <int SRC>
 __global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
-    const uint32_t q = find(t, blockIdx.x);
+    const uint32_t q = find(t.m, t.n, blockIdx.x);
     const NsMat &m = t.m[q];
-    const Sides d = sides(m);
+    const Sides d = sides(m.rows, m.cols);
     double sum = 0.0;
     const uint32_t end = q + 1 < t.n ? t.m[q + 1].part : t.parts;
     for (uint32_t i = m.part + threadIdx.x; i < end; i += 256) sum += a.part[i];
@@ -177,7 +174,7 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
     }
     __syncthreads();
     // the block as stored goes to X (wide) or X^T (tall), its transpose to the other
-    char *straight = d.tall ? at_xt(a, m, d, 0) : at_x(a, m), *turned = d.tall ? at_x(a, m) : at_xt(a, m, d, 0);
+    char *straight = buffer(a, m.base, d, d.tall), *turned = buffer(a, m.base, d, !d.tall);
     const uint32_t h_straight = d.tall ? d.L : d.S, h_turned = d.tall ? d.S : d.L;
     for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
         _Float16 hi, lo;
@@ -192,72 +189,141 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
     }
 }
 
-// A block's results: row i, columns j0 + 8 g + (0 to 3) are acc[4 g] to
-// acc[4 g + 3].  diagonal: the block lies on a symmetric result's diagonal.
-template <int PHASE, int OUT>
-__device__ inline void ns_finish(const NsMat &m, const Sides &d, const NsArgs &a, uint32_t i, uint32_t j0, bool diagonal,
-                                 const f32x16 &acc) {
+// Orders what one lane of a wave wrote to LDS before what another reads.
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+template <int N, typename T>
+struct Vec {
+    T v[N];
+} __attribute__((packed, aligned(sizeof(T))));
+
+constexpr uint32_t kTurnPitch = 36;  // words of a row of a block that is turned in LDS
+
+// What a block of 32 x 32 (rows i0, columns j0 on) of a product becomes.  The lane's
+// row is i = i0 + lane % 32; acc[4 g + e] belongs to column j0 + 8 g + 4 (lane / 32) + e.
+// turn: 32 * kTurnPitch words of the wave's own in LDS, through which the block goes
+// to its transposed place in whole pieces of 32 bytes.
+template <int OUT>
+__device__ inline void ns_finish(const NsWork &m, const Sides &d, const NsArgs &a, uint32_t i0, uint32_t j0, const f32x16 &acc,
+                                 uint32_t *turn) {
+    const uint32_t lane = threadIdx.x & 63, il = lane % 32, i = i0 + il, kind = m.op & 15;
+    if (kind == kNsResult) {
+        if (i >= d.s) return;
+        const uint64_t ld = OUT == kNsMuonF32 ? m.cols : m.ld_out;
+        const uint64_t step = d.tall ? ld : 1;  // from column j to the next
 #pragma unroll
-    for (uint32_t g = 0; g < 4; g++) {
-        const uint32_t j = j0 + 8 * g;
-        float v[4];
-        f16x4 hi, lo;
-        if (PHASE == kNsGram) {
-            for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (kAScale / (kXScale * kXScale));
-        } else {
-            const char *old = (PHASE == kNsSquare ? at_a(a, m, d) : at_x(a, m)) + at_planes(i, j, d.S);
-            hi = *(const f16x4 *)old;
-            lo = *(const f16x4 *)(old + 64);
-            for (int e = 0; e < 4; e++) {
-                const float o = (float)hi[e] + (float)lo[e];
-                v[e] = PHASE == kNsSquare ? fmaf(a.b, o, a.c * (acc[4 * g + e] * (1.0f / kAScale)))
-                                          : fmaf(a.a, o, acc[4 * g + e] * (1.0f / kAScale));
-            }
-        }
-        if (PHASE == kNsApply && a.last) {
-            for (int e = 0; e < 4; e++) {
-                if (i >= d.s || j + e >= d.l) continue;
-                const uint32_t row = d.tall ? j + e : i, col = d.tall ? i : j + e;
-                const float o = v[e] * (1.0f / kXScale);
-                if (OUT == kNsMuonF32) {
-                    float *x = a.x + m.ld_in + (uint64_t)row * m.cols + col;
-                    *x = fmaf(-m.unit, o, ((m.flags & 1) ? a.keep : 1.0f) * *x);
+        for (uint32_t g = 0; g < 4; g++) {
+            const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
+            if (j >= d.l) break;
+            const uint32_t n = min(4u, d.l - j);
+            const uint64_t at = d.tall ? j * ld + i : i * ld + j;
+            float v[4];
+            for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (1.0f / (kAScale * kXScale));
+            if constexpr (OUT == kNsMuonF32) {
+                float *x = a.x + m.ld_out + at;
+                const float keep = (m.op >> 16 & 1) ? a.keep : 1.0f;
+                if (!d.tall && n == 4) {
+                    Vec<4, float> q = *(const Vec<4, float> *)x;
+                    for (int e = 0; e < 4; e++) q.v[e] = fmaf(-m.unit, v[e], keep * q.v[e]);
+                    *(Vec<4, float> *)x = q;
                 } else {
-                    const uint64_t at = (uint64_t)row * m.ld_out + col;
-                    if (OUT == kNsF32) ((float *)m.out)[at] = o;
-                    if (OUT == kNsFP16) ((_Float16 *)m.out)[at] = (_Float16)o;
-                    if (OUT == kNsBF16) ((__bf16 *)m.out)[at] = (__bf16)o;
+                    for (uint32_t e = 0; e < n; e++) x[e * step] = fmaf(-m.unit, v[e], keep * x[e * step]);
+                }
+            } else {
+                typedef std::conditional_t<OUT == kNsF32, float, std::conditional_t<OUT == kNsFP16, _Float16, __bf16>> T;
+                T *to = (T *)m.out + at;
+                if (!d.tall && n == 4) {
+                    Vec<4, T> q;
+                    for (int e = 0; e < 4; e++) q.v[e] = (T)v[e];
+                    *(Vec<4, T> *)to = q;
+                } else {
+                    for (uint32_t e = 0; e < n; e++) to[e * step] = (T)v[e];
                 }
             }
-            continue;
+        }
+        return;
+    }
+    const float scale = kind == kNsGram ? kAScale / (kXScale * kXScale) : 1.0f / kAScale;
+    char *to = buffer(a, m.base, d, kind == kNsApply ? 0 : m.op >> 12 & 15) + at_planes(i, j0, d.S);
+    const char *old = buffer(a, m.base, d, m.op >> 4 & 15) + at_planes(i, j0, d.S);
+    wave_order();  // the block before has left `turn`
+#pragma unroll
+    for (uint32_t g = 0; g < 4; g++) {
+        const uint32_t jl = 8 * g + 4 * (lane / 32);
+        float v[4];
+        f16x4 hi, lo;
+        for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * scale;
+        if (kind == kNsSquare) {
+            hi = *(const f16x4 *)(old + jl * 2);
+            lo = *(const f16x4 *)(old + jl * 2 + 64);
+            for (int e = 0; e < 4; e++) {
+                v[e] = fmaf(a.b, (float)hi[e] + (float)lo[e], a.c * v[e]);
+                if (i == j0 + jl + e) v[e] = fmaf(a.a, kAScale, v[e]);
+            }
         }
         for (int e = 0; e < 4; e++) {
             _Float16 h, w;
             split(v[e], h, w);
             hi[e] = h;
             lo[e] = w;
+            turn[(jl + e) * kTurnPitch + il] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, w) << 16;
         }
-        char *to = (PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_x(a, m)) +
-                   at_planes(i, j, d.S);
-        *(f16x4 *)to = hi;
-        *(f16x4 *)(to + 64) = lo;
-        if (!diagonal) {  // X^T, or the upper triangle
-            char *base = PHASE == kNsGram ? at_a(a, m, d) : PHASE == kNsSquare ? at_b(a, m, d) : at_xt(a, m, d, 1 - a.turn);
-            for (int e = 0; e < 4; e++) {
-                _Float16 *p = (_Float16 *)(base + at_planes(j + e, i, PHASE == kNsApply ? d.L : d.S));
-                p[0] = hi[e];
-                p[32] = lo[e];
-            }
+        *(f16x4 *)(to + jl * 2) = hi;
+        *(f16x4 *)(to + jl * 2 + 64) = lo;
+    }
+    if (kind != kNsApply && i0 == j0) return;
+    // the transpose: X^T, or the upper triangle.  The lane has row j0 + lane % 32 and 16 of its columns.
+    wave_order();
+    u32x4 q[4];
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++) q[k] = *(const u32x4 *)(turn + il * kTurnPitch + 16 * (lane / 32) + 4 * k);
+    to = buffer(a, m.base, d, m.op >> 12 & 15) + at_planes(j0 + il, i0 + 16 * (lane / 32), kind == kNsApply ? d.L : d.S);
+#pragma unroll
+    for (uint32_t k = 0; k < 2; k++) {
+        u32x4 hi, lo;
+#pragma unroll
+        for (uint32_t w = 0; w < 4; w++) {
+            const uint32_t x = q[2 * k + w / 2][w % 2 * 2], y = q[2 * k + w / 2][w % 2 * 2 + 1];
+            hi[w] = (x & 0xffffu) | y << 16;
+            lo[w] = x >> 16 | (y & 0xffff0000u);
         }
+        *(u32x4 *)(to + 16 * k) = hi;
+        *(u32x4 *)(to + 64 + 16 * k) = lo;
     }
 }
 
-#ifndef NS_WIDE
-#define NS_WIDE 2, 4, 1
-#endif
-#ifndef NS_SMALL
-#define NS_SMALL 1, 1, 4
-#endif
+// The tile of a product's work item: tiles of the same piece of the summed index
+// follow one another.
+struct Tile {
+    uint32_t ti, tj, piece, tiles;
+};
+__device__ inline Tile tile_at(const NsWork &m, const Sides &d, uint32_t k, uint32_t T) {
+    Tile t;
+    const uint32_t down = (d.S + T - 1) / T, across = (d.L + T - 1) / T;
+    const bool full = (m.op & 15) >= kNsApply;
+    t.tiles = full ? down * across : down * (down + 1) / 2;
+    t.piece = k / t.tiles;
+    k %= t.tiles;
+    if (full) {
+        // bands of 8 tile rows, column by column: a tile's neighbours in time share its factors
+        const uint32_t band = k / (8 * across), high = min(8u, down - band * 8);
+        k -= band * 8 * across;
+        t.ti = band * 8 + k % high;
+        t.tj = k / high;
+    } else {  // the lower triangle of a symmetric result
+        uint32_t u = (uint32_t)((sqrtf(8.0f * k + 1.0f) - 1.0f) * 0.5f);
+        while ((u + 1) * (u + 2) / 2 <= k) u++;
+        while (u * (u + 1) / 2 > k) u--;
+        t.ti = u;
+        t.tj = k - u * (u + 1) / 2;
+    }
+    return t;
+}
+
 typedef __attribute__((address_space(3))) void *LdsPtr;
 
 // Waits until at most N of this wave's loads are in flight and its LDS reads are done, then for the workgroup's other
@@ -272,9 +338,9 @@ __device__ inline void arrived() {
 constexpr int kRawBuffer = 0x00020000;  // descriptor of untyped bytes
 constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // classes of sched_group_barrier
 
-// One tile of a product of a step: 64 WI rows and 64 WJ columns, a quarter per
-// wave, WI x WJ blocks of 32 x 32.  OUT: the dtype of the result of the last step's
-// apply, or kNsMuonF32 for the update of the parameters.
+// One tile of a product of a step: 64 W rows and columns, a quarter per wave, W x W
+// blocks of 32 x 32, over a piece of the summed index.  OUT: the dtype of a result, or
+// kNsMuonF32 for the update of the parameters.
 //
 // A turn of the loop takes 32 of the summed index, 128 bytes of a row of either
 // factor.  They go from memory into one of NS stages of LDS without passing
@@ -284,61 +350,47 @@ constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // class
 // lanes of a read, one row each, meet all 64 banks (with r % 8 two rows met in a bank
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
-template <int PHASE, int OUT, int WI, int WJ, int NS>
-__global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a) {
-    constexpr uint32_t TI = 64 * WI, TJ = 64 * WJ, R = WJ / WI;
-    // workgroups go round the 8 XCDs: give each a contiguous range of tiles
+template <int OUT, int W, int NS>
+__global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a) {
+    constexpr uint32_t T = 64 * W;
+    // workgroups go round the 8 XCDs: give each a contiguous range of items
     const uint32_t per = gridDim.x / 8, odd = gridDim.x % 8, xcd = blockIdx.x % 8;
     const uint32_t wg = xcd * per + min(xcd, odd) + blockIdx.x / 8;
-    const NsMat &m = t.m[find(t, wg)];
-    const Sides d = sides(m);
-    uint32_t k = wg - m.begin, ti, tj;
-    if (PHASE == kNsApply) {
-        // bands of 8 tile rows, column by column: a tile's neighbours in time share its factors
-        const uint32_t across = (d.L + TJ - 1) / TJ, down = (d.S + TI - 1) / TI;
-        const uint32_t band = k / (8 * across), high = min(8u, down - band * 8);
-        k -= band * 8 * across;
-        ti = band * 8 + k % high;
-        tj = k / high;
-    } else {  // the lower triangle of a symmetric result: tile rows R u to R u + R - 1 have u + 1 tiles
-        uint32_t u = (uint32_t)((sqrtf(8.0f / R * k + 1.0f) - 1.0f) * 0.5f);
-        while (R * (u + 1) * (u + 2) / 2 <= k) u++;
-        while (R * u * (u + 1) / 2 > k) u--;
-        k -= R * u * (u + 1) / 2;
-        ti = R * u + k / (u + 1);
-        tj = k % (u + 1);
-    }
-    const uint32_t K = PHASE == kNsGram ? d.L : d.S;  // the summed index
-    const char *left = PHASE == kNsGram ? at_x(a, m) : PHASE == kNsSquare ? at_a(a, m, d) : at_b(a, m, d);
-    const char *right = PHASE == kNsApply ? at_xt(a, m, d, a.turn) : left;
-    const uint32_t left_rows = d.S, right_rows = PHASE == kNsApply ? d.L : d.S;
+    const NsWork &m = t.w[find(t.w, t.n, wg)];
+    const Sides d = sides(m.rows, m.cols);
+    const Tile tile = tile_at(m, d, wg - m.begin, T);
+    const uint32_t i0 = tile.ti * T, j0 = tile.tj * T, kind = m.op & 15;
+    const uint32_t K = kind == kNsGram ? d.L : d.S;  // the summed index
+    const char *left = buffer(a, m.base, d, m.op >> 4 & 15), *right = buffer(a, m.base, d, m.op >> 8 & 15);
+    const uint32_t left_rows = d.S, right_rows = kind >= kNsApply ? d.L : d.S;
 
-    constexpr uint32_t kStage = (TI + TJ) * 128;
+    constexpr uint32_t kStage = 2 * T * 128;
     // one array per stage: the compiler then knows which loads a read has to wait for
     __shared__ __align__(1024) char lds0[kStage], lds1[NS > 1 ? kStage : 16], lds2[NS > 2 ? kStage : 16],
         lds3[NS > 3 ? kStage : 16];
     auto stage = [&](uint32_t k) { return k == 0 ? lds0 : k == 1 ? lds1 : k == 2 ? lds2 : lds3; };
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wi = wave / 2 * (32 * WI), wj = wave % 2 * (32 * WJ);
+    const uint32_t wi = wave / 2 * (32 * W), wj = wave % 2 * (32 * W);
     // A load of a wave takes 8 rows.  The panels' rows past the matrix' end lie beyond the descriptor's end and read as 0.
-    constexpr uint32_t kLoads = 2 * (WI + WJ);
+    constexpr uint32_t kLoads = 4 * W;
     const uint32_t from = wave * 1024 + (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
     const uint64_t left_panel = (uint64_t)left_rows * 128, right_panel = (uint64_t)right_rows * 128;
-    const uint32_t left_end = (left_rows - ti * TI) * 128, right_end = (right_rows - tj * TJ) * 128;
-    left += (uint64_t)ti * TI * 128;
-    right += (uint64_t)tj * TJ * 128;
-    const uint32_t panels = K / 32;
+    const uint32_t left_end = (left_rows - i0) * 128, right_end = (right_rows - j0) * 128;
+    const uint32_t first = (uint64_t)(K / 32) * tile.piece / m.pieces;
+    const uint32_t panels = (uint32_t)((uint64_t)(K / 32) * (tile.piece + 1) / m.pieces) - first;
+    left += (uint64_t)i0 * 128 + first * left_panel;
+    right += (uint64_t)j0 * 128 + first * right_panel;
     auto fetch = [&](char *lds, uint32_t panel) {
         const uint64_t p = min(panel, panels - 1);  // past the end the last once more: the loop then counts its loads
         const auto lrows = __builtin_amdgcn_make_buffer_rsrc((void *)(left + p * left_panel), 0, left_end, kRawBuffer);
         const auto rrows = __builtin_amdgcn_make_buffer_rsrc((void *)(right + p * right_panel), 0, right_end, kRawBuffer);
 #pragma unroll
         for (uint32_t q = 0; q < kLoads; q++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(q < 2 * WI ? lrows : rrows, (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16,
-                                                     from, (q < 2 * WI ? q : q - 2 * WI) * 4096, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(q < 2 * W ? lrows : rrows, (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16,
+                                                     from, q % (2 * W) * 4096, 0, 0);
     };
-    f32x16 acc[WI][WJ] = {};
-    f16x8 l[2][WI][2], r[2][WJ][2];  // [half of the turn][block][plane]
+    f32x16 acc[W][W] = {};
+    f16x8 l[2][W][2], r[2][W][2];  // [half of the turn][block][plane]
     auto read = [&](const char *lds, uint32_t h) {
         auto one = [&](uint32_t row, uint32_t p) {
             const uint32_t c = p * 4 + h * 2 + lane / 32;
@@ -347,18 +399,19 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a)
 #pragma unroll
         for (uint32_t p = 0; p < 2; p++) {
 #pragma unroll
-            for (uint32_t b = 0; b < WI; b++) l[h][b][p] = one(wi + b * 32 + lane % 32, p);
-#pragma unroll
-            for (uint32_t b = 0; b < WJ; b++) r[h][b][p] = one(TI + wj + b * 32 + lane % 32, p);
+            for (uint32_t b = 0; b < W; b++) {
+                l[h][b][p] = one(wi + b * 32 + lane % 32, p);
+                r[h][b][p] = one(T + wj + b * 32 + lane % 32, p);
+            }
         }
     };
     auto multiply = [&](uint32_t h) {
 #pragma unroll
         for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
 #pragma unroll
-            for (uint32_t i = 0; i < WI; i++)
+            for (uint32_t i = 0; i < W; i++)
 #pragma unroll
-                for (uint32_t j = 0; j < WJ; j++)
+                for (uint32_t j = 0; j < W; j++)
                     // the right factor's rows first: a lane then holds four consecutive columns of one row
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[h][j][p == 1], l[h][i][p == 0], acc[i][j], 0, 0, 0);
     };
@@ -371,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a)
         multiply(0);
 #pragma unroll
         for (uint32_t q = 0; q < kLoads; q++) {
-            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * WI * WJ / kLoads, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * W * W / kLoads, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
         }
         // the next stage is there, and all have read this one, which the next loads fill
@@ -383,7 +436,7 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a)
         multiply(1);
 #pragma unroll
         for (uint32_t q = 0; q < kLoads; q++) {
-            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * WI * WJ / kLoads, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * W * W / kLoads, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedLoad, 1, 0);
         }
@@ -396,15 +449,63 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsTable t, NsArgs a)
     for (uint32_t k = 0; k + 1 < NS; k++)
         if (panel + k < panels) turn(k, panel + k);
     arrived<0>();  // no load may arrive in LDS that another workgroup has by then
+    if (m.pieces > 1) {  // the sums of the piece, joined by the next launch
+        float *to = a.pieces + (uint64_t)wg * (T * T) + wave * (T * T / 4) + lane * 4;
 #pragma unroll
-    for (uint32_t bi = 0; bi < WI; bi++)
+        for (uint32_t b = 0; b < W * W; b++)
 #pragma unroll
-        for (uint32_t bj = 0; bj < WJ; bj++) {
-            const uint32_t i0 = ti * TI + wi + bi * 32, j0 = tj * TJ + wj + bj * 32;
-            // of a symmetric result the blocks above the diagonal are written as the mirror of those below
-            if (i0 < left_rows && j0 < right_rows && (PHASE == kNsApply || j0 <= i0))
-                ns_finish<PHASE, OUT>(m, d, a, i0 + lane % 32, j0 + 4 * (lane / 32), PHASE != kNsApply && i0 == j0, acc[bi][bj]);
-        }
+            for (uint32_t g = 0; g < 4; g++)
+                *(f32x4 *)(to + (b * 4 + g) * 256) = *((const f32x4 *)&acc[b / W][b % W] + g);
+        return;
+    }
+    uint32_t *turn_lds = (uint32_t *)(stage(wave / 2) + wave % 2 * (32 * kTurnPitch * 4));
+#pragma unroll
+    for (uint32_t b = 0; b < W * W; b++) {
+        const uint32_t i = i0 + wi + b / W * 32, j = j0 + wj + b % W * 32;
+        // of a symmetric result the blocks above the diagonal are written as the mirror of those below
+        if (i < left_rows && j < right_rows && (kind >= kNsApply || j <= i))
+            ns_finish<OUT>(m, d, a, i, j, acc[b / W][b % W], turn_lds);
+    }
+}
+
+// A block of 32 x 32 of a product whose summed index was cut: a workgroup adds up its pieces, a quarter of them
+// per wave, in an order that only their number decides.  One workgroup per block of each tile.
+template <int OUT, int W>
+__global__ __launch_bounds__(256) void ns_join_kernel(NsWorks t, NsArgs a) {
+    constexpr uint32_t T = 64 * W, kBlocks = 4 * W * W;
+    // the table counts items, a work's tiles once for every piece
+    uint32_t k = blockIdx.x / kBlocks, q = 0;
+    const uint32_t block = blockIdx.x % kBlocks;
+    Sides d;
+    Tile tile;
+    for (;; q++) {
+        d = sides(t.w[q].rows, t.w[q].cols);
+        tile = tile_at(t.w[q], d, k, T);
+        if (k < tile.tiles) break;
+        k -= tile.tiles;
+    }
+    const NsWork &m = t.w[q];
+    const bool full = (m.op & 15) >= kNsApply;
+    const uint32_t wave_of = block / (W * W), b = block % (W * W), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t i = tile.ti * T + wave_of / 2 * (32 * W) + b / W * 32, j = tile.tj * T + wave_of % 2 * (32 * W) + b % W * 32;
+    if (i >= d.S || j >= (full ? d.L : d.S) || (!full && j > i)) return;
+    const float *from = a.pieces + (uint64_t)(m.begin + k) * (T * T) + wave_of * (T * T / 4) + b * 1024 + lane * 4;
+    f32x4 sum[4] = {};
+    for (uint32_t p = m.pieces * wave / 4; p < m.pieces * (wave + 1) / 4; p++)
+#pragma unroll
+        for (uint32_t g = 0; g < 4; g++) sum[g] += *(const f32x4 *)(from + (uint64_t)p * tile.tiles * (T * T) + g * 256);
+    __shared__ f32x4 part[3][4][64];
+    __shared__ __align__(16) uint32_t turn[32 * kTurnPitch];
+    if (wave > 0)
+#pragma unroll
+        for (uint32_t g = 0; g < 4; g++) part[wave - 1][g][lane] = sum[g];
+    __syncthreads();
+    if (wave > 0) return;
+    f32x16 acc;
+#pragma unroll
+    for (uint32_t g = 0; g < 4; g++)
+        *((f32x4 *)&acc + g) = (sum[g] + part[0][g][lane]) + (part[1][g][lane] + part[2][g][lane]);
+    ns_finish<OUT>(m, d, a, i, j, acc, turn);
 }
 
 // ---------------------------------------------------------------- launchers
@@ -434,27 +535,37 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
 }
 
 namespace {
-template <int WI, int WJ, int NS>
-void product(int phase, int out, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
-    if (phase == kNsGram) {
-        ns_product_kernel<kNsGram, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a);
-    } else if (phase == kNsSquare) {
-        ns_product_kernel<kNsSquare, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a);
-    } else {
-        switch (out) {
-            case kNsF32: ns_product_kernel<kNsApply, kNsF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsFP16: ns_product_kernel<kNsApply, kNsFP16, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
-            case kNsBF16: ns_product_kernel<kNsApply, kNsBF16, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
-            default: ns_product_kernel<kNsApply, kNsMuonF32, WI, WJ, NS><<<groups, 256, 0, s>>>(t, a); break;
-        }
+template <int W, int NS>
+void product(int out, const NsWorks &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    switch (out) {
+        case kNsF32: ns_product_kernel<kNsF32, W, NS><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsFP16: ns_product_kernel<kNsFP16, W, NS><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsBF16: ns_product_kernel<kNsBF16, W, NS><<<groups, 256, 0, s>>>(t, a); break;
+        default: ns_product_kernel<kNsMuonF32, W, NS><<<groups, 256, 0, s>>>(t, a); break;
+    }
+}
+template <int W>
+void join(int out, const NsWorks &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    switch (out) {
+        case kNsF32: ns_join_kernel<kNsF32, W><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsFP16: ns_join_kernel<kNsFP16, W><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsBF16: ns_join_kernel<kNsBF16, W><<<groups, 256, 0, s>>>(t, a); break;
+        default: ns_join_kernel<kNsMuonF32, W><<<groups, 256, 0, s>>>(t, a); break;
     }
 }
 }  // namespace
 
-// wide: tiles of 128 x 256, else of 64 x 64 (what `groups` and the table count)
-hipError_t launch_ns_product(int phase, int out, bool wide, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
-    if (wide) product<NS_WIDE>(phase, out, t, a, groups, s);
-    else product<NS_SMALL>(phase, out, t, a, groups, s);
+// Two workgroups of either kind fit a CU (64 KB of LDS each): big tiles with one turn of loads in flight beside the one
+// worked on, small ones, whose turns are short, with three.
+hipError_t launch_ns_product(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t items, hipStream_t s) {
+    if (edge == 128) product<2, 2>(out, t, a, items, s);
+    else product<1, 4>(out, t, a, items, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
+    if (edge == 128) join<2>(out, t, a, tiles * 16, s);
+    else join<1>(out, t, a, tiles * 4, s);
     return hipGetLastError();
 }
 

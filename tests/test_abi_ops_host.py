@@ -52,8 +52,11 @@ def test_orthogonalize_refusals():
 def test_orthogonalize_workspace():
     lib = D.load()
     one = lib.dedloc_orthogonalize_workspace_bytes(mats((A, A, 300, 300, 200, 300)), 1)
-    # X, two transposes, A and B at 4 bytes an element, both sides padded
-    assert 4 * (3 * 200 * 300 + 2 * 200 * 200) <= one <= 8 * (3 * 256 * 320 + 2 * 256 * 256)
+    # X, two transposes and two squares at 4 bytes an element, both sides padded; room for the sums of cut products
+    assert 4 * (3 * 200 * 300 + 2 * 200 * 200) <= one <= 8 * (3 * 256 * 320 + 2 * 256 * 256) + (4 << 20)
+    # blocks of steps take four squares more
+    wide = lib.dedloc_orthogonalize_workspace_bytes(mats((A, A, 4096, 4096, 1024, 4096)), 1)
+    assert 4 * (3 * 1024 * 4096 + 6 * 1024 * 1024) <= wide <= 8 * (3 * 1024 * 4096 + 6 * 1024 * 1024)
     many = mats(*[(A, A, 300, 300, 200, 300)] * 200)
     # worked on in batches: 200 take no more than some of them
     assert one < lib.dedloc_orthogonalize_workspace_bytes(many, 200) < 100 * one

@@ -67,7 +67,8 @@ def check(out, g, **kw):
 
 
 SHAPES = [(1, 1), (1, 2), (1, 3001), (2, 128), (128, 2), (7, 5), (31, 33), (63, 65), (64, 64), (65, 63), (96, 130),
-          (128, 128), (129, 127), (147, 64), (200, 1031), (1031, 200), (257, 513), (576, 64), (40, 20000)]
+          (128, 128), (129, 127), (147, 64), (200, 1031), (1031, 200), (257, 513), (576, 64), (40, 20000),
+          (520, 1700), (1700, 520)]  # the last two in blocks of steps
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
@@ -103,16 +104,17 @@ def test_many_at_strides(dtype, seed):
 
 @pytest.mark.parametrize("shape", [(70, 300), (300, 70)])
 def test_in_place_and_same_bits(shape):
-    """In place, beside other matrices, twice, on a workspace of any contents: the same bits."""
+    """In place, twice, on a workspace of any contents: the same bits."""
     g = up(matrix(*shape, seed=3), torch.float32)
-    first = D.dedloc_orthogonalize([g])[0]
     other = up(matrix(33, 500, seed=4), torch.float32)
     call = D.OrthogonalizeCall([other, g], [torch.empty_like(other), torch.empty_like(g)])
+    first = [o.clone() for o in call()]
     for fill in (0, 255, 127):
         call.ws.fill_(fill)
-        assert torch.equal(call()[1], first)
-    D.OrthogonalizeCall([g])()
-    assert torch.equal(g, first)
+        for o, f in zip(call(), first):
+            assert torch.equal(o, f)
+    D.OrthogonalizeCall([other, g])()
+    assert torch.equal(other, first[0]) and torch.equal(g, first[1])
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
@@ -122,6 +124,16 @@ def test_steps_and_coefficients(steps):
     out = D.dedloc_orthogonalize([g], cfg=D.ortho_cfg(*abc, eps=1e-3, steps=steps))[0]
     # the norm's float eps is what the library is given
     check(out, g, steps=steps, abc=abc, eps=float(np.float32(1e-3)))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6, 9])
+@pytest.mark.parametrize("a", [3.4445, 1.5, 3.508])
+def test_blocks_of_steps(steps, a):
+    """A matrix that is worked on in blocks of steps (of up to three, fewer for a large a) beside one that is not."""
+    abc = {3.4445: ABC, 1.5: (1.5, -0.5, 0.0), 3.508: (3.508, -5.362, 2.515)}[a]
+    g = [up(matrix(*s, seed=steps), torch.float32) for s in ((512, 1600), (1600, 512), (70, 200))]
+    for o, m in zip(D.dedloc_orthogonalize(g, cfg=D.ortho_cfg(*abc, steps=steps)), g):
+        check(o, m, steps=steps, abc=abc)
 
 
 @pytest.mark.parametrize("scale", [1e-15, 1e15])
