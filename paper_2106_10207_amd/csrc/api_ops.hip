@@ -17,6 +17,11 @@ static_assert(kNsMaxShort == DEDLOC_ORTHO_MAX_SHORT && kNsMaxLong == DEDLOC_ORTH
 
 namespace {
 
+#ifndef NS_BLOCKED
+#define NS_BLOCKED (1ull << 26)
+#endif
+constexpr uint64_t kNsBlocked = NS_BLOCKED;
+
 uint32_t blocks(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 1) / per); }
 
 int check_sides(uint32_t k, uint32_t rows, uint32_t cols) {
@@ -86,13 +91,9 @@ void make_program(const dedloc_ortho_cfg &c, bool blocked, Program &p) {
     }
 }
 
-#ifndef NS_BLOCKED
-#define NS_BLOCKED (1ull << 28)
-#endif
-constexpr uint64_t kNsBlocked = NS_BLOCKED;
-
 // Whether a matrix is worked on in blocks of steps.  Five steps as blocks of three and two
-// are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15.
+// are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15: worth it from
+// 9 s^2 (l - s) = 6e8 on.
 bool blocked(uint32_t rows, uint32_t cols) {
     const uint64_t s = std::min(rows, cols), l = std::max(rows, cols);
     return s * s * (l - s) >= kNsBlocked;
@@ -154,44 +155,47 @@ uint32_t panels_of(const NsWork &w) {
 }
 uint32_t pieces_of(uint32_t panels, uint32_t most) { return panels > most + most / 2 ? blocks(panels, most) : 1; }
 
-#ifndef NS_FORCE_EDGE
-#define NS_FORCE_EDGE 0
-#endif
-#ifndef NS_FORCE_CUT
-#define NS_FORCE_CUT 0
-#endif
-
 // How a launch's products are cut: the edge of the tiles, and pieces of at most
 // `most` panels of the summed index.
 struct Cut {
     uint32_t edge, most;
 };
 
-// Estimated time of a launch in ns, below 0 if the sums of its cut items take more than `room` bytes.
+// Estimated time of a launch in us, below 0 if the sums of its cut items take
+// more than `room` bytes.  W turns of 32 of the summed index, in `items` tiles of which
+// `full` are not symmetric (and written twice), the longest of `longest` turns: bound by
+// one workgroup alone on its CU, or by 256 CUs that hold two each; the join
+// reads its pieces back.  Fitted to 672 launches (the products of 14 calls of 1 to 54
+// matrices, sides of 1 to 8192) timed in tiles of 128 and 64, uncut and in pieces of at most 64,
+// 32, 16 and 8 panels: the choice by this estimate takes 1.02 of the best times' sum, always 128
+// uncut 1.37, always 64 uncut 1.33.
 double cost_of(const NsWorks &t, Cut c, size_t room) {
-    const double busy = c.edge == 128 ? 575 : 165, alone = c.edge == 128 ? 750 : 230, once = c.edge == 128 ? 3000 : 2000;
-    double turns = 0, cut = 0;
+    const bool big = c.edge == 128;
+    const double alone = big ? 0.78 : 0.17, once = big ? 6.8 : 5.4, busy = big ? 0.63 : 0.21, item = big ? 2.0 : 1.6,
+                 twice = big ? 4.3 : 2.0;
+    double W = 0, items = 0, full = 0, cut = 0;
     uint32_t longest = 0;
     for (uint32_t k = 0; k < t.n; k++) {
-        const uint32_t P = panels_of(t.w[k]), z = pieces_of(P, c.most), len = blocks(P, z);
+        const uint32_t P = panels_of(t.w[k]), z = pieces_of(P, c.most);
         const double tiles = tiles_of(t.w[k], c.edge);
-        turns += tiles * (P + z * (once / busy));
-        longest = std::max(longest, len);
+        W += tiles * P;
+        items += tiles * z;
+        if ((t.w[k].op & 15) >= kNsApply) full += tiles;
         if (z > 1) cut += tiles * z * c.edge * c.edge * sizeof(float);
+        longest = std::max(longest, blocks(P, z));
     }
     if (cut > (double)room) return -1.0;
-    return std::max(turns / 256 * busy + 0.5 * longest * busy, longest * alone + once) + (cut > 0 ? 4000 + cut / 2000 : 0);
+    const double filled = (W * busy + items * item + full * twice) / 256 + 0.7 * busy * longest + 5.5;
+    return std::max(longest * alone + once, filled) + (cut > 0 ? 3.9 + cut * 0.27e-6 : 0);
 }
 
 Cut choose_cut(const NsWorks &t, size_t room) {
     Cut best = {};
     double cost = 0;
     for (uint32_t edge : {128u, 64u})
-        for (uint32_t most : {1u << 30, 512u, 256u, 128u, 64u, 32u, 16u, 8u}) {
-            if (NS_FORCE_EDGE && edge != NS_FORCE_EDGE) continue;
-            if (NS_FORCE_CUT && most != NS_FORCE_CUT && most != 1u << 30) continue;
+        for (uint32_t most : {1u << 30, 256u, 128u, 64u, 32u, 16u, 8u}) {
             const double c = cost_of(t, {edge, most}, room);
-            if (c >= 0 && (best.edge == 0 || c < cost || (NS_FORCE_CUT && most == NS_FORCE_CUT))) {
+            if (c >= 0 && (best.edge == 0 || c < cost)) {
                 cost = c;
                 best = {edge, most};
             }
