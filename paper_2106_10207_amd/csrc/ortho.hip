@@ -338,8 +338,22 @@ __device__ inline void arrived() {
 constexpr int kRawBuffer = 0x00020000;  // descriptor of untyped bytes
 constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // classes of sched_group_barrier
 
-// One tile of a product of a step: 64 W rows and columns, a quarter per wave, W x W
-// blocks of 32 x 32, over a piece of the summed index.  OUT: the dtype of a result, or
+// A shape of tile: `edge` rows and columns, wi x wj blocks of 32 x 32 per wave, two
+// waves to a row of them.  Two workgroups of either kind fit a CU (64 KB of LDS
+// each): big tiles with one turn of loads in flight beside the one worked on, little ones, whose
+// turns are short, with three.
+template <uint32_t EDGE, uint32_t WI, uint32_t WJ, uint32_t STAGES, uint32_t PER_SIMD>
+struct Shape {
+    static constexpr uint32_t edge = EDGE, wi = WI, wj = WJ, waves = EDGE / 32 * EDGE / 32 / (WI * WJ), stages = STAGES,
+                              per_simd = PER_SIMD;
+};
+#ifndef NS_BIG
+#define NS_BIG 128, 2, 2, 2, 2
+#endif
+typedef Shape<NS_BIG> Big;
+typedef Shape<64, 1, 1, 4, 2> Little;
+
+// One tile of a product of a step over a piece of the summed index.  OUT: the dtype of a result, or
 // kNsMuonF32 for the update of the parameters.
 //
 // A turn of the loop takes 32 of the summed index, 128 bytes of a row of either
@@ -350,9 +364,9 @@ constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // class
 // lanes of a read, one row each, meet all 64 banks (with r % 8 two rows met in a bank
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
-template <int OUT, int W, int NS>
-__global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a) {
-    constexpr uint32_t T = 64 * W;
+template <int OUT, typename C>
+__global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(NsWorks t, NsArgs a) {
+    constexpr uint32_t T = C::edge, NW = C::waves, WI = C::wi, WJ = C::wj, NS = C::stages;
     // workgroups go round the 8 XCDs: give each a contiguous range of items
     const uint32_t per = gridDim.x / 8, odd = gridDim.x % 8, xcd = blockIdx.x % 8;
     const uint32_t wg = xcd * per + min(xcd, odd) + blockIdx.x / 8;
@@ -370,9 +384,9 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
         lds3[NS > 3 ? kStage : 16];
     auto stage = [&](uint32_t k) { return k == 0 ? lds0 : k == 1 ? lds1 : k == 2 ? lds2 : lds3; };
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t wi = wave / 2 * (32 * W), wj = wave % 2 * (32 * W);
+    const uint32_t wi = wave / 2 * (32 * WI), wj = wave % 2 * (32 * WJ);
     // A load of a wave takes 8 rows.  The panels' rows past the matrix' end lie beyond the descriptor's end and read as 0.
-    constexpr uint32_t kLoads = 4 * W;
+    constexpr uint32_t kLoads = 2 * T / 8 / NW;
     const uint32_t from = wave * 1024 + (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
     const uint64_t left_panel = (uint64_t)left_rows * 128, right_panel = (uint64_t)right_rows * 128;
     const uint32_t left_end = (left_rows - i0) * 128, right_end = (right_rows - j0) * 128;
@@ -386,11 +400,11 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
         const auto rrows = __builtin_amdgcn_make_buffer_rsrc((void *)(right + p * right_panel), 0, right_end, kRawBuffer);
 #pragma unroll
         for (uint32_t q = 0; q < kLoads; q++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(q < 2 * W ? lrows : rrows, (LdsPtr)(lds + (q * 32 + wave * 8) * 128), 16,
-                                                     from, q % (2 * W) * 4096, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(q < kLoads / 2 ? lrows : rrows, (LdsPtr)(lds + (q * NW + wave) * 1024), 16,
+                                                     from, q % (kLoads / 2) * NW * 1024, 0, 0);
     };
-    f32x16 acc[W][W] = {};
-    f16x8 l[2][W][2], r[2][W][2];  // [half of the turn][block][plane]
+    f32x16 acc[WI][WJ] = {};
+    f16x8 l[2][WI][2], r[2][WJ][2];  // [half of the turn][block][plane]
     auto read = [&](const char *lds, uint32_t h) {
         auto one = [&](uint32_t row, uint32_t p) {
             const uint32_t c = p * 4 + h * 2 + lane / 32;
@@ -399,19 +413,18 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
 #pragma unroll
         for (uint32_t p = 0; p < 2; p++) {
 #pragma unroll
-            for (uint32_t b = 0; b < W; b++) {
-                l[h][b][p] = one(wi + b * 32 + lane % 32, p);
-                r[h][b][p] = one(T + wj + b * 32 + lane % 32, p);
-            }
+            for (uint32_t b = 0; b < WI; b++) l[h][b][p] = one(wi + b * 32 + lane % 32, p);
+#pragma unroll
+            for (uint32_t b = 0; b < WJ; b++) r[h][b][p] = one(T + wj + b * 32 + lane % 32, p);
         }
     };
     auto multiply = [&](uint32_t h) {
 #pragma unroll
         for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
 #pragma unroll
-            for (uint32_t i = 0; i < W; i++)
+            for (uint32_t i = 0; i < WI; i++)
 #pragma unroll
-                for (uint32_t j = 0; j < W; j++)
+                for (uint32_t j = 0; j < WJ; j++)
                     // the right factor's rows first: a lane then holds four consecutive columns of one row
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[h][j][p == 1], l[h][i][p == 0], acc[i][j], 0, 0, 0);
     };
@@ -420,11 +433,13 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
     arrived<(NS - 1) * kLoads>();
     read(stage(0), 0);
     auto turn = [&](uint32_t k, uint32_t panel) {
+        constexpr uint32_t kRead = 2 * (WI + WJ), kEach = 3 * WI * WJ > kRead ? 3 * WI * WJ / kRead : 1;
+        static_assert(kLoads <= kRead, "");
         read(stage(k), 1);
         multiply(0);
 #pragma unroll
-        for (uint32_t q = 0; q < kLoads; q++) {
-            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * W * W / kLoads, 0);
+        for (uint32_t q = 0; q < kRead; q++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, kEach, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
         }
         // the next stage is there, and all have read this one, which the next loads fill
@@ -435,10 +450,10 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
         fetch(stage(k), panel + NS);
         multiply(1);
 #pragma unroll
-        for (uint32_t q = 0; q < kLoads; q++) {
-            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 3 * W * W / kLoads, 0);
+        for (uint32_t q = 0; q < kRead; q++) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, kEach, 0);
             __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kSchedLoad, 1, 0);
+            if (q < kLoads) __builtin_amdgcn_sched_group_barrier(kSchedLoad, 1, 0);
         }
     };
     uint32_t panel = 0;
@@ -450,29 +465,31 @@ __global__ __launch_bounds__(256, 2) void ns_product_kernel(NsWorks t, NsArgs a)
         if (panel + k < panels) turn(k, panel + k);
     arrived<0>();  // no load may arrive in LDS that another workgroup has by then
     if (m.pieces > 1) {  // the sums of the piece, joined by the next launch
-        float *to = a.pieces + (uint64_t)wg * (T * T) + wave * (T * T / 4) + lane * 4;
+        float *to = a.pieces + (uint64_t)wg * (T * T) + wave * (T * T / NW) + lane * 4;
 #pragma unroll
-        for (uint32_t b = 0; b < W * W; b++)
+        for (uint32_t b = 0; b < WI * WJ; b++)
 #pragma unroll
             for (uint32_t g = 0; g < 4; g++)
-                *(f32x4 *)(to + (b * 4 + g) * 256) = *((const f32x4 *)&acc[b / W][b % W] + g);
+                *(f32x4 *)(to + (b * 4 + g) * 256) = *((const f32x4 *)&acc[b / WJ][b % WJ] + g);
         return;
     }
-    uint32_t *turn_lds = (uint32_t *)(stage(wave / 2) + wave % 2 * (32 * kTurnPitch * 4));
+    constexpr uint32_t kTurnBytes = 32 * kTurnPitch * 4, kTurns = kStage / kTurnBytes;  // that a stage has room for
+    static_assert(kTurns * NS >= NW, "");
+    uint32_t *turn_lds = (uint32_t *)(stage(wave / kTurns) + wave % kTurns * kTurnBytes);
 #pragma unroll
-    for (uint32_t b = 0; b < W * W; b++) {
-        const uint32_t i = i0 + wi + b / W * 32, j = j0 + wj + b % W * 32;
+    for (uint32_t b = 0; b < WI * WJ; b++) {
+        const uint32_t i = i0 + wi + b / WJ * 32, j = j0 + wj + b % WJ * 32;
         // of a symmetric result the blocks above the diagonal are written as the mirror of those below
         if (i < left_rows && j < right_rows && (kind >= kNsApply || j <= i))
-            ns_finish<OUT>(m, d, a, i, j, acc[b / W][b % W], turn_lds);
+            ns_finish<OUT>(m, d, a, i, j, acc[b / WJ][b % WJ], turn_lds);
     }
 }
 
 // A block of 32 x 32 of a product whose summed index was cut: a workgroup adds up its pieces, a quarter of them
 // per wave, in an order that only their number decides.  One workgroup per block of each tile.
-template <int OUT, int W>
+template <int OUT, typename C>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsWorks t, NsArgs a) {
-    constexpr uint32_t T = 64 * W, kBlocks = 4 * W * W;
+    constexpr uint32_t T = C::edge, WI = C::wi, WJ = C::wj, kBlocks = T * T / 1024;
     // the table counts items, a work's tiles once for every piece
     uint32_t k = blockIdx.x / kBlocks, q = 0;
     const uint32_t block = blockIdx.x % kBlocks;
@@ -486,10 +503,10 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsWorks t, NsArgs a) {
     }
     const NsWork &m = t.w[q];
     const bool full = (m.op & 15) >= kNsApply;
-    const uint32_t wave_of = block / (W * W), b = block % (W * W), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t i = tile.ti * T + wave_of / 2 * (32 * W) + b / W * 32, j = tile.tj * T + wave_of % 2 * (32 * W) + b % W * 32;
+    const uint32_t wave_of = block / (WI * WJ), b = block % (WI * WJ), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t i = tile.ti * T + wave_of / 2 * (32 * WI) + b / WJ * 32, j = tile.tj * T + wave_of % 2 * (32 * WJ) + b % WJ * 32;
     if (i >= d.S || j >= (full ? d.L : d.S) || (!full && j > i)) return;
-    const float *from = a.pieces + (uint64_t)(m.begin + k) * (T * T) + wave_of * (T * T / 4) + b * 1024 + lane * 4;
+    const float *from = a.pieces + (uint64_t)(m.begin + k) * (T * T) + (wave_of * (WI * WJ) + b) * 1024 + lane * 4;
     f32x4 sum[4] = {};
     for (uint32_t p = m.pieces * wave / 4; p < m.pieces * (wave + 1) / 4; p++)
 #pragma unroll
@@ -535,37 +552,36 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
 }
 
 namespace {
-template <int W, int NS>
+template <typename C>
 void product(int out, const NsWorks &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
     switch (out) {
-        case kNsF32: ns_product_kernel<kNsF32, W, NS><<<groups, 256, 0, s>>>(t, a); break;
-        case kNsFP16: ns_product_kernel<kNsFP16, W, NS><<<groups, 256, 0, s>>>(t, a); break;
-        case kNsBF16: ns_product_kernel<kNsBF16, W, NS><<<groups, 256, 0, s>>>(t, a); break;
-        default: ns_product_kernel<kNsMuonF32, W, NS><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsF32: ns_product_kernel<kNsF32, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
+        case kNsFP16: ns_product_kernel<kNsFP16, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
+        case kNsBF16: ns_product_kernel<kNsBF16, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
+        default: ns_product_kernel<kNsMuonF32, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
     }
 }
-template <int W>
-void join(int out, const NsWorks &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+template <typename C>
+void join(int out, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
+    const uint32_t groups = tiles * (C::edge * C::edge / 1024);
     switch (out) {
-        case kNsF32: ns_join_kernel<kNsF32, W><<<groups, 256, 0, s>>>(t, a); break;
-        case kNsFP16: ns_join_kernel<kNsFP16, W><<<groups, 256, 0, s>>>(t, a); break;
-        case kNsBF16: ns_join_kernel<kNsBF16, W><<<groups, 256, 0, s>>>(t, a); break;
-        default: ns_join_kernel<kNsMuonF32, W><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsF32: ns_join_kernel<kNsF32, C><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsFP16: ns_join_kernel<kNsFP16, C><<<groups, 256, 0, s>>>(t, a); break;
+        case kNsBF16: ns_join_kernel<kNsBF16, C><<<groups, 256, 0, s>>>(t, a); break;
+        default: ns_join_kernel<kNsMuonF32, C><<<groups, 256, 0, s>>>(t, a); break;
     }
 }
 }  // namespace
 
-// Two workgroups of either kind fit a CU (64 KB of LDS each): big tiles with one turn of loads in flight beside the one
-// worked on, small ones, whose turns are short, with three.
 hipError_t launch_ns_product(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t items, hipStream_t s) {
-    if (edge == 128) product<2, 2>(out, t, a, items, s);
-    else product<1, 4>(out, t, a, items, s);
+    if (edge == 128) product<Big>(out, t, a, items, s);
+    else product<Little>(out, t, a, items, s);
     return hipGetLastError();
 }
 
 hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
-    if (edge == 128) join<2>(out, t, a, tiles * 16, s);
-    else join<1>(out, t, a, tiles * 4, s);
+    if (edge == 128) join<Big>(out, t, a, tiles, s);
+    else join<Little>(out, t, a, tiles, s);
     return hipGetLastError();
 }
 
