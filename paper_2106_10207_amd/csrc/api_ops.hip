@@ -316,15 +316,19 @@ size_t batches_bytes(bool muon, uint32_t n, S sides) {
 
 struct EmbedWs {
     size_t pairs, counts, total;
-    uint32_t chunk;
+    uint32_t chunk, run;
 };
+#ifndef EMB_RUN
+#define EMB_RUN 0
+#endif
 EmbedWs embed_ws(uint64_t n, uint32_t width) {
     EmbedWs w;
     w.pairs = round_up((size_t)n * sizeof(uint2), 256);
     const uint32_t tiles = std::max(1u, blocks(n, kSortTile));
     w.chunk = (tiles + kSortChunks - 1) / kSortChunks * kSortTile;
+    w.run = EMB_RUN ? EMB_RUN : n * width < (1u << 22) ? 8 : 32;
     w.counts = (size_t)blocks(n, w.chunk) * 256 * sizeof(uint32_t);
-    w.total = 2 * w.pairs + w.counts + round_up((size_t)blocks(n, kRunChunk) * 2 * width * sizeof(float), 256);
+    w.total = 2 * w.pairs + w.counts + round_up((size_t)blocks(n, w.run) * 2 * width * sizeof(float), 256);
     w.total = std::max(w.total, (size_t)256);
     return w;
 }
@@ -525,12 +529,17 @@ int dedloc_embed_grad(float *grad, uint64_t vocab, uint32_t width, uint64_t ld_g
     if (rc) return rc;
     char *b = (char *)ws;
     const EmbedGradArgs a = {grad, ld_grad, ids, dy, ld_dy, (uint32_t)vocab, width, (uint32_t)n, id_bytes == 8,
-                             scale * batch_samples, w.chunk, {(uint2 *)b, (uint2 *)(b + w.pairs)}, (uint32_t *)(b + 2 * w.pairs),
+                             scale * batch_samples, w.chunk, w.run, {(uint2 *)b, (uint2 *)(b + w.pairs)}, (uint32_t *)(b + 2 * w.pairs),
                              (float *)(b + 2 * w.pairs + w.counts)};
     hipStream_t s = (hipStream_t)stream;
     int from = -1;
+    if (n <= kSortOne) {
+        const hipError_t e = timed(K_EMBED_SORT, s, [&] { return launch_embed_sort(a, s); });
+        if (e != hipSuccess) return hip_fail(e, "embed sort launch");
+        from = 0;
+    }
     // digits of the tokens and of `vocab`, which stands for a masked position
-    for (uint32_t shift = 0; shift == 0 || vocab >> shift; shift += 8) {
+    for (uint32_t shift = 0; n > kSortOne && (shift == 0 || vocab >> shift); shift += 8) {
         hipError_t e = timed(K_EMBED_COUNT, s, [&] { return launch_embed_count(a, from, shift, s); });
         if (e != hipSuccess) return hip_fail(e, "embed count launch");
         e = timed(K_EMBED_SCATTER, s, [&] { return launch_embed_scatter(a, from, shift, s); });

@@ -41,6 +41,21 @@ __device__ inline void store(T *p, const float *o) {
     *(Vec<N, T> *)p = q;
 }
 
+// A product rounded to fp32 before it is rounded to 16 bits (without this the
+// two become one instruction with one rounding).
+__device__ inline float times(float a, float b) {
+    float p = a * b;
+    asm("" : "+v"(p));
+    return p;
+}
+
+// Orders what one lane of a wave wrote to LDS before what another reads.
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // The token at a position; `vocab` for an id outside the table.
 __device__ inline uint32_t token(const void *ids, int wide, uint32_t vocab, uint32_t i) {
     const int64_t id = wide ? ((const int64_t *)ids)[i] : (int64_t)((const int32_t *)ids)[i];
@@ -50,25 +65,39 @@ __device__ inline uint32_t token(const void *ids, int wide, uint32_t vocab, uint
 }  // namespace
 
 // A row of threads (tx of them, a power of two) per position, N elements per
-// thread and turn.
-template <typename TI, typename TO, int N>
+// thread and turn; ROWS positions at a time, whose loads are all on their way
+// before the first is scaled.
+template <typename TI, typename TO, int N, int ROWS>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {
-    const uint32_t x = threadIdx.x & (tx - 1);
-    const uint64_t row = (uint64_t)blockIdx.x * (256 / tx) + threadIdx.x / tx;
-    if (row >= a.n) return;
-    const uint32_t tok = token(a.ids, a.wide_ids, a.vocab, (uint32_t)row);
-    const TI *from = (const TI *)a.table + (uint64_t)tok * a.ld_table;
-    TO *to = (TO *)a.out + row * a.ld_out;
-    const bool named = tok < a.vocab;
+    const uint32_t x = threadIdx.x & (tx - 1), rows = 256 / tx;
+    const uint64_t row0 = (uint64_t)blockIdx.x * (rows * ROWS) + threadIdx.x / tx;
+    uint32_t tok[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; k++) {
+        const uint64_t row = row0 + k * rows;
+        tok[k] = row < a.n ? token(a.ids, a.wide_ids, a.vocab, (uint32_t)row) : a.vocab;
+    }
     for (uint32_t c = x * N; c < a.width; c += tx * N) {
-        float v[N] = {};
-        if (c + N <= a.width) {
-            if (named) load<N>(from + c, v);
-            for (int i = 0; i < N; i++) v[i] *= a.scale;
-            if (!named) for (int i = 0; i < N; i++) v[i] = 0.0f;
-            store<N>(to + c, v);
-        } else {
-            for (uint32_t i = c; i < a.width; i++) to[i] = (TO)(named ? load1(from + i) * a.scale : 0.0f);
+        const bool whole = c + N <= a.width;
+        float v[ROWS][N] = {};
+        if (whole) {
+#pragma unroll
+            for (int k = 0; k < ROWS; k++)
+                if (tok[k] < a.vocab) load<N>((const TI *)a.table + (uint64_t)tok[k] * a.ld_table + c, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; k++) {
+            const uint64_t row = row0 + k * rows;
+            if (row >= a.n) break;
+            const bool named = tok[k] < a.vocab;
+            TO *to = (TO *)a.out + row * a.ld_out;
+            if (whole) {
+                for (int i = 0; i < N; i++) v[k][i] = named ? times(v[k][i], a.scale) : 0.0f;
+                store<N>(to + c, v[k]);
+            } else {
+                const TI *from = (const TI *)a.table + (uint64_t)tok[k] * a.ld_table;
+                for (uint32_t i = c; i < a.width; i++) to[i] = (TO)(named ? times(load1(from + i), a.scale) : 0.0f);
+            }
         }
     }
 }
@@ -95,48 +124,77 @@ __global__ __launch_bounds__(256) void embed_count_kernel(EmbedGradArgs a, const
     a.counts[blockIdx.x * 256 + threadIdx.x] = count[threadIdx.x];
 }
 
-// Orders what one lane of a wave wrote to LDS before what another reads.
-__device__ inline void wave_order() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+// The lanes of a wave that have the same 8-bit digit (of those with `in`).
+__device__ inline unsigned long long same_digit(uint32_t digit, bool in) {
+    unsigned long long same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 8; b++) {
+        const unsigned long long m = __ballot((digit >> b) & 1u);
+        same &= (digit >> b) & 1u ? m : ~m;
+    }
+    return same;
+}
+
+// Positions of a wave, 64 a round, in order: an item's rank is how many of the
+// wave's items before it have its digit.  at[256]: the wave's counters, zeroed by
+// the caller; afterwards how many items have each digit.
+template <uint32_t R>
+__device__ inline void rank_digits(const uint2 *p, uint32_t left, uint32_t shift, uint32_t *at, uint16_t *rank) {
+    const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+    for (uint32_t r = 0; r < R; r++) {
+        const bool in = r * 64 + lane < left;
+        const uint32_t digit = (p[r].x >> shift) & 255u;
+        const unsigned long long same = same_digit(digit, in);
+        const uint32_t mine = __popcll(same & ((1ull << lane) - 1));
+        rank[r] = (uint16_t)(at[digit] + mine);
+        wave_order();
+        if (in && mine == 0) at[digit] += __popcll(same);
+        wave_order();
+    }
+}
+
+// Exclusive sum over threads 0 to 255 of the workgroup (the others pass 0).
+__device__ inline uint32_t scan_256(uint32_t v, uint32_t *part) {
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    uint32_t scan = v;
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t up = __shfl_up(scan, off, 64);
+        if (lane >= (uint32_t)off) scan += up;
+    }
+    if (wave < 4 && lane == 63) part[wave] = scan;
+    __syncthreads();
+    for (uint32_t w = 0; w < wave && w < 3; w++) scan += part[w];
+    return scan - v;
 }
 
 template <bool FIRST>
 __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, const uint2 *from, uint2 *to, uint32_t shift) {
     constexpr uint32_t R = kSortTile / 256;
-    __shared__ uint32_t at[4][256];  // per wave and digit: where its next position goes
-    __shared__ uint32_t total[4];
+    __shared__ uint32_t at[4][256];  // per wave and digit
+    __shared__ uint32_t part[4];
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, chunks = gridDim.x;
     // the first place of digit t: all smaller digits, and this digit in the chunks before
     uint32_t before = 0, all = 0;
+#pragma unroll 16
     for (uint32_t k = 0; k < chunks; k++) {
         const uint32_t c = a.counts[k * 256 + t];
         all += c;
         before += k < blockIdx.x ? c : 0;
     }
-    uint32_t scan = all;
-    for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t up = __shfl_up(scan, off, 64);
-        if (lane >= (uint32_t)off) scan += up;
-    }
-    if (lane == 63) total[wave] = scan;
-    __syncthreads();
-    uint32_t start = scan - all + before;
-    for (uint32_t w = 0; w < wave; w++) start += total[w];
+    uint32_t start = scan_256(all, part) + before;
     const uint32_t end = min((blockIdx.x + 1) * a.chunk, a.n);
     for (uint32_t tile = blockIdx.x * a.chunk; tile < end; tile += kSortTile) {
         for (int w = 0; w < 4; w++) at[w][t] = 0;
-        __syncthreads();
         // each wave takes a quarter of the tile, in order
-        const uint32_t i0 = tile + wave * (kSortTile / 4) + lane;
+        const uint32_t i0 = tile + wave * (kSortTile / 4), left = i0 < end ? end - i0 : 0;
         uint2 p[R];
+        uint16_t rank[R];
 #pragma unroll
-        for (uint32_t r = 0; r < R; r++) {
-            const uint32_t i = i0 + r * 64;
-            p[r] = i < end ? pair_at<FIRST>(a, from, i) : make_uint2(0xffffffffu, 0u);
-            if (i < end) atomicAdd(&at[wave][(p[r].x >> shift) & 255u], 1u);
-        }
+        for (uint32_t r = 0; r < R; r++)
+            p[r] = r * 64 + lane < left ? pair_at<FIRST>(a, from, i0 + r * 64 + lane) : make_uint2(0xffffffffu, 0u);
+        __syncthreads();
+        rank_digits<R>(p, left, shift, at[wave], rank);
         __syncthreads();
         for (int w = 0; w < 4; w++) {
             const uint32_t c = at[w][t];
@@ -145,77 +203,182 @@ __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, con
         }
         __syncthreads();
 #pragma unroll
-        for (uint32_t r = 0; r < R; r++) {
-            const bool in = i0 + r * 64 < end;
-            const uint32_t digit = (p[r].x >> shift) & 255u;
-            unsigned long long same = __ballot(in);
-#pragma unroll
-            for (int b = 0; b < 8; b++) {
-                const unsigned long long m = __ballot((digit >> b) & 1u);
-                same &= (digit >> b) & 1u ? m : ~m;
-            }
-            const uint32_t rank = __popcll(same & ((1ull << lane) - 1));
-            if (in) to[at[wave][digit] + rank] = p[r];
-            wave_order();
-            if (in && rank == 0) at[wave][digit] += __popcll(same);
-            wave_order();
-        }
+        for (uint32_t r = 0; r < R; r++)
+            if (r * 64 + lane < left) to[at[wave][(p[r].x >> shift) & 255u] + rank[r]] = p[r];
         __syncthreads();
     }
 }
 
+// Every pass at once where one workgroup holds all positions: 1024 threads, 16
+// waves of R rounds, the pairs in LDS between the passes.
+template <uint32_t R>
+__global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2 *to) {
+    __shared__ uint2 pairs[R * 1024];
+    __shared__ uint32_t at[16][256];
+    __shared__ uint32_t part[4];
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const uint32_t i0 = wave * (R * 64), left = i0 < a.n ? a.n - i0 : 0;
+    uint2 p[R];
+    uint16_t rank[R];
+#pragma unroll
+    for (uint32_t r = 0; r < R; r++)
+        p[r] = r * 64 + lane < left ? pair_at<true>(a, nullptr, i0 + r * 64 + lane) : make_uint2(0xffffffffu, 0u);
+    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += 8) {
+        for (uint32_t k = t; k < 16 * 256; k += 1024) (&at[0][0])[k] = 0;
+        __syncthreads();
+        rank_digits<R>(p, left, shift, at[wave], rank);
+        __syncthreads();
+        uint32_t all = 0;
+        if (t < 256)
+            for (int w = 0; w < 16; w++) all += at[w][t];
+        uint32_t start = scan_256(all, part);
+        if (t < 256)
+            for (int w = 0; w < 16; w++) {
+                const uint32_t c = at[w][t];
+                at[w][t] = start;
+                start += c;
+            }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < R; r++)
+            if (r * 64 + lane < left) pairs[at[wave][(p[r].x >> shift) & 255u] + rank[r]] = p[r];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < R; r++)
+            if (r * 64 + lane < left) p[r] = pairs[i0 + r * 64 + lane];
+        __syncthreads();
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < R; r++)
+        if (r * 64 + lane < left) to[i0 + r * 64 + lane] = p[r];
+}
+
 // ------------------------------------------------------------------ the sums
 
-// A row of tx threads sums one chunk of kRunChunk sorted positions, four
-// columns per thread.
-template <typename T>
+// A row of tx threads sums one chunk of a.run sorted positions, N columns per
+// thread, kBatch rows of dy (and the accumulator's rows that they end) on their way at a time.
+constexpr uint32_t kBatch = 8;
+
+template <typename T, int N>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const uint2 *pairs, uint32_t tx) {
     const uint32_t x = threadIdx.x & (tx - 1);
     const uint32_t chunk = blockIdx.x * (256 / tx) + threadIdx.x / tx;
-    const uint64_t i0 = (uint64_t)chunk * kRunChunk;
+    const uint64_t i0 = (uint64_t)chunk * a.run;
     if (i0 >= a.n) return;
-    const uint32_t i1 = (uint32_t)(i0 + kRunChunk < a.n ? i0 + kRunChunk : a.n);
-    const uint32_t c = (blockIdx.y * tx + x) * 4;
+    const uint32_t i1 = (uint32_t)(i0 + a.run < a.n ? i0 + a.run : a.n);
+    const uint32_t c = (blockIdx.y * tx + x) * N;
     if (c >= a.width) return;
-    const uint32_t live = min(4u, a.width - c);
+    const bool whole = c + N <= a.width;
+    const uint32_t live = whole ? N : a.width - c;
     const T *dy = (const T *)a.dy + c;
-    const uint32_t prev = i0 > 0 ? pairs[i0 - 1].x : 0xffffffffu, next = i1 < a.n ? pairs[i1].x : 0xffffffffu;
-    float sum[4] = {};
-    bool head = pairs[i0].x == prev;  // the run began in an earlier chunk
-    for (uint32_t i = (uint32_t)i0; i < i1; i++) {
-        const uint2 p = pairs[i];
-        if (p.x == a.vocab) return;  // masked positions come last
-        const T *row = dy + (uint64_t)p.y * a.ld_dy;
-        float v[4] = {};
-        if (live == 4) load<4>(row, v);
-        else for (uint32_t e = 0; e < live; e++) v[e] = load1(row + e);
-        for (int e = 0; e < 4; e++) sum[e] += v[e];
-        const bool end = i + 1 == i1, more = (end ? next : pairs[i + 1].x) == p.x;
-        if (more && !end) continue;
-        float *to = head || more ? a.cut + ((uint64_t)chunk * 2 + (head ? 0 : 1)) * a.width + c
-                                 : a.grad + (uint64_t)p.x * a.ld_grad + c;
-        for (uint32_t e = 0; e < live; e++) to[e] = head || more ? sum[e] : fmaf(a.factor, sum[e], to[e]);
-        head = false;
-        for (int e = 0; e < 4; e++) sum[e] = 0.0f;
+    uint32_t tok = i0 > 0 ? pairs[i0 - 1].x : 0xffffffffu;
+    bool head = pairs[i0].x == tok;  // the run began in an earlier chunk
+    float sum[N] = {};
+    for (uint32_t i = (uint32_t)i0; i < i1; i += kBatch) {
+        uint2 p[kBatch + 1];
+#pragma unroll
+        for (uint32_t k = 0; k <= kBatch; k++) p[k] = i + k < a.n ? pairs[i + k] : make_uint2(0xffffffffu, 0u);
+        float v[kBatch][N] = {}, old[kBatch][N] = {};
+        // what becomes of row k: nothing (masked, or past the chunk), added, or added as its run's last here
+        bool in[kBatch], last[kBatch], cut[kBatch];
+        bool began = head;
+#pragma unroll
+        for (uint32_t k = 0; k < kBatch; k++) {
+            in[k] = i + k < i1 && p[k].x < a.vocab;
+            const bool more = p[k + 1].x == p[k].x;
+            last[k] = in[k] && (!more || i + k + 1 == i1);
+            cut[k] = began || (last[k] && more);
+            if (last[k]) began = false;
+            const T *row = dy + (uint64_t)p[k].y * a.ld_dy;
+            const float *acc = a.grad + (uint64_t)p[k].x * a.ld_grad + c;
+            if (whole) {
+                if (in[k]) load<N>(row, v[k]);
+                if (last[k] && !cut[k]) load<N>(acc, old[k]);
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < N; e++) {
+                    if (e < live && in[k]) v[k][e] = load1(row + e);
+                    if (e < live && last[k] && !cut[k]) old[k][e] = acc[e];
+                }
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kBatch; k++) {
+            if (!in[k]) continue;
+            for (int e = 0; e < N; e++) sum[e] += v[k][e];
+            if (!last[k]) continue;
+            float *to = cut[k] ? a.cut + ((uint64_t)chunk * 2 + (head ? 0 : 1)) * a.width + c
+                               : a.grad + (uint64_t)p[k].x * a.ld_grad + c;
+            for (int e = 0; e < N; e++) {
+                if (!cut[k]) sum[e] = fmaf(a.factor, sum[e], old[k][e]);
+            }
+            if (whole) store<N>(to, sum);
+            else {
+#pragma unroll
+                for (uint32_t e = 0; e < N; e++)
+                    if (e < live) to[e] = sum[e];
+            }
+            head = false;
+            for (int e = 0; e < N; e++) sum[e] = 0.0f;
+        }
     }
 }
 
-// The run that leaves a chunk it began in: its parts, in ascending order.
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const uint2 *pairs, uint32_t tx) {
-    const uint32_t x = threadIdx.x & (tx - 1);
-    uint64_t chunk = (uint64_t)blockIdx.x * (256 / tx) + threadIdx.x / tx;
-    const uint64_t i1 = (chunk + 1) * kRunChunk;
-    if (i1 >= a.n) return;
-    const uint32_t tok = pairs[i1 - 1].x;
-    if (tok == a.vocab || pairs[i1].x != tok) return;
-    const uint64_t i0 = i1 - kRunChunk;
-    if (i0 > 0 && pairs[i0].x == tok && pairs[i0 - 1].x == tok) return;  // it began earlier
-    for (uint32_t c = x; c < a.width; c += tx) {
-        float sum = a.cut[(chunk * 2 + 1) * a.width + c];
-        for (uint64_t k = chunk + 1; k * kRunChunk < a.n && pairs[k * kRunChunk].x == tok; k++)
-            sum += a.cut[k * 2 * a.width + c];
+// The runs that leave the chunk they began in: their parts, a quarter per wave, in
+// ascending order.  A workgroup looks after 256 columns of the runs that begin in
+// kJoinChunks chunks.
+constexpr uint32_t kJoinChunks = 4;
+
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const uint2 *pairs) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (a.n + a.run - 1) / a.run;
+    const uint32_t c = (blockIdx.y * 64 + lane) * 4, live = c < a.width ? min(4u, a.width - c) : 0;
+    __shared__ float part[3][64][4];
+    for (uint32_t chunk = blockIdx.x * kJoinChunks; chunk < (blockIdx.x + 1) * kJoinChunks; chunk++) {
+        const uint64_t i1 = (uint64_t)(chunk + 1) * a.run;
+        if (i1 >= a.n) return;
+        const uint32_t tok = pairs[i1 - 1].x;
+        const uint64_t i0 = i1 - a.run;
+        if (tok >= a.vocab || pairs[i1].x != tok) continue;                      // it ends here
+        if (i0 > 0 && pairs[i0].x == tok && pairs[i0 - 1].x == tok) continue;  // it began earlier
+        // the chunks after this one that begin with the run
+        uint32_t more = 0;
+        for (;; more += 64) {
+            const uint32_t k = chunk + 1 + more + lane;
+            const unsigned long long m = __ballot(k < chunks && pairs[(uint64_t)k * a.run].x == tok);
+            if (m != ~0ull) {
+                more += (uint32_t)__builtin_ctzll(~m);
+                break;
+            }
+        }
+        float sum[4] = {};
+        auto add = [&](const float *from) {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; e++)
+                if (e < live) sum[e] += from[e];
+        };
+        if (wave == 0) add(a.cut + ((uint64_t)chunk * 2 + 1) * a.width + c);
+        const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / 4);
+        uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / 4);
+        if (live == 4) {
+            for (; k + 8 <= k1; k += 8) {
+                float v[8][4];
+#pragma unroll
+                for (uint32_t b = 0; b < 8; b++) load<4>(a.cut + (uint64_t)(k + b) * 2 * a.width + c, v[b]);
+#pragma unroll
+                for (uint32_t b = 0; b < 8; b++)
+                    for (int e = 0; e < 4; e++) sum[e] += v[b][e];
+            }
+        }
+        for (; k < k1; k++) add(a.cut + (uint64_t)k * 2 * a.width + c);
+        __syncthreads();  // the run before has left `part`
+        if (wave > 0)
+            for (int e = 0; e < 4; e++) part[wave - 1][lane][e] = sum[e];
+        __syncthreads();
+        if (wave > 0) continue;
         float *to = a.grad + (uint64_t)tok * a.ld_grad + c;
-        *to = fmaf(a.factor, sum, *to);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; e++)
+            if (e < live) to[e] = fmaf(a.factor, (sum[e] + part[0][lane][e]) + (part[1][lane][e] + part[2][lane][e]), to[e]);
     }
 }
 
@@ -224,6 +387,11 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const 
 namespace {
 
 // Threads per row: the power of two that covers `units`, at most 256.
+#ifndef EMB_MANY
+#define EMB_MANY (1ull << 20)
+#endif
+constexpr uint64_t kEmbedManyThreads = EMB_MANY;
+
 uint32_t row_threads(uint32_t units) {
     uint32_t tx = 1;
     while (tx < units && tx < 256) tx *= 2;
@@ -234,7 +402,10 @@ template <typename TI, typename TO>
 void embed(const EmbedArgs &a, hipStream_t s) {
     constexpr int N = 16 / (sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO));
     const uint32_t tx = row_threads((a.width + N - 1) / N), rows = 256 / tx;
-    embed_kernel<TI, TO, N><<<(a.n + rows - 1) / rows, 256, 0, s>>>(a, tx);
+    if ((uint64_t)a.n * tx >= kEmbedManyThreads)
+        embed_kernel<TI, TO, N, 4><<<(a.n + 4 * rows - 1) / (4 * rows), 256, 0, s>>>(a, tx);
+    else
+        embed_kernel<TI, TO, N, 1><<<(a.n + rows - 1) / rows, 256, 0, s>>>(a, tx);
 }
 template <typename TI>
 void embed(int out, const EmbedArgs &a, hipStream_t s) {
@@ -244,7 +415,15 @@ void embed(int out, const EmbedArgs &a, hipStream_t s) {
 }
 
 uint32_t sort_chunks(const EmbedGradArgs &a) { return (a.n + a.chunk - 1) / a.chunk; }
-uint32_t run_chunks(const EmbedGradArgs &a) { return (a.n + kRunChunk - 1) / kRunChunk; }
+uint32_t run_chunks(const EmbedGradArgs &a) { return (a.n + a.run - 1) / a.run; }
+
+template <typename T>
+void sum(const EmbedGradArgs &a, const uint2 *pairs, hipStream_t s) {
+    constexpr int N = 16 / sizeof(T);
+    const uint32_t units = (a.width + N - 1) / N, tx = row_threads(units), rows = 256 / tx;
+    const dim3 grid((run_chunks(a) + rows - 1) / rows, (units + tx - 1) / tx);
+    embed_sum_kernel<T, N><<<grid, 256, 0, s>>>(a, pairs, tx);
+}
 
 }  // namespace
 
@@ -255,7 +434,6 @@ hipError_t launch_embed(int table, int out, const EmbedArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// from: the buffer that holds the pairs, or -1: the ids
 hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s) {
     if (from < 0) embed_count_kernel<true><<<sort_chunks(a), 256, 0, s>>>(a, nullptr, shift);
     else embed_count_kernel<false><<<sort_chunks(a), 256, 0, s>>>(a, a.pairs[from], shift);
@@ -268,18 +446,25 @@ hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift
     return hipGetLastError();
 }
 
+hipError_t launch_embed_sort(const EmbedGradArgs &a, hipStream_t s) {
+    const uint32_t rounds = (a.n + 1023) / 1024;
+    if (rounds <= 1) embed_sort_kernel<1><<<1, 1024, 0, s>>>(a, a.pairs[0]);
+    else if (rounds <= 4) embed_sort_kernel<4><<<1, 1024, 0, s>>>(a, a.pairs[0]);
+    else if (rounds <= 8) embed_sort_kernel<8><<<1, 1024, 0, s>>>(a, a.pairs[0]);
+    else embed_sort_kernel<16><<<1, 1024, 0, s>>>(a, a.pairs[0]);
+    return hipGetLastError();
+}
+
 hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStream_t s) {
-    const uint32_t units = (a.width + 3) / 4, tx = row_threads(units), rows = 256 / tx;
-    const dim3 grid((run_chunks(a) + rows - 1) / rows, (units + tx - 1) / tx);
-    if (dy == kF32) embed_sum_kernel<float><<<grid, 256, 0, s>>>(a, a.pairs[sorted], tx);
-    else if (dy == kFP16) embed_sum_kernel<_Float16><<<grid, 256, 0, s>>>(a, a.pairs[sorted], tx);
-    else embed_sum_kernel<__bf16><<<grid, 256, 0, s>>>(a, a.pairs[sorted], tx);
+    if (dy == kF32) sum<float>(a, a.pairs[sorted], s);
+    else if (dy == kFP16) sum<_Float16>(a, a.pairs[sorted], s);
+    else sum<__bf16>(a, a.pairs[sorted], s);
     return hipGetLastError();
 }
 
 hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s) {
-    const uint32_t tx = row_threads(a.width), rows = 256 / tx;
-    embed_join_kernel<<<(run_chunks(a) + rows - 1) / rows, 256, 0, s>>>(a, a.pairs[sorted], tx);
+    const dim3 grid((run_chunks(a) + kJoinChunks - 1) / kJoinChunks, (a.width + 255) / 256);
+    embed_join_kernel<<<grid, 256, 0, s>>>(a, a.pairs[sorted]);
     return hipGetLastError();
 }
 

@@ -100,7 +100,8 @@ constexpr uint32_t kEmbedMaxWidth = 1u << 20;
 // workgroup each: every workgroup reads the digit counts of all chunks.
 constexpr uint32_t kSortTile = 2048;
 constexpr uint32_t kSortChunks = 512;
-constexpr uint32_t kRunChunk = 32;     // sorted positions summed by one row of threads
+// Up to kSortOne positions are sorted by one workgroup in one launch.
+constexpr uint32_t kSortOne = 16384;
 
 struct EmbedArgs {
     const void *table;
@@ -123,6 +124,7 @@ struct EmbedGradArgs {
     int32_t wide_ids;
     float factor;    // scale * batch_samples
     uint32_t chunk;  // positions of a chunk of the sort
+    uint32_t run;    // sorted positions summed by one row of threads
     // workspace: (token, position) pairs sorted in turn between two buffers,
     // digit counts per chunk, and the sums of runs cut by a chunk's edge
     uint2 *pairs[2];
@@ -131,6 +133,9 @@ struct EmbedGradArgs {
 };
 
 hipError_t launch_embed(int table, int out, const EmbedArgs &a, hipStream_t s);
+// All of the sort for at most kSortOne positions, into pairs[0].
+hipError_t launch_embed_sort(const EmbedGradArgs &a, hipStream_t s);
+// One pass over 8 bits; from: the buffer that holds the pairs, or -1: the ids.
 hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
 hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
 hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStream_t s);
