@@ -40,6 +40,20 @@ __device__ inline void store(T *p, const float *o) {
     for (int i = 0; i < N; i++) q.v[i] = (T)o[i];
     *(Vec<N, T> *)p = q;
 }
+// A store of what nothing here reads again; the address at any alignment of the element.
+template <int N, typename T>
+__device__ inline void store_stream(T *p, const float *o) {
+    Vec<N, T> q;
+#pragma unroll
+    for (int i = 0; i < N; i++) q.v[i] = (T)o[i];
+    if constexpr (sizeof(q) == 16) {
+        typedef unsigned U __attribute__((ext_vector_type(4), aligned(2)));
+        __builtin_nontemporal_store(__builtin_bit_cast(U, q), (U *)p);
+    } else {
+        typedef unsigned U __attribute__((ext_vector_type(2), aligned(2)));
+        __builtin_nontemporal_store(__builtin_bit_cast(U, q), (U *)p);
+    }
+}
 
 // A product rounded to fp32 before it is rounded to 16 bits (without this the
 // two become one instruction with one rounding).
@@ -93,7 +107,7 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {
             TO *to = (TO *)a.out + row * a.ld_out;
             if (whole) {
                 for (int i = 0; i < N; i++) v[k][i] = named ? times(v[k][i], a.scale) : 0.0f;
-                store<N>(to + c, v[k]);
+                store_stream<N>(to + c, v[k]);
             } else {
                 const TI *from = (const TI *)a.table + (uint64_t)tok[k] * a.ld_table;
                 for (uint32_t i = c; i < a.width; i++) to[i] = (TO)(named ? times(load1(from + i), a.scale) : 0.0f);
@@ -209,55 +223,72 @@ __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, con
     }
 }
 
-// Every pass at once where one workgroup holds all positions: 1024 threads, 16
-// waves of R rounds, the pairs in LDS between the passes.
-template <uint32_t R>
+// A chunk of 1024 positions sorted by one workgroup, every pass at once, the pairs in
+// LDS between the passes.
 __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2 *to) {
-    __shared__ uint2 pairs[R * 1024];
+    __shared__ uint2 pairs[1024];
     __shared__ uint32_t at[16][256];
     __shared__ uint32_t part[4];
-    const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const uint32_t i0 = wave * (R * 64), left = i0 < a.n ? a.n - i0 : 0;
-    uint2 p[R];
-    uint16_t rank[R];
-#pragma unroll
-    for (uint32_t r = 0; r < R; r++)
-        p[r] = r * 64 + lane < left ? pair_at<true>(a, nullptr, i0 + r * 64 + lane) : make_uint2(0xffffffffu, 0u);
+    const uint32_t t = threadIdx.x, wave = t >> 6, i0 = blockIdx.x * 1024, n = min(1024u, a.n - i0);
+    const uint32_t left = wave * 64 < n ? n - wave * 64 : 0;
+    uint2 p = t < n ? pair_at<true>(a, nullptr, i0 + t) : make_uint2(0xffffffffu, 0u);
     for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += 8) {
         for (uint32_t k = t; k < 16 * 256; k += 1024) (&at[0][0])[k] = 0;
         __syncthreads();
-        rank_digits<R>(p, left, shift, at[wave], rank);
+        uint16_t rank;
+        rank_digits<1>(&p, left, shift, at[wave], &rank);
         __syncthreads();
-        uint32_t all = 0;
+        uint32_t c[16], all = 0;
         if (t < 256)
-            for (int w = 0; w < 16; w++) all += at[w][t];
+#pragma unroll
+            for (int w = 0; w < 16; w++) all += c[w] = at[w][t];
         uint32_t start = scan_256(all, part);
         if (t < 256)
+#pragma unroll
             for (int w = 0; w < 16; w++) {
-                const uint32_t c = at[w][t];
                 at[w][t] = start;
-                start += c;
+                start += c[w];
             }
         __syncthreads();
-#pragma unroll
-        for (uint32_t r = 0; r < R; r++)
-            if (r * 64 + lane < left) pairs[at[wave][(p[r].x >> shift) & 255u] + rank[r]] = p[r];
+        if (t < n) pairs[at[wave][(p.x >> shift) & 255u] + rank] = p;
         __syncthreads();
-#pragma unroll
-        for (uint32_t r = 0; r < R; r++)
-            if (r * 64 + lane < left) p[r] = pairs[i0 + r * 64 + lane];
-        __syncthreads();
+        if (t < n) p = pairs[t];
     }
+    if (t < n) to[i0 + t] = p;
+}
+
+// Up to kSortOne positions: the sorted chunks merged.  A pair goes to its place in
+// its chunk plus, for every other chunk, the number of pairs that come before it, which
+// a binary search finds: those of a smaller token, and in earlier chunks those of its own too.
+// Eight lanes share a pair's searches; all tokens lie in LDS.
+__global__ __launch_bounds__(512) void embed_merge_kernel(EmbedGradArgs a, const uint2 *from, uint2 *to) {
+    extern __shared__ uint32_t tok[];
+    const uint32_t chunks = (a.n + 1023) / 1024;
+#pragma unroll 8
+    for (uint32_t k = threadIdx.x; k < chunks * 1024; k += 512) tok[k] = k < a.n ? from[k].x : 0xffffffffu;
+    __syncthreads();
+    const uint32_t i = blockIdx.x * 64 + threadIdx.x / 8, own = i / 1024;
+    const uint32_t mine = tok[min(i, a.n - 1)];
+    uint32_t place = 0;
+    for (uint32_t c = threadIdx.x % 8; c < chunks; c += 8) {
+        // the first pair of chunk c that is not before this one (0 to 1024)
+        const uint32_t limit = mine + (c < own);  // tokens below it are before; a token is at most 2^30
+        uint32_t low = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < R; r++)
-        if (r * 64 + lane < left) to[i0 + r * 64 + lane] = p[r];
+        for (uint32_t step = 512; step > 0; step /= 2)
+            if (tok[c * 1024 + low + step - 1] < limit) low += step;
+        low += tok[c * 1024 + low] < limit;
+        place += c == own ? i % 1024 : low;
+    }
+    for (int off = 1; off < 8; off <<= 1) place += __shfl_xor(place, off, 64);
+    if (threadIdx.x % 8 == 0 && i < a.n) to[place] = from[i];
 }
 
 // ------------------------------------------------------------------ the sums
 
 // A row of tx threads sums one chunk of a.run sorted positions, N columns per
 // thread, kBatch rows of dy (and the accumulator's rows that they end) on their way at a time.
-constexpr uint32_t kBatch = 8;
+constexpr uint32_t kBatch = 4;  // 131072 x 1024 bf16: 2 112 us, 4 107, 8 155
 
 template <typename T, int N>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const uint2 *pairs, uint32_t tx) {
@@ -278,7 +309,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const u
         uint2 p[kBatch + 1];
 #pragma unroll
         for (uint32_t k = 0; k <= kBatch; k++) p[k] = i + k < a.n ? pairs[i + k] : make_uint2(0xffffffffu, 0u);
-        float v[kBatch][N] = {}, old[kBatch][N] = {};
+        Vec<N, T> v[kBatch];
+        float old[kBatch][N];
         // what becomes of row k: nothing (masked, or past the chunk), added, or added as its run's last here
         bool in[kBatch], last[kBatch], cut[kBatch];
         bool began = head;
@@ -292,20 +324,20 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const u
             const T *row = dy + (uint64_t)p[k].y * a.ld_dy;
             const float *acc = a.grad + (uint64_t)p[k].x * a.ld_grad + c;
             if (whole) {
-                if (in[k]) load<N>(row, v[k]);
+                if (in[k]) v[k] = *(const Vec<N, T> *)row;
                 if (last[k] && !cut[k]) load<N>(acc, old[k]);
             } else {
 #pragma unroll
                 for (uint32_t e = 0; e < N; e++) {
-                    if (e < live && in[k]) v[k][e] = load1(row + e);
-                    if (e < live && last[k] && !cut[k]) old[k][e] = acc[e];
+                    v[k].v[e] = e < live && in[k] ? row[e] : (T)0.0f;
+                    old[k][e] = e < live && last[k] && !cut[k] ? acc[e] : 0.0f;
                 }
             }
         }
 #pragma unroll
         for (uint32_t k = 0; k < kBatch; k++) {
             if (!in[k]) continue;
-            for (int e = 0; e < N; e++) sum[e] += v[k][e];
+            for (int e = 0; e < N; e++) sum[e] += (float)v[k].v[e];
             if (!last[k]) continue;
             float *to = cut[k] ? a.cut + ((uint64_t)chunk * 2 + (head ? 0 : 1)) * a.width + c
                                : a.grad + (uint64_t)p[k].x * a.ld_grad + c;
@@ -325,61 +357,57 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const u
 }
 
 // The runs that leave the chunk they began in: their parts, a quarter per wave, in
-// ascending order.  A workgroup looks after 256 columns of the runs that begin in
-// kJoinChunks chunks.
-constexpr uint32_t kJoinChunks = 4;
+// ascending order.  A workgroup looks after 256 columns of the run that leaves one
+// chunk (four chunks each: 5 us more at 131072 x 1024, 1 us more at 8192 x 128).
 
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const uint2 *pairs) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (a.n + a.run - 1) / a.run;
     const uint32_t c = (blockIdx.y * 64 + lane) * 4, live = c < a.width ? min(4u, a.width - c) : 0;
     __shared__ float part[3][64][4];
-    for (uint32_t chunk = blockIdx.x * kJoinChunks; chunk < (blockIdx.x + 1) * kJoinChunks; chunk++) {
-        const uint64_t i1 = (uint64_t)(chunk + 1) * a.run;
-        if (i1 >= a.n) return;
-        const uint32_t tok = pairs[i1 - 1].x;
-        const uint64_t i0 = i1 - a.run;
-        if (tok >= a.vocab || pairs[i1].x != tok) continue;                      // it ends here
-        if (i0 > 0 && pairs[i0].x == tok && pairs[i0 - 1].x == tok) continue;  // it began earlier
-        // the chunks after this one that begin with the run
-        uint32_t more = 0;
-        for (;; more += 64) {
-            const uint32_t k = chunk + 1 + more + lane;
-            const unsigned long long m = __ballot(k < chunks && pairs[(uint64_t)k * a.run].x == tok);
-            if (m != ~0ull) {
-                more += (uint32_t)__builtin_ctzll(~m);
-                break;
-            }
+    const uint32_t chunk = blockIdx.x;
+    const uint64_t i1 = (uint64_t)(chunk + 1) * a.run, i0 = i1 - a.run;
+    if (i1 >= a.n) return;
+    const uint32_t tok = pairs[i1 - 1].x;
+    if (tok >= a.vocab || pairs[i1].x != tok) return;                      // it ends here
+    if (i0 > 0 && pairs[i0].x == tok && pairs[i0 - 1].x == tok) return;  // it began earlier
+    // the chunks after this one that begin with the run
+    uint32_t more = 0;
+    for (;; more += 64) {
+        const uint32_t k = chunk + 1 + more + lane;
+        const unsigned long long m = __ballot(k < chunks && pairs[(uint64_t)k * a.run].x == tok);
+        if (m != ~0ull) {
+            more += (uint32_t)__builtin_ctzll(~m);
+            break;
         }
-        float sum[4] = {};
-        auto add = [&](const float *from) {
-#pragma unroll
-            for (uint32_t e = 0; e < 4; e++)
-                if (e < live) sum[e] += from[e];
-        };
-        if (wave == 0) add(a.cut + ((uint64_t)chunk * 2 + 1) * a.width + c);
-        const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / 4);
-        uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / 4);
-        if (live == 4) {
-            for (; k + 8 <= k1; k += 8) {
-                float v[8][4];
-#pragma unroll
-                for (uint32_t b = 0; b < 8; b++) load<4>(a.cut + (uint64_t)(k + b) * 2 * a.width + c, v[b]);
-#pragma unroll
-                for (uint32_t b = 0; b < 8; b++)
-                    for (int e = 0; e < 4; e++) sum[e] += v[b][e];
-            }
-        }
-        for (; k < k1; k++) add(a.cut + (uint64_t)k * 2 * a.width + c);
-        __syncthreads();  // the run before has left `part`
-        if (wave > 0)
-            for (int e = 0; e < 4; e++) part[wave - 1][lane][e] = sum[e];
-        __syncthreads();
-        if (wave > 0) continue;
-        float *to = a.grad + (uint64_t)tok * a.ld_grad + c;
+    }
+    float sum[4] = {};
+    auto add = [&](const float *from) {
 #pragma unroll
         for (uint32_t e = 0; e < 4; e++)
-            if (e < live) to[e] = fmaf(a.factor, (sum[e] + part[0][lane][e]) + (part[1][lane][e] + part[2][lane][e]), to[e]);
+            if (e < live) sum[e] += from[e];
+    };
+    if (wave == 0) add(a.cut + ((uint64_t)chunk * 2 + 1) * a.width + c);
+    const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / 4);
+    uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / 4);
+    if (live == 4) {
+        for (; k + 8 <= k1; k += 8) {
+            float v[8][4];
+#pragma unroll
+            for (uint32_t b = 0; b < 8; b++) load<4>(a.cut + (uint64_t)(k + b) * 2 * a.width + c, v[b]);
+#pragma unroll
+            for (uint32_t b = 0; b < 8; b++)
+                for (int e = 0; e < 4; e++) sum[e] += v[b][e];
+        }
     }
+    for (; k < k1; k++) add(a.cut + (uint64_t)k * 2 * a.width + c);
+    if (wave > 0)
+        for (int e = 0; e < 4; e++) part[wave - 1][lane][e] = sum[e];
+    __syncthreads();
+    if (wave > 0) return;
+    float *to = a.grad + (uint64_t)tok * a.ld_grad + c;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; e++)
+        if (e < live) to[e] = fmaf(a.factor, (sum[e] + part[0][lane][e]) + (part[1][lane][e] + part[2][lane][e]), to[e]);
 }
 
 // ---------------------------------------------------------------- launchers
@@ -387,10 +415,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const 
 namespace {
 
 // Threads per row: the power of two that covers `units`, at most 256.
-#ifndef EMB_MANY
-#define EMB_MANY (1ull << 20)
-#endif
-constexpr uint64_t kEmbedManyThreads = EMB_MANY;
+constexpr uint64_t kEmbedManyThreads = 1ull << 20;
 
 uint32_t row_threads(uint32_t units) {
     uint32_t tx = 1;
@@ -447,11 +472,13 @@ hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift
 }
 
 hipError_t launch_embed_sort(const EmbedGradArgs &a, hipStream_t s) {
-    const uint32_t rounds = (a.n + 1023) / 1024;
-    if (rounds <= 1) embed_sort_kernel<1><<<1, 1024, 0, s>>>(a, a.pairs[0]);
-    else if (rounds <= 4) embed_sort_kernel<4><<<1, 1024, 0, s>>>(a, a.pairs[0]);
-    else if (rounds <= 8) embed_sort_kernel<8><<<1, 1024, 0, s>>>(a, a.pairs[0]);
-    else embed_sort_kernel<16><<<1, 1024, 0, s>>>(a, a.pairs[0]);
+    embed_sort_kernel<<<(a.n + 1023) / 1024, 1024, 0, s>>>(a, a.pairs[0]);
+    return hipGetLastError();
+}
+
+hipError_t launch_embed_merge(const EmbedGradArgs &a, hipStream_t s) {
+    const uint32_t bytes = (a.n + 1023) / 1024 * 4096;
+    embed_merge_kernel<<<(a.n + 63) / 64, 512, bytes, s>>>(a, a.pairs[0], a.pairs[1]);
     return hipGetLastError();
 }
 
@@ -463,7 +490,7 @@ hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStrea
 }
 
 hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s) {
-    const dim3 grid((run_chunks(a) + kJoinChunks - 1) / kJoinChunks, (a.width + 255) / 256);
+    const dim3 grid(run_chunks(a), (a.width + 255) / 256);
     embed_join_kernel<<<grid, 256, 0, s>>>(a, a.pairs[sorted]);
     return hipGetLastError();
 }

@@ -672,16 +672,18 @@ def _dtype(t, name: str) -> int:
 
 
 def _rows(t, name: str):
-    """(address, row stride in elements) of a 2-D device tensor whose rows are
-    contiguous."""
+    """(address, row stride in elements, rows, columns) of a 2-D device tensor
+    whose rows are contiguous."""
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a device tensor")
-    if t.dim() != 2:
-        raise ValueError(f"{name}: expected a matrix, got {t.dim()} dimensions")
-    r, c = t.shape
-    if c > 1 and t.stride(1) != 1 or r > 1 and t.stride(0) < c:
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name}: expected a matrix, got {len(shape)} dimensions")
+    r, c = shape
+    sr, sc = t.stride()
+    if c > 1 and sc != 1 or r > 1 and sr < c:
         raise ValueError(f"{name}: expected contiguous rows that do not overlap")
-    return t.data_ptr(), (t.stride(0) if r > 1 else max(c, 1))
+    return t.data_ptr(), (sr if r > 1 else c or 1), r, c
 
 
 class OrthogonalizeCall:
@@ -703,8 +705,8 @@ class OrthogonalizeCall:
                 raise ValueError(f"matrix {k}: expected {mats[0].dtype}, got {g.dtype} and {o.dtype}")
             if g.shape != o.shape:
                 raise ValueError(f"matrix {k}: {tuple(g.shape)} in, {tuple(o.shape)} out")
-            (gp, gl), (op, ol) = _rows(g, f"mats[{k}]"), _rows(o, f"out[{k}]")
-            self.mats[k] = dedloc_matrix(gp, op, gl, ol, *g.shape)
+            (gp, gl, r, c), (op, ol, _, _) = _rows(g, f"mats[{k}]"), _rows(o, f"out[{k}]")
+            self.mats[k] = dedloc_matrix(gp, op, gl, ol, r, c)
         need = load().dedloc_orthogonalize_workspace_bytes(self.mats, len(mats))
         if need == 0:
             raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
@@ -773,10 +775,17 @@ def dedloc_muon_step(x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, g
     return call.ws
 
 
+@functools.lru_cache(maxsize=None)
+def _id_bytes():
+    import torch
+    return {torch.int32: 4, torch.int64: 8}
+
+
 def _ids(ids):
-    """(address, bytes of an id, count) of a tensor of int32 or int64 ids of any shape."""
-    size = ids.element_size()
-    if ids.is_floating_point() or size not in (4, 8):
+    """(address, bytes of an id, count) of a contiguous tensor of int32 or int64
+    ids of any shape."""
+    size = _id_bytes().get(ids.dtype)
+    if size is None:
         raise ValueError(f"ids: expected int32 or int64, got {ids.dtype}")
     return _dev(ids, name="ids"), size, ids.numel()
 
@@ -784,16 +793,16 @@ def _ids(ids):
 def dedloc_embed(table, ids, scale: float = 1.0, out=None, out_dtype=None, stream=None):
     """scale * table[ids], rows of zeros where an id names no row; `out` has a
     row per id (ids.numel() of them) at any stride."""
-    import torch
     p, size, n = _ids(ids)
-    tp, tl = _rows(table, "table")
+    tp, tl, vocab, width = _rows(table, "table")
     if out is None:
-        out = torch.empty(n, table.shape[1], dtype=out_dtype or table.dtype, device=table.device)
-    op, ol = _rows(out, "out")
-    if tuple(out.shape) != (n, table.shape[1]):
-        raise ValueError(f"out: expected {n} rows of {table.shape[1]}, got {tuple(out.shape)}")
-    _check(load().dedloc_embed(tp, _dtype(table, "table"), table.shape[0], table.shape[1], tl, p, size, n, scale, op,
-                               _dtype(out, "out"), ol, _stream(stream)))
+        import torch
+        out = torch.empty(n, width, dtype=out_dtype or table.dtype, device=table.device)
+    op, ol, r, c = _rows(out, "out")
+    if r != n or c != width:
+        raise ValueError(f"out: expected {n} rows of {width}, got {tuple(out.shape)}")
+    _check(load().dedloc_embed(tp, _dtype(table, "table"), vocab, width, tl, p, size, n, scale, op, _dtype(out, "out"),
+                               ol, _stream(stream)))
     return out
 
 
@@ -810,15 +819,15 @@ def dedloc_embed_grad(grad, ids, dy, scale: float = 1.0, batch_samples: float = 
     """grad[ids[i]] += scale * batch_samples * dy[i] for every id that names a
     row of the fp32 accumulator `grad`; returns it."""
     p, size, n = _ids(ids)
-    gp, gl = _rows(grad, "grad")
-    dp, dl = _rows(dy, "dy")
+    gp, gl, vocab, width = _rows(grad, "grad")
+    dp, dl, r, c = _rows(dy, "dy")
     if grad.dtype is not _float32():
         raise ValueError(f"grad: expected float32, got {grad.dtype}")
-    if tuple(dy.shape) != (n, grad.shape[1]):
-        raise ValueError(f"dy: expected {n} rows of {grad.shape[1]}, got {tuple(dy.shape)}")
+    if r != n or c != width:
+        raise ValueError(f"dy: expected {n} rows of {width}, got {tuple(dy.shape)}")
     if ws is None:
-        ws = make_embed_workspace(n, *grad.shape, grad.device)
-    _check(load().dedloc_embed_grad(gp, *grad.shape, gl, p, size, n, dp, _dtype(dy, "dy"), dl, scale, batch_samples,
+        ws = make_embed_workspace(n, vocab, width, grad.device)
+    _check(load().dedloc_embed_grad(gp, vocab, width, gl, p, size, n, dp, _dtype(dy, "dy"), dl, scale, batch_samples,
                                     _dev(ws, name="ws"), _nbytes(ws), _stream(stream)))
     return grad
 
