@@ -17,11 +17,6 @@ static_assert(kNsMaxShort == DEDLOC_ORTHO_MAX_SHORT && kNsMaxLong == DEDLOC_ORTH
 
 namespace {
 
-#ifndef NS_BLOCKED
-#define NS_BLOCKED (1ull << 26)
-#endif
-constexpr uint64_t kNsBlocked = NS_BLOCKED;
-
 uint32_t blocks(uint64_t n, uint32_t per) { return (uint32_t)((n + per - 1) / per); }
 
 int check_sides(uint32_t k, uint32_t rows, uint32_t cols) {
@@ -90,6 +85,8 @@ void make_program(const dedloc_ortho_cfg &c, bool blocked, Program &p) {
         turn = 3 - turn;
     }
 }
+
+constexpr uint64_t kNsBlocked = 1ull << 26;
 
 // Whether a matrix is worked on in blocks of steps.  Five steps as blocks of three and two
 // are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15: worth it from

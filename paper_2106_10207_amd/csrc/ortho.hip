@@ -29,6 +29,7 @@
 // on one of the L2's channels.)
 // Both factors of every product have the summed index along their rows: the
 // small matrices are symmetric, and X^T is kept beside X.
+#include <algorithm>
 #include <type_traits>
 
 #include "ops_internal.h"
@@ -117,8 +118,8 @@ __device__ inline double block_sum(double v) {
 }  // namespace
 
 // Sums of squares in 64 bits, one per block of kNsTile rows and columns.
-template <int SRC>
-__global__ __launch_bounds__(256) void ns_sum_kernel(NsTable t, NsArgs a) {
+template <int SRC, int N>
+__global__ __launch_bounds__(256) void ns_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin, across = (m.cols + kNsTile - 1) / kNsTile;
     const uint32_t r0 = k / across * kNsTile, col = k % across * kNsTile + threadIdx.x % kNsTile;
@@ -134,8 +135,8 @@ __global__ __launch_bounds__(256) void ns_sum_kernel(NsTable t, NsArgs a) {
 
 // Muon: m' = fma(mu, m, g), and the sums of squares of the update, one per
 // kSumChunk elements.
-template <int SRC>
-__global__ __launch_bounds__(256) void muon_sum_kernel(NsTable t, NsArgs a) {
+template <int SRC, int N>
+__global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin;
     const uint64_t n = (uint64_t)m.rows * m.cols, end = (uint64_t)(k + 1) * kSumChunk < n ? (uint64_t)(k + 1) * kSumChunk : n;
@@ -153,8 +154,8 @@ __global__ __launch_bounds__(256) void muon_sum_kernel(NsTable t, NsArgs a) {
 
 // X0 and its transpose in two planes, zeros in the padding: one workgroup per
 // block of 64 x 64 of the matrix as it is stored.
-template <int SRC>
-__global__ __launch_bounds__(256) void ns_prepare_kernel(NsTable t, NsArgs a) {
+template <int SRC, int N>
+__global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) {
     const uint32_t q = find(t.m, t.n, blockIdx.x);
     const NsMat &m = t.m[q];
     const Sides d = sides(m.rows, m.cols);
@@ -347,10 +348,7 @@ struct Shape {
     static constexpr uint32_t edge = EDGE, wi = WI, wj = WJ, waves = EDGE / 32 * EDGE / 32 / (WI * WJ), stages = STAGES,
                               per_simd = PER_SIMD;
 };
-#ifndef NS_BIG
-#define NS_BIG 128, 2, 2, 2, 2
-#endif
-typedef Shape<NS_BIG> Big;
+typedef Shape<128, 2, 2, 2, 2> Big;
 typedef Shape<64, 1, 1, 4, 2> Little;
 
 // One tile of a product of a step over a piece of the summed index.  OUT: the dtype of a result, or
@@ -364,8 +362,8 @@ typedef Shape<64, 1, 1, 4, 2> Little;
 // lanes of a read, one row each, meet all 64 banks (with r % 8 two rows met in a bank
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
-template <int OUT, typename C>
-__global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(NsWorks t, NsArgs a) {
+template <int OUT, typename C, int N>
+__global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(NsList<N> t, NsArgs a) {
     constexpr uint32_t T = C::edge, NW = C::waves, WI = C::wi, WJ = C::wj, NS = C::stages;
     // workgroups go round the 8 XCDs: give each a contiguous range of items
     const uint32_t per = gridDim.x / 8, odd = gridDim.x % 8, xcd = blockIdx.x % 8;
@@ -487,8 +485,8 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
 
 // A block of 32 x 32 of a product whose summed index was cut: a workgroup adds up its pieces, a quarter of them
 // per wave, in an order that only their number decides.  One workgroup per block of each tile.
-template <int OUT, typename C>
-__global__ __launch_bounds__(256) void ns_join_kernel(NsWorks t, NsArgs a) {
+template <int OUT, typename C, int N>
+__global__ __launch_bounds__(256) void ns_join_kernel(NsList<N> t, NsArgs a) {
     constexpr uint32_t T = C::edge, WI = C::wi, WJ = C::wj, kBlocks = T * T / 1024;
     // the table counts items, a work's tiles once for every piece
     uint32_t k = blockIdx.x / kBlocks, q = 0;
@@ -527,7 +525,29 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsWorks t, NsArgs a) {
 
 // ---------------------------------------------------------------- launchers
 
-hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+namespace {
+
+// The table in as few arguments as it fits.
+template <typename F>
+void with_table(const NsTable &t, F launch) {
+    if (t.n > (uint32_t)kNsFew) return launch(t);
+    NsMats<kNsFew> few;
+    std::copy(t.m, t.m + t.n, few.m);
+    few.n = t.n;
+    few.parts = t.parts;
+    launch(few);
+}
+template <typename F>
+void with_table(const NsWorks &t, F launch) {
+    if (t.n > (uint32_t)kNsFew) return launch(t);
+    NsList<kNsFew> few;
+    std::copy(t.w, t.w + t.n, few.w);
+    few.n = t.n;
+    launch(few);
+}
+
+template <int N>
+void sums(int src, const NsMats<N> &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
     switch (src) {
         case kNsF32: ns_sum_kernel<kNsF32><<<groups, 256, 0, s>>>(t, a); break;
         case kNsFP16: ns_sum_kernel<kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
@@ -536,10 +556,9 @@ hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t gr
         case kNsMuonFP16: muon_sum_kernel<kNsMuonFP16><<<groups, 256, 0, s>>>(t, a); break;
         default: muon_sum_kernel<kNsMuonI8><<<groups, 256, 0, s>>>(t, a); break;
     }
-    return hipGetLastError();
 }
-
-hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+template <int N>
+void prepare(int src, const NsMats<N> &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
     switch (src) {
         case kNsF32: ns_prepare_kernel<kNsF32><<<groups, 256, 0, s>>>(t, a); break;
         case kNsFP16: ns_prepare_kernel<kNsFP16><<<groups, 256, 0, s>>>(t, a); break;
@@ -548,21 +567,18 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
         case kNsMuonFP16: ns_prepare_kernel<kNsMuonFP16><<<groups, 256, 0, s>>>(t, a); break;
         default: ns_prepare_kernel<kNsMuonI8><<<groups, 256, 0, s>>>(t, a); break;
     }
-    return hipGetLastError();
 }
-
-namespace {
-template <typename C>
-void product(int out, const NsWorks &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+template <typename C, int N>
+void product(int out, const NsList<N> &t, const NsArgs &a, uint32_t items, hipStream_t s) {
     switch (out) {
-        case kNsF32: ns_product_kernel<kNsF32, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
-        case kNsFP16: ns_product_kernel<kNsFP16, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
-        case kNsBF16: ns_product_kernel<kNsBF16, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
-        default: ns_product_kernel<kNsMuonF32, C><<<groups, 64 * C::waves, 0, s>>>(t, a); break;
+        case kNsF32: ns_product_kernel<kNsF32, C><<<items, 64 * C::waves, 0, s>>>(t, a); break;
+        case kNsFP16: ns_product_kernel<kNsFP16, C><<<items, 64 * C::waves, 0, s>>>(t, a); break;
+        case kNsBF16: ns_product_kernel<kNsBF16, C><<<items, 64 * C::waves, 0, s>>>(t, a); break;
+        default: ns_product_kernel<kNsMuonF32, C><<<items, 64 * C::waves, 0, s>>>(t, a); break;
     }
 }
-template <typename C>
-void join(int out, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
+template <typename C, int N>
+void join(int out, const NsList<N> &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
     const uint32_t groups = tiles * (C::edge * C::edge / 1024);
     switch (out) {
         case kNsF32: ns_join_kernel<kNsF32, C><<<groups, 256, 0, s>>>(t, a); break;
@@ -571,17 +587,32 @@ void join(int out, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_
         default: ns_join_kernel<kNsMuonF32, C><<<groups, 256, 0, s>>>(t, a); break;
     }
 }
+
 }  // namespace
 
+hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    with_table(t, [&](const auto &q) { sums(src, q, a, groups, s); });
+    return hipGetLastError();
+}
+
+hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
+    with_table(t, [&](const auto &q) { prepare(src, q, a, groups, s); });
+    return hipGetLastError();
+}
+
 hipError_t launch_ns_product(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t items, hipStream_t s) {
-    if (edge == 128) product<Big>(out, t, a, items, s);
-    else product<Little>(out, t, a, items, s);
+    with_table(t, [&](const auto &q) {
+        if (edge == 128) product<Big>(out, q, a, items, s);
+        else product<Little>(out, q, a, items, s);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s) {
-    if (edge == 128) join<Big>(out, t, a, tiles, s);
-    else join<Little>(out, t, a, tiles, s);
+    with_table(t, [&](const auto &q) {
+        if (edge == 128) join<Big>(out, q, a, tiles, s);
+        else join<Little>(out, q, a, tiles, s);
+    });
     return hipGetLastError();
 }
 
