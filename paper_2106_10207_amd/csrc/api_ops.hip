@@ -87,6 +87,7 @@ void make_program(const dedloc_ortho_cfg &c, bool blocked, Program &p) {
 }
 
 constexpr uint64_t kNsBlocked = 1ull << 26;
+constexpr uint32_t kNarrowMost = 512;  // workgroups
 
 // Whether a matrix is worked on in blocks of steps.  Five steps as blocks of three and two
 // are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15: worth it from
@@ -234,9 +235,37 @@ Items cut_works(NsWorks &t, Cut c) {
     return n;
 }
 
+// Whether a batch takes the narrow path, a launch per step: every shorter side at
+// most 128, few enough turns per workgroup, no more workgroups than the GPU takes at once.  Sets up
+// the works, the workgroups and the widest matrix.  Narrow against the products' path, us:
+// 64 x 64 48 / 81, 64 x 1024 (one turn) 61 / 113, 64 x 4096 (four) 102 / 115, 64 x 8192 (eight) 153 / 120;
+// 128 x 128 81 / 93, 128 x 1024 (two) 117 / 110, eight of them 138 / 160, 32 205 / 262.
+struct Narrow {
+    NsWorks t;
+    uint32_t groups, widest;
+    uint64_t floats() const { return (uint64_t)groups * narrow_part(widest); }  // of one set of parts
+};
+bool narrow(const Batch &b, Narrow &n) {
+    n.groups = n.widest = 0;
+    n.t.n = b.t.n;
+    for (uint32_t k = 0; k < b.t.n; k++) {
+        NsWork &w = n.t.w[k] = b.w[k];
+        const uint32_t S = padded(std::min(w.rows, w.cols)), L = padded(std::max(w.rows, w.cols));
+        if (S > kNarrowShort) return false;
+        const uint32_t tiles = L / kNarrowCols, most = S == 64 ? 16 : 8, subs = blocks(tiles, most);
+        if (subs > (S == 64 ? 4u : b.t.n >= 4 ? 2u : 1u)) return false;
+        w.pieces = blocks(tiles, subs);
+        w.op |= subs << 20;
+        w.begin = n.groups;
+        n.groups += w.pieces;
+        n.widest = std::max(n.widest, S);
+    }
+    return n.groups <= kNarrowMost && 2 * n.floats() * sizeof(float) <= b.piece_bytes();
+}
+
 // The steps on a batch.  src: where the matrices come from; out: where the
 // results go (a dtype, or kNsMuonF32).
-int run_batch(Batch &b, const Program p[2], int src, int out, NsArgs a, void *ws, hipStream_t s) {
+int run_batch(Batch &b, const Program p[2], uint32_t steps, int src, int out, NsArgs a, void *ws, hipStream_t s) {
     a.ws = (char *)ws;
     a.part = (double *)((char *)ws + b.regions);
     a.pieces = (float *)((char *)ws + b.regions + b.part_bytes());
@@ -246,6 +275,18 @@ int run_batch(Batch &b, const Program p[2], int src, int out, NsArgs a, void *ws
     g = b.spread([&](const NsMat &m) { return blocks(m.rows, kNsPad) * blocks(m.cols, kNsPad); });
     e = timed(K_NS_PREPARE, s, [&] { return launch_ns_prepare(src, b.t, a, g, s); });
     if (e != hipSuccess) return hip_fail(e, "prepare launch");
+    Narrow n;
+    if (narrow(b, n)) {
+        // the parts of A go to one half of the room for pieces and come from the other
+        for (uint32_t k = 0; k <= steps; k++) {
+            float *to = a.pieces + (k % 2) * n.floats(), *from = a.pieces + (1 - k % 2) * n.floats();
+            e = timed(K_NS_NARROW, s, [&] {
+                return launch_ns_narrow(out, n.t, a, from, to, k == 0, k == steps, n.groups, n.widest, s);
+            });
+            if (e != hipSuccess) return hip_fail(e, "narrow step launch");
+        }
+        return DEDLOC_OK;
+    }
     NsWorks t;
     for (uint32_t k = 0; k < std::max(p[0].n, p[1].n); k++) {
         works_of(b, p, k, t);
@@ -417,7 +458,7 @@ int dedloc_orthogonalize(const dedloc_matrix *mats, uint32_t n, int32_t dtype, c
             const dedloc_matrix &m = mats[k];
             b.add(m.in, m.ld_in, m.out, m.ld_out, m.rows, m.cols, 0, 0.0f);
         },
-        [&](Batch &b) { return run_batch(b, p, dtype, dtype, a, ws, (hipStream_t)stream); });
+        [&](Batch &b) { return run_batch(b, p, cfg->steps, dtype, dtype, a, ws, (hipStream_t)stream); });
 }
 
 size_t dedloc_muon_workspace_bytes(const uint32_t *rows, const uint32_t *cols, uint32_t n_tensors) {
@@ -493,7 +534,7 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
                 flags[k] & DEDLOC_TENSOR_ADAPT ? (double)cfg->rms * sqrt((double)std::max(rows[k], cols[k])) : 1.0;
             b.add(nullptr, offsets[k], nullptr, offsets[k], rows[k], cols[k], flags[k], (float)((double)cfg->lr * ratio));
         },
-        [&](Batch &b) { return run_batch(b, p, src, kNsMuonF32, a, ws, (hipStream_t)stream); });
+        [&](Batch &b) { return run_batch(b, p, cfg->ortho.steps, src, kNsMuonF32, a, ws, (hipStream_t)stream); });
 }
 
 int dedloc_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_t width, uint64_t ld_table,

@@ -63,7 +63,7 @@ struct NsWork {
     uint32_t rows, cols;
     uint32_t begin;   // its first work item in this launch
     uint32_t pieces;  // that the summed index is cut into
-    uint32_t op;      // kind | left << 4 | right << 8 | out << 12 (buffers) | decay << 16
+    uint32_t op;      // kind | left << 4 | right << 8 | out << 12 (buffers) | decay << 16; narrow: turns << 20
     float unit;       // Muon: lr * s_t
 };
 template <int N>
@@ -85,6 +85,12 @@ struct NsArgs {
     int32_t nesterov;
 };
 
+// Narrow matrices: a workgroup owns kNarrowCols columns of X and, of a long matrix,
+// as many more times as leave at most 16 workgroups (8 with a side of 128; each adds up
+// every part of A: 16 KB of a side of 64, 64 KB less the upper triangle of 128).
+constexpr uint32_t kNarrowShort = 128;
+constexpr uint32_t kNarrowCols = 64;
+
 // Where prepare takes its matrix from: a dtype of orthogonalize, or the Muon
 // step's update formed from the momentum and a gradient of this codec.
 enum NsSrc : int { kNsF32 = 0, kNsFP16 = 1, kNsBF16 = 2, kNsMuonF32 = 3, kNsMuonFP16 = 4, kNsMuonI8 = 5 };
@@ -96,6 +102,12 @@ hipError_t launch_ns_prepare(int src, const NsTable &t, const NsArgs &a, uint32_
 // table; join takes their number of tiles.
 hipError_t launch_ns_product(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t items, hipStream_t s);
 hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs &a, uint32_t tiles, hipStream_t s);
+
+// A step of narrow matrices.  widest: the largest S among them; the parts of A, one of narrow_part(widest) floats per
+// workgroup, are read from `from` and left in `to`.
+inline uint32_t narrow_part(uint32_t widest) { return (widest / 32) * (widest / 32 + 1) / 2 * 1024; }
+hipError_t launch_ns_narrow(int out, const NsWorks &t, const NsArgs &a, const float *from, float *to, bool first, bool last,
+                            uint32_t groups, uint32_t widest, hipStream_t s);
 
 // ------------------------------------------------ embedding and its gradient
 

@@ -204,6 +204,46 @@ struct Vec {
 
 constexpr uint32_t kTurnPitch = 36;  // words of a row of a block that is turned in LDS
 
+// A block of the call's result: the lane's row is i of X; acc[4 g + e] belongs to
+// column j0 + 8 g + 4 (lane / 32) + e.
+template <int OUT>
+__device__ inline void ns_result(const NsWork &m, const Sides &d, const NsArgs &a, uint32_t i, uint32_t j0, const f32x16 &acc) {
+    const uint32_t lane = threadIdx.x & 63;
+            if (i >= d.s) return;
+            const uint64_t ld = OUT == kNsMuonF32 ? m.cols : m.ld_out;
+            const uint64_t step = d.tall ? ld : 1;  // from column j to the next
+    #pragma unroll
+            for (uint32_t g = 0; g < 4; g++) {
+                const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
+                if (j >= d.l) break;
+                const uint32_t n = min(4u, d.l - j);
+                const uint64_t at = d.tall ? j * ld + i : i * ld + j;
+                float v[4];
+                for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (1.0f / (kAScale * kXScale));
+                if constexpr (OUT == kNsMuonF32) {
+                    float *x = a.x + m.ld_out + at;
+                    const float keep = (m.op >> 16 & 1) ? a.keep : 1.0f;
+                    if (!d.tall && n == 4) {
+                        Vec<4, float> q = *(const Vec<4, float> *)x;
+                        for (int e = 0; e < 4; e++) q.v[e] = fmaf(-m.unit, v[e], keep * q.v[e]);
+                        *(Vec<4, float> *)x = q;
+                    } else {
+                        for (uint32_t e = 0; e < n; e++) x[e * step] = fmaf(-m.unit, v[e], keep * x[e * step]);
+                    }
+                } else {
+                    typedef std::conditional_t<OUT == kNsF32, float, std::conditional_t<OUT == kNsFP16, _Float16, __bf16>> T;
+                    T *to = (T *)m.out + at;
+                    if (!d.tall && n == 4) {
+                        Vec<4, T> q;
+                        for (int e = 0; e < 4; e++) q.v[e] = (T)v[e];
+                        *(Vec<4, T> *)to = q;
+                    } else {
+                        for (uint32_t e = 0; e < n; e++) to[e * step] = (T)v[e];
+                    }
+                }
+            }
+}
+
 // What a block of 32 x 32 (rows i0, columns j0 on) of a product becomes.  The lane's
 // row is i = i0 + lane % 32; acc[4 g + e] belongs to column j0 + 8 g + 4 (lane / 32) + e.
 // turn: 32 * kTurnPitch words of the wave's own in LDS, through which the block goes
@@ -212,42 +252,7 @@ template <int OUT>
 __device__ inline void ns_finish(const NsWork &m, const Sides &d, const NsArgs &a, uint32_t i0, uint32_t j0, const f32x16 &acc,
                                  uint32_t *turn) {
     const uint32_t lane = threadIdx.x & 63, il = lane % 32, i = i0 + il, kind = m.op & 15;
-    if (kind == kNsResult) {
-        if (i >= d.s) return;
-        const uint64_t ld = OUT == kNsMuonF32 ? m.cols : m.ld_out;
-        const uint64_t step = d.tall ? ld : 1;  // from column j to the next
-#pragma unroll
-        for (uint32_t g = 0; g < 4; g++) {
-            const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
-            if (j >= d.l) break;
-            const uint32_t n = min(4u, d.l - j);
-            const uint64_t at = d.tall ? j * ld + i : i * ld + j;
-            float v[4];
-            for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (1.0f / (kAScale * kXScale));
-            if constexpr (OUT == kNsMuonF32) {
-                float *x = a.x + m.ld_out + at;
-                const float keep = (m.op >> 16 & 1) ? a.keep : 1.0f;
-                if (!d.tall && n == 4) {
-                    Vec<4, float> q = *(const Vec<4, float> *)x;
-                    for (int e = 0; e < 4; e++) q.v[e] = fmaf(-m.unit, v[e], keep * q.v[e]);
-                    *(Vec<4, float> *)x = q;
-                } else {
-                    for (uint32_t e = 0; e < n; e++) x[e * step] = fmaf(-m.unit, v[e], keep * x[e * step]);
-                }
-            } else {
-                typedef std::conditional_t<OUT == kNsF32, float, std::conditional_t<OUT == kNsFP16, _Float16, __bf16>> T;
-                T *to = (T *)m.out + at;
-                if (!d.tall && n == 4) {
-                    Vec<4, T> q;
-                    for (int e = 0; e < 4; e++) q.v[e] = (T)v[e];
-                    *(Vec<4, T> *)to = q;
-                } else {
-                    for (uint32_t e = 0; e < n; e++) to[e * step] = (T)v[e];
-                }
-            }
-        }
-        return;
-    }
+    if (kind == kNsResult) return ns_result<OUT>(m, d, a, i, j0, acc);
     const float scale = kind == kNsGram ? kAScale / (kXScale * kXScale) : 1.0f / kAScale;
     char *to = buffer(a, m.base, d, kind == kNsApply ? 0 : m.op >> 12 & 15) + at_planes(i, j0, d.S);
     const char *old = buffer(a, m.base, d, m.op >> 4 & 15) + at_planes(i, j0, d.S);
@@ -523,6 +528,202 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsList<N> t, NsArgs a) {
     ns_finish<OUT>(m, d, a, i, j, acc, turn);
 }
 
+// -------------------------------------------------------- narrow matrices
+
+// Matrices whose shorter side is at most 128 take a launch per step instead of
+// three or four: the work of each is too little to be worth the launches (4.5 us each, of which
+// 1.3 pass before the kernel's first instruction).  A workgroup owns kNarrowCols * subs columns
+// of X.  It adds up the parts of A = X X^T that all workgroups of its matrix left
+// at the launch before, forms M in LDS, takes its columns through X <- M X, and leaves
+// its part of the next A.  Each workgroup forms M for itself: 128^3 multiply-adds, three times, 1.5 us.
+//
+// LDS, two-plane panels as in memory with the product's swizzle: A and then M
+// [s][s], the columns' X^T [64][s], and X [s][64] for the next A.
+template <typename F>
+__device__ inline void put_block(char *lds, uint32_t rows, uint32_t i0, uint32_t j0, bool mirror, F value) {
+    const uint32_t lane = threadIdx.x & 63, i = i0 + lane % 32;
+#pragma unroll
+    for (uint32_t g = 0; g < 4; g++) {
+        const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            _Float16 h, w;
+            split(value(g, e), h, w);
+            hi[e] = h;
+            lo[e] = w;
+        }
+        if (mirror) {  // element (j + e, i)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                char *row = lds + ((i / 32) * rows + j + e) * 128;
+                const uint32_t turn = (j + e) / 2 % 8, c = i % 32 / 8, at = i % 8 * 2;
+                *(_Float16 *)(row + ((c ^ turn) * 16) + at) = hi[e];
+                *(_Float16 *)(row + (((c + 4) ^ turn) * 16) + at) = lo[e];
+            }
+        } else {
+            char *row = lds + ((j / 32) * rows + i) * 128;
+            const uint32_t turn = i / 2 % 8, c = j % 32 / 8, at = j % 8 * 2;
+            *(f16x4 *)(row + ((c ^ turn) * 16) + at) = hi;
+            *(f16x4 *)(row + (((c + 4) ^ turn) * 16) + at) = lo;
+        }
+    }
+}
+// Elements (i, j) to (i, j + 3), j a multiple of 4.
+__device__ inline void get_entries(const char *lds, uint32_t rows, uint32_t i, uint32_t j, float *v) {
+    const char *row = lds + ((j / 32) * rows + i) * 128;
+    const uint32_t turn = i / 2 % 8, c = j % 32 / 8, at = j % 8 * 2;
+    const f16x4 hi = *(const f16x4 *)(row + ((c ^ turn) * 16) + at), lo = *(const f16x4 *)(row + (((c + 4) ^ turn) * 16) + at);
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
+}
+// acc += rows i0 on of `left` times rows j0 on of `right`, over `panels` panels.
+__device__ inline void multiply_blocks(const char *left, uint32_t left_rows, uint32_t i0, const char *right, uint32_t right_rows,
+                                       uint32_t j0, uint32_t panels, f32x16 &acc) {
+    const uint32_t lane = threadIdx.x & 63, i = i0 + lane % 32, j = j0 + lane % 32;
+    for (uint32_t p = 0; p < panels; p += 2) {  // a multiple of two: every read of two panels before their products
+        f16x8 lh[4], ll[4], rh[4], rl[4];
+#pragma unroll
+        for (uint32_t h = 0; h < 4; h++) {
+            const char *l = left + ((p + h / 2) * left_rows + i) * 128, *r = right + ((p + h / 2) * right_rows + j) * 128;
+            const uint32_t c = h % 2 * 2 + lane / 32;
+            lh[h] = *(const f16x8 *)(l + ((c ^ (i / 2 % 8)) * 16));
+            rl[h] = *(const f16x8 *)(r + (((c + 4) ^ (j / 2 % 8)) * 16));
+            ll[h] = *(const f16x8 *)(l + (((c + 4) ^ (i / 2 % 8)) * 16));
+            rh[h] = *(const f16x8 *)(r + ((c ^ (j / 2 % 8)) * 16));
+        }
+#pragma unroll
+        for (uint32_t h = 0; h < 4; h++) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], lh[h], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], ll[h], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], lh[h], acc, 0, 0, 0);
+        }
+    }
+}
+
+// first: X is X0, and only its A is formed.  Parts are read from `from` and left in `to`.
+template <int OUT, int N>
+__global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, const float *from, float *to, uint32_t part_floats,
+                                                        int first, int last) {
+    const NsWork &m = t.w[find(t.w, t.n, blockIdx.x)];
+    const Sides d = sides(m.rows, m.cols);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t S = d.S, nb = S / 32, lower = nb * (nb + 1) / 2, wg = blockIdx.x - m.begin;
+    const uint32_t subs = m.op >> 20, groups = m.pieces;
+    extern __shared__ __align__(1024) char lds[];
+    char *sq = lds, *xt = lds + S * S * 4, *xg = xt + kNarrowCols * S * 4;
+    const float *parts = from + (uint64_t)m.begin * part_floats;
+    float *part = to + (uint64_t)blockIdx.x * part_floats;
+    // the blocks of A that this wave looks after: `wave` and `wave` + 8 of the lower triangle, row by row
+    auto block_of = [&](uint32_t b, uint32_t &bi, uint32_t &bj) {
+        bi = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3;
+        bj = b - bi * (bi + 1) / 2;
+    };
+    if (!first) {
+        f32x16 v[2] = {};
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            const uint32_t b = wave + 8 * q;
+            if (b >= lower) continue;
+#pragma unroll 8
+            for (uint32_t p = 0; p < groups; p++)
+#pragma unroll
+                for (uint32_t g = 0; g < 4; g++)
+                    *((f32x4 *)&v[q] + g) += *(const f32x4 *)(parts + (uint64_t)p * part_floats + b * 1024 + g * 256 + lane * 4);
+            uint32_t bi, bj;
+            block_of(b, bi, bj);
+            auto value = [&](uint32_t g, int e) { return v[q][4 * g + e] * (kAScale / (kXScale * kXScale)); };
+            put_block(sq, S, bi * 32, bj * 32, false, value);
+            if (bi != bj) put_block(sq, S, bi * 32, bj * 32, true, value);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            const uint32_t b = wave + 8 * q;
+            if (b >= lower) continue;
+            uint32_t bi, bj;
+            block_of(b, bi, bj);
+            f32x16 acc = {};
+            multiply_blocks(sq, S, bi * 32, sq, S, bj * 32, nb, acc);
+#pragma unroll
+            for (uint32_t g = 0; g < 4; g++) {
+                const uint32_t i = bi * 32 + lane % 32, j = bj * 32 + 8 * g + 4 * (lane / 32);
+                float old[4];
+                get_entries(sq, S, i, j, old);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float x = fmaf(a.b, old[e], a.c * (acc[4 * g + e] * (1.0f / kAScale)));
+                    v[q][4 * g + e] = i == j + e ? fmaf(a.a, kAScale, x) : x;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            const uint32_t b = wave + 8 * q;
+            if (b >= lower) continue;
+            uint32_t bi, bj;
+            block_of(b, bi, bj);
+            auto value = [&](uint32_t g, int e) { return v[q][4 * g + e]; };
+            put_block(sq, S, bi * 32, bj * 32, false, value);
+            if (bi != bj) put_block(sq, S, bi * 32, bj * 32, true, value);
+        }
+    }
+    f32x16 gram[2] = {};
+    for (uint32_t sub = 0; sub < subs; sub++) {
+        const uint32_t l0 = (wg * subs + sub) * kNarrowCols;
+        if (l0 >= d.L) break;
+        // 16-byte pieces of X^T's rows l0 on (for X0: of X's columns), to their swizzled places
+        char *const mem = buffer(a, m.base, d, first ? 0 : 1);
+        const uint32_t rows = first ? S : kNarrowCols, panels = first ? kNarrowCols / 32 : nb;
+        auto piece_at = [&](uint32_t k) {  // of piece k: its place in memory
+            const uint32_t p = k / (rows * 8), r = k / 8 % rows;
+            return mem + (first ? ((uint64_t)(l0 / 32 + p) * S + r) : ((uint64_t)p * d.L + l0 + r)) * 128 + k % 8 * 16;
+        };
+        auto swizzled = [&](uint32_t k) { return k / 8 * 128 + ((k % 8) ^ (k / 8 % rows / 2 % 8)) * 16; };
+        for (uint32_t k = threadIdx.x; k < panels * rows * 8; k += 512)
+            *(u32x4 *)((first ? xg : xt) + swizzled(k)) = *(const u32x4 *)piece_at(k);
+        __syncthreads();
+        if (!first) {
+            // blocks (bi, bj) of X' [s][64]: 2 nb of them, one per wave
+            const uint32_t bi = wave / 2, bj = wave % 2;
+            f32x16 acc = {};
+            if (bi < nb) multiply_blocks(sq, S, bi * 32, xt, kNarrowCols, bj * 32, nb, acc);
+            if (last) {
+                if (bi < nb) ns_result<OUT>(m, d, a, bi * 32 + lane % 32, l0 + bj * 32, acc);
+                __syncthreads();
+                continue;
+            }
+            __syncthreads();
+            if (bi < nb) {
+                auto value = [&](uint32_t g, int e) { return acc[4 * g + e] * (1.0f / kAScale); };
+                put_block(xg, S, bi * 32, bj * 32, false, value);
+                put_block(xt, kNarrowCols, bi * 32, bj * 32, true, value);
+            }
+            __syncthreads();
+            for (uint32_t k = threadIdx.x; k < panels * rows * 8; k += 512)
+                *(u32x4 *)piece_at(k) = *(const u32x4 *)(xt + swizzled(k));
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            const uint32_t b = wave + 8 * q;
+            if (b >= lower) continue;
+            uint32_t bi, bj;
+            block_of(b, bi, bj);
+            multiply_blocks(xg, S, bi * 32, xg, S, bj * 32, kNarrowCols / 32, gram[q]);
+        }
+        __syncthreads();
+    }
+    if (last) return;
+#pragma unroll
+    for (uint32_t q = 0; q < 2; q++) {
+        const uint32_t b = wave + 8 * q;
+        if (b >= lower) continue;
+#pragma unroll
+        for (uint32_t g = 0; g < 4; g++) *(f32x4 *)(part + b * 1024 + g * 256 + lane * 4) = *((const f32x4 *)&gram[q] + g);
+    }
+}
+
 // ---------------------------------------------------------------- launchers
 
 namespace {
@@ -614,6 +815,28 @@ hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs
         else join<Little>(out, q, a, tiles, s);
     });
     return hipGetLastError();
+}
+
+hipError_t launch_ns_narrow(int out, const NsWorks &t, const NsArgs &a, const float *from, float *to, bool first, bool last,
+                            uint32_t groups, uint32_t widest, hipStream_t s) {
+    const uint32_t lds = widest * widest * 4 + 2 * kNarrowCols * widest * 4;
+    hipError_t e = hipSuccess;
+    with_table(t, [&](const auto &q) {
+        auto go = [&](auto kernel) {
+            // beyond the default of 64 KB; at every launch, since it belongs to the current device
+            if (lds > 65536)
+                e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e == hipSuccess) kernel<<<groups, 512, lds, s>>>(q, a, from, to, narrow_part(widest), first, last);
+        };
+        constexpr int N = sizeof(q.w) / sizeof(q.w[0]);
+        switch (out) {
+            case kNsF32: go(ns_narrow_kernel<kNsF32, N>); break;
+            case kNsFP16: go(ns_narrow_kernel<kNsFP16, N>); break;
+            case kNsBF16: go(ns_narrow_kernel<kNsBF16, N>); break;
+            default: go(ns_narrow_kernel<kNsMuonF32, N>); break;
+        }
+    });
+    return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace dedloc

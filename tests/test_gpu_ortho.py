@@ -136,6 +136,20 @@ def test_blocks_of_steps(steps, a):
         check(o, m, steps=steps, abc=abc)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shapes", [[(128, 64)], [(100, 8192)], [(8192, 64)], [(64, 8256), (3, 9000)], [(128, 4096)], [(128, 4160)],
+                                    [(65, 66), (20, 4000), (128, 1024), (1, 1), (4000, 33)], [(96, 70)] * 9,
+                                    [(64, 4096)] * 70])
+def test_narrow(dtype, shapes):
+    """Matrices of at most 128 on their shorter side, a launch per step, and just beyond what that path takes."""
+    g = [up(matrix(*s, seed=k), dtype, pad=k % 3) for k, s in enumerate(shapes)]
+    for o, m in zip(D.dedloc_orthogonalize(g), g):
+        check(o, m)
+    for steps in (1, 2, 4):
+        for o, m in zip(D.dedloc_orthogonalize(g[:3], cfg=D.ortho_cfg(steps=steps)), g):
+            check(o, m, steps=steps)
+
+
 @pytest.mark.parametrize("scale", [1e-15, 1e15])
 def test_range_of_the_input(scale):
     g = up(matrix(64, 100, seed=1) * scale, torch.float32)
