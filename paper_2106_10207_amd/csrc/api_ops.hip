@@ -361,9 +361,12 @@ EmbedWs embed_ws(uint64_t n, uint32_t width) {
     w.pairs = round_up((size_t)n * sizeof(uint2), 256);
     const uint32_t tiles = std::max(1u, blocks(n, kSortTile));
     w.chunk = (tiles + kSortChunks - 1) / kSortChunks * kSortTile;
-    // short chunks where there are few (8192 x 128: 8 positions 31 us, 32 43; 131072 x 1024: 8 246, 32 181)
-    w.run = n * width < 1u << 22 ? 8 : 32;
-    w.counts = (size_t)blocks(n, w.chunk) * 256 * sizeof(uint32_t);
+    // Short chunks where there is little to sum, long ones where the parts of cut runs are many.  4, 8, 16, 32 positions, us: 1000 x
+    // 512 14, 16, 21, 29; 8192 x 128 22.9, 22.2, 24.5, 30; 8192 x 768 28.7, 27.3, 30.3, 39; 40000 x 333 88, 81, 76, 95; 65536 x 1024
+    // 147, 102, 84, 75.
+    const uint64_t all = n * width;
+    w.run = all < 1u << 20 ? 4 : all < 1u << 23 ? 8 : all < 1u << 25 ? 16 : 32;
+    w.counts = ((size_t)blocks(n, w.chunk) << kSortBits) * sizeof(uint32_t);
     w.total = 2 * w.pairs + w.counts + round_up((size_t)blocks(n, w.run) * 2 * width * sizeof(float), 256);
     w.total = std::max(w.total, (size_t)256);
     return w;
@@ -579,13 +582,18 @@ int dedloc_embed_grad(float *grad, uint64_t vocab, uint32_t width, uint64_t ld_g
             from = 1;
         }
     }
-    // digits of the tokens and of `vocab`, which stands for a masked position
-    for (uint32_t shift = 0; n > kSortOne && (shift == 0 || vocab >> shift); shift += 8) {
-        hipError_t e = timed(K_EMBED_COUNT, s, [&] { return launch_embed_count(a, from, shift, s); });
-        if (e != hipSuccess) return hip_fail(e, "embed count launch");
-        e = timed(K_EMBED_SCATTER, s, [&] { return launch_embed_scatter(a, from, shift, s); });
-        if (e != hipSuccess) return hip_fail(e, "embed scatter launch");
-        from = from < 0 ? 0 : 1 - from;
+    if (n > kSortOne) {
+        // as few digits as hold the tokens and `vocab`, which stands for a masked position
+        uint32_t all = 1;
+        while (vocab >> all) all++;
+        const uint32_t passes = (all + kSortBits - 1) / kSortBits, bits = std::max(8u, (all + passes - 1) / passes);
+        for (uint32_t shift = 0; shift < all; shift += bits) {
+            hipError_t e = timed(K_EMBED_COUNT, s, [&] { return launch_embed_count(a, from, bits, shift, s); });
+            if (e != hipSuccess) return hip_fail(e, "embed count launch");
+            e = timed(K_EMBED_SCATTER, s, [&] { return launch_embed_scatter(a, from, bits, shift, s); });
+            if (e != hipSuccess) return hip_fail(e, "embed scatter launch");
+            from = from < 0 ? 0 : 1 - from;
+        }
     }
     hipError_t e = timed(K_EMBED_SUM, s, [&] { return launch_embed_sum(dy_dtype, a, from, s); });
     if (e != hipSuccess) return hip_fail(e, "embed sum launch");

@@ -118,31 +118,32 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {
 
 // ------------------------------------------------------------------ the sort
 
-// One pass orders the positions by 8 bits of their token, keeping the order of
-// equal ones.  Chunk k counts its digits into counts[k][256].
+// One pass orders the positions by a digit of their token, BITS bits, keeping the
+// order of equal ones.  Chunk k counts its digits into counts[k][2^BITS].
 template <bool FIRST>
 __device__ inline uint2 pair_at(const EmbedGradArgs &a, const uint2 *from, uint32_t i) {
     if (FIRST) return make_uint2(token(a.ids, a.wide_ids, a.vocab, i), i);
     return from[i];
 }
 
-template <bool FIRST>
+template <bool FIRST, int BITS>
 __global__ __launch_bounds__(256) void embed_count_kernel(EmbedGradArgs a, const uint2 *from, uint32_t shift) {
-    __shared__ uint32_t count[256];
-    count[threadIdx.x] = 0;
+    constexpr uint32_t D = 1u << BITS;
+    __shared__ uint32_t count[D];
+    for (uint32_t d = threadIdx.x; d < D; d += 256) count[d] = 0;
     __syncthreads();
     const uint32_t i0 = blockIdx.x * a.chunk, i1 = min(i0 + a.chunk, a.n);
-    for (uint32_t i = i0 + threadIdx.x; i < i1; i += 256)
-        atomicAdd(&count[(pair_at<FIRST>(a, from, i).x >> shift) & 255u], 1u);
+    for (uint32_t i = i0 + threadIdx.x; i < i1; i += 256) atomicAdd(&count[(pair_at<FIRST>(a, from, i).x >> shift) & (D - 1)], 1u);
     __syncthreads();
-    a.counts[blockIdx.x * 256 + threadIdx.x] = count[threadIdx.x];
+    for (uint32_t d = threadIdx.x; d < D; d += 256) a.counts[blockIdx.x * D + d] = count[d];
 }
 
-// The lanes of a wave that have the same 8-bit digit (of those with `in`).
+// The lanes of a wave that have the same digit (of those with `in`).
+template <int BITS>
 __device__ inline unsigned long long same_digit(uint32_t digit, bool in) {
     unsigned long long same = __ballot(in);
 #pragma unroll
-    for (int b = 0; b < 8; b++) {
+    for (int b = 0; b < BITS; b++) {
         const unsigned long long m = __ballot((digit >> b) & 1u);
         same &= (digit >> b) & 1u ? m : ~m;
     }
@@ -150,16 +151,16 @@ __device__ inline unsigned long long same_digit(uint32_t digit, bool in) {
 }
 
 // Positions of a wave, 64 a round, in order: an item's rank is how many of the
-// wave's items before it have its digit.  at[256]: the wave's counters, zeroed by
+// wave's items before it have its digit.  at[2^BITS]: the wave's counters, zeroed by
 // the caller; afterwards how many items have each digit.
-template <uint32_t R>
+template <uint32_t R, int BITS>
 __device__ inline void rank_digits(const uint2 *p, uint32_t left, uint32_t shift, uint32_t *at, uint16_t *rank) {
     const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
     for (uint32_t r = 0; r < R; r++) {
         const bool in = r * 64 + lane < left;
-        const uint32_t digit = (p[r].x >> shift) & 255u;
-        const unsigned long long same = same_digit(digit, in);
+        const uint32_t digit = (p[r].x >> shift) & ((1u << BITS) - 1);
+        const unsigned long long same = same_digit<BITS>(digit, in);
         const uint32_t mine = __popcll(same & ((1ull << lane) - 1));
         rank[r] = (uint16_t)(at[digit] + mine);
         wave_order();
@@ -182,24 +183,33 @@ __device__ inline uint32_t scan_256(uint32_t v, uint32_t *part) {
     return scan - v;
 }
 
-template <bool FIRST>
+template <bool FIRST, int BITS>
 __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, const uint2 *from, uint2 *to, uint32_t shift) {
-    constexpr uint32_t R = kSortTile / 256;
-    __shared__ uint32_t at[4][256];  // per wave and digit
+    constexpr uint32_t R = kSortTile / 256, D = 1u << BITS, E = D / 256;
+    __shared__ uint32_t at[4][D];  // per wave and digit
     __shared__ uint32_t part[4];
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, chunks = gridDim.x;
-    // the first place of digit t: all smaller digits, and this digit in the chunks before
-    uint32_t before = 0, all = 0;
+    // the first places of digits E t on: all smaller digits, and the same digit in the chunks before
+    uint32_t before[E] = {}, all[E] = {}, sum = 0;
 #pragma unroll 16
-    for (uint32_t k = 0; k < chunks; k++) {
-        const uint32_t c = a.counts[k * 256 + t];
-        all += c;
-        before += k < blockIdx.x ? c : 0;
+    for (uint32_t k = 0; k < chunks; k++)
+#pragma unroll
+        for (uint32_t e = 0; e < E; e++) {
+            const uint32_t c = a.counts[k * D + t * E + e];
+            all[e] += c;
+            before[e] += k < blockIdx.x ? c : 0;
+        }
+#pragma unroll
+    for (uint32_t e = 0; e < E; e++) sum += all[e];
+    uint32_t next = scan_256(sum, part), start[E];
+#pragma unroll
+    for (uint32_t e = 0; e < E; e++) {
+        start[e] = next + before[e];
+        next += all[e];
     }
-    uint32_t start = scan_256(all, part) + before;
     const uint32_t end = min((blockIdx.x + 1) * a.chunk, a.n);
     for (uint32_t tile = blockIdx.x * a.chunk; tile < end; tile += kSortTile) {
-        for (int w = 0; w < 4; w++) at[w][t] = 0;
+        for (uint32_t d = t; d < 4 * D; d += 256) (&at[0][0])[d] = 0;
         // each wave takes a quarter of the tile, in order
         const uint32_t i0 = tile + wave * (kSortTile / 4), left = i0 < end ? end - i0 : 0;
         uint2 p[R];
@@ -208,17 +218,19 @@ __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, con
         for (uint32_t r = 0; r < R; r++)
             p[r] = r * 64 + lane < left ? pair_at<FIRST>(a, from, i0 + r * 64 + lane) : make_uint2(0xffffffffu, 0u);
         __syncthreads();
-        rank_digits<R>(p, left, shift, at[wave], rank);
+        rank_digits<R, BITS>(p, left, shift, at[wave], rank);
         __syncthreads();
-        for (int w = 0; w < 4; w++) {
-            const uint32_t c = at[w][t];
-            at[w][t] = start;
-            start += c;
-        }
+#pragma unroll
+        for (uint32_t e = 0; e < E; e++)
+            for (int w = 0; w < 4; w++) {
+                const uint32_t c = at[w][t * E + e];
+                at[w][t * E + e] = start[e];
+                start[e] += c;
+            }
         __syncthreads();
 #pragma unroll
         for (uint32_t r = 0; r < R; r++)
-            if (r * 64 + lane < left) to[at[wave][(p[r].x >> shift) & 255u] + rank[r]] = p[r];
+            if (r * 64 + lane < left) to[at[wave][(p[r].x >> shift) & (D - 1)] + rank[r]] = p[r];
         __syncthreads();
     }
 }
@@ -236,7 +248,7 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2
         for (uint32_t k = t; k < 16 * 256; k += 1024) (&at[0][0])[k] = 0;
         __syncthreads();
         uint16_t rank;
-        rank_digits<1>(&p, left, shift, at[wave], &rank);
+        rank_digits<1, 8>(&p, left, shift, at[wave], &rank);
         __syncthreads();
         uint32_t c[16], all = 0;
         if (t < 256)
@@ -262,23 +274,38 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2
 // a binary search finds: those of a smaller token, and in earlier chunks those of its own too.
 // Eight lanes share a pair's searches; all tokens lie in LDS.
 __global__ __launch_bounds__(512) void embed_merge_kernel(EmbedGradArgs a, const uint2 *from, uint2 *to) {
-    extern __shared__ uint32_t tok[];
+    extern __shared__ __align__(16) uint32_t tok[];
     const uint32_t chunks = (a.n + 1023) / 1024;
-#pragma unroll 8
-    for (uint32_t k = threadIdx.x; k < chunks * 1024; k += 512) tok[k] = k < a.n ? from[k].x : 0xffffffffu;
+#pragma unroll 16
+    for (uint32_t k = threadIdx.x * 2; k < chunks * 1024; k += 1024) {
+        uint4 p = make_uint4(0xffffffffu, 0u, 0xffffffffu, 0u);
+        if (k + 1 < a.n) p = *(const uint4 *)(from + k);
+        else if (k < a.n) p.x = from[k].x;
+        *(uint2 *)(tok + k) = make_uint2(p.x, p.z);
+    }
     __syncthreads();
     const uint32_t i = blockIdx.x * 64 + threadIdx.x / 8, own = i / 1024;
     const uint32_t mine = tok[min(i, a.n - 1)];
     uint32_t place = 0;
-    for (uint32_t c = threadIdx.x % 8; c < chunks; c += 8) {
-        // the first pair of chunk c that is not before this one (0 to 1024)
-        const uint32_t limit = mine + (c < own);  // tokens below it are before; a token is at most 2^30
-        uint32_t low = 0;
+    for (uint32_t c0 = threadIdx.x % 8; c0 < chunks; c0 += 16) {
+        // in two chunks at a time: the first pair that is not before this one (0 to 1024)
+        uint32_t low[2] = {}, limit[2], at[2];
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            const uint32_t c = c0 + 8 * q;
+            limit[q] = c < chunks ? mine + (c < own) : 0;  // tokens below it are before; a token is at most 2^30
+            at[q] = min(c, chunks - 1) * 1024;
+        }
 #pragma unroll
         for (uint32_t step = 512; step > 0; step /= 2)
-            if (tok[c * 1024 + low + step - 1] < limit) low += step;
-        low += tok[c * 1024 + low] < limit;
-        place += c == own ? i % 1024 : low;
+#pragma unroll
+            for (uint32_t q = 0; q < 2; q++)
+                if (tok[at[q] + low[q] + step - 1] < limit[q]) low[q] += step;
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            low[q] += tok[at[q] + low[q]] < limit[q];
+            place += c0 + 8 * q == own ? i % 1024 : low[q];
+        }
     }
     for (int off = 1; off < 8; off <<= 1) place += __shfl_xor(place, off, 64);
     if (threadIdx.x % 8 == 0 && i < a.n) to[place] = from[i];
@@ -381,25 +408,29 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const 
         }
     }
     float sum[4] = {};
-    auto add = [&](const float *from) {
+    if (wave == 0) {
+        const float *from = a.cut + ((uint64_t)chunk * 2 + 1) * a.width + c;
 #pragma unroll
         for (uint32_t e = 0; e < 4; e++)
-            if (e < live) sum[e] += from[e];
-    };
-    if (wave == 0) add(a.cut + ((uint64_t)chunk * 2 + 1) * a.width + c);
+            if (e < live) sum[e] = from[e];
+    }
     const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / 4);
     uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / 4);
-    if (live == 4) {
-        for (; k + 8 <= k1; k += 8) {
-            float v[8][4];
+    for (; k < k1; k += 8) {
+        float v[8][4] = {};
 #pragma unroll
-            for (uint32_t b = 0; b < 8; b++) load<4>(a.cut + (uint64_t)(k + b) * 2 * a.width + c, v[b]);
+        for (uint32_t b = 0; b < 8; b++) {
+            const float *from = a.cut + (uint64_t)(k + b) * 2 * a.width + c;
+            if (k + b < k1 && live == 4) load<4>(from, v[b]);
+            if (k + b < k1 && live < 4)
 #pragma unroll
-            for (uint32_t b = 0; b < 8; b++)
-                for (int e = 0; e < 4; e++) sum[e] += v[b][e];
+                for (uint32_t e = 0; e < 3; e++)
+                    if (e < live) v[b][e] = from[e];
         }
+#pragma unroll
+        for (uint32_t b = 0; b < 8; b++)
+            for (int e = 0; e < 4; e++) sum[e] += v[b][e];
     }
-    for (; k < k1; k++) add(a.cut + (uint64_t)k * 2 * a.width + c);
     if (wave > 0)
         for (int e = 0; e < 4; e++) part[wave - 1][lane][e] = sum[e];
     __syncthreads();
@@ -459,15 +490,30 @@ hipError_t launch_embed(int table, int out, const EmbedArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s) {
-    if (from < 0) embed_count_kernel<true><<<sort_chunks(a), 256, 0, s>>>(a, nullptr, shift);
-    else embed_count_kernel<false><<<sort_chunks(a), 256, 0, s>>>(a, a.pairs[from], shift);
+namespace {
+template <int BITS>
+void count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s) {
+    if (from < 0) embed_count_kernel<true, BITS><<<sort_chunks(a), 256, 0, s>>>(a, nullptr, shift);
+    else embed_count_kernel<false, BITS><<<sort_chunks(a), 256, 0, s>>>(a, a.pairs[from], shift);
+}
+template <int BITS>
+void scatter(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s) {
+    if (from < 0) embed_scatter_kernel<true, BITS><<<sort_chunks(a), 256, 0, s>>>(a, nullptr, a.pairs[0], shift);
+    else embed_scatter_kernel<false, BITS><<<sort_chunks(a), 256, 0, s>>>(a, a.pairs[from], a.pairs[1 - from], shift);
+}
+}  // namespace
+
+hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t bits, uint32_t shift, hipStream_t s) {
+    if (bits <= 8) count<8>(a, from, shift, s);
+    else if (bits == 9) count<9>(a, from, shift, s);
+    else count<kSortBits>(a, from, shift, s);
     return hipGetLastError();
 }
 
-hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s) {
-    if (from < 0) embed_scatter_kernel<true><<<sort_chunks(a), 256, 0, s>>>(a, nullptr, a.pairs[0], shift);
-    else embed_scatter_kernel<false><<<sort_chunks(a), 256, 0, s>>>(a, a.pairs[from], a.pairs[1 - from], shift);
+hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t bits, uint32_t shift, hipStream_t s) {
+    if (bits <= 8) scatter<8>(a, from, shift, s);
+    else if (bits == 9) scatter<9>(a, from, shift, s);
+    else scatter<kSortBits>(a, from, shift, s);
     return hipGetLastError();
 }
 

@@ -118,6 +118,7 @@ constexpr uint32_t kEmbedMaxWidth = 1u << 20;
 // workgroup each: every workgroup reads the digit counts of all chunks.
 constexpr uint32_t kSortTile = 2048;
 constexpr uint32_t kSortChunks = 512;
+constexpr uint32_t kSortBits = 10;  // of a digit at most
 // Up to kSortOne positions are sorted in chunks of 1024 and merged.
 constexpr uint32_t kSortOne = 16384;
 
@@ -154,9 +155,10 @@ hipError_t launch_embed(int table, int out, const EmbedArgs &a, hipStream_t s);
 // The sort of at most kSortOne positions: chunks of 1024 into pairs[0], merged into pairs[1].
 hipError_t launch_embed_sort(const EmbedGradArgs &a, hipStream_t s);
 hipError_t launch_embed_merge(const EmbedGradArgs &a, hipStream_t s);
-// One pass over 8 bits; from: the buffer that holds the pairs, or -1: the ids.
-hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
-hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t shift, hipStream_t s);
+// One pass over a digit of 8 bits (fewer are taken as 8), 9 or kSortBits; from: the
+// buffer that holds the pairs, or -1: the ids.
+hipError_t launch_embed_count(const EmbedGradArgs &a, int from, uint32_t bits, uint32_t shift, hipStream_t s);
+hipError_t launch_embed_scatter(const EmbedGradArgs &a, int from, uint32_t bits, uint32_t shift, hipStream_t s);
 hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStream_t s);
 hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s);
 

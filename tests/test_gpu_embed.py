@@ -119,7 +119,9 @@ def grad_case(dy_dtype, n, vocab, width, pad, offset, kind, wide, seed):
                                                       (33, 255, 128, 0, 0), (64, 256, 33, 0, 0), (2047, 257, 9, 1, 0),
                                                       (2049, 65535, 40, 0, 0), (4500, 65536, 24, 0, 2),
                                                       (9000, 70000, 16, 0, 0), (700, 1 << 20, 4, 0, 0),
-                                                      (100, 40, 1100, 0, 0), (16385, 1000, 8, 0, 0), (70001, 3000, 3, 0, 0)])
+                                                      (100, 40, 1100, 0, 0), (16384, 40000, 2, 0, 0), (16385, 1000, 8, 0, 0), (70001, 3000, 3, 0, 0),
+                                                      (16500, 100000, 3, 0, 0), (17000, 1000000, 2, 0, 0),
+                                                      (17000, (1 << 21) + 5, 1, 0, 0)])
 def test_embed_grad(dy, n, vocab, width, pad, offset):
     grad_case(dy, n, vocab, width, pad, offset, "zipf", n % 2 == 0, n)
 
