@@ -114,7 +114,8 @@ struct Batch {
     }
     bool fits(uint32_t rows, uint32_t cols) const { return works + 1 + blocked(rows, cols) <= (uint32_t)kNsWorks; }
     uint32_t sums(const NsMat &m) const {
-        return muon ? blocks((uint64_t)m.rows * m.cols, kSumChunk) : blocks(m.rows, kNsTile) * blocks(m.cols, kNsTile);
+        const uint32_t n = muon ? blocks((uint64_t)m.rows * m.cols, kSumChunk) : blocks(m.rows, kNsTile) * blocks(m.cols, kNsTile);
+        return std::min(n, kSumMost);
     }
     void add(const void *in, uint64_t ld_in, void *out, uint64_t ld_out, uint32_t rows, uint32_t cols, uint32_t flags, float unit) {
         const uint64_t s = padded(std::min(rows, cols)), l = padded(std::max(rows, cols));

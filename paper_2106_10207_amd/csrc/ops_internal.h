@@ -20,7 +20,9 @@ constexpr uint32_t kNsPad = 64;   // both sides of a matrix are padded with zero
 constexpr uint32_t kNsTile = 64;  // edge of a block of the elementwise passes
 constexpr uint32_t kNsMaxShort = 32768;
 constexpr uint32_t kNsMaxLong = 1u << 26;
-constexpr uint32_t kSumChunk = 8192;  // flat elements summed by one workgroup of the momentum pass
+constexpr uint32_t kSumChunk = 8192;  // flat elements that a workgroup of the momentum pass sums at a time
+// Sums of squares of a matrix at most: every workgroup of the next pass adds them all up, 8 a thread.
+constexpr uint32_t kSumMost = 2048;
 
 // A matrix has a region of the workspace.  s is its shorter side, l the longer; S
 // and L are s and l rounded up to kNsPad.  The region holds, 4 bytes an element,

@@ -117,36 +117,43 @@ __device__ inline double block_sum(double v) {
 
 }  // namespace
 
-// Sums of squares in 64 bits, one per block of kNsTile rows and columns.
+// Sums of squares in 64 bits, each of every kSumMost-th block of kNsTile rows and
+// columns: one block for most matrices.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void ns_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin, across = (m.cols + kNsTile - 1) / kNsTile;
-    const uint32_t r0 = k / across * kNsTile, col = k % across * kNsTile + threadIdx.x % kNsTile;
+    const uint32_t blocks = across * ((m.rows + kNsTile - 1) / kNsTile);
     double sum = 0.0;
-    if (col < m.cols)
-        for (uint32_t r = r0 + threadIdx.x / kNsTile; r < r0 + kNsTile && r < m.rows; r += 256 / kNsTile) {
-            const double v = entry<SRC>(a, m, r, col);
-            sum = fma(v, v, sum);
-        }
+    for (uint32_t b = k; b < blocks; b += kSumMost) {
+        const uint32_t r0 = b / across * kNsTile, col = b % across * kNsTile + threadIdx.x % kNsTile;
+        if (col < m.cols)
+            for (uint32_t r = r0 + threadIdx.x / kNsTile; r < r0 + kNsTile && r < m.rows; r += 256 / kNsTile) {
+                const double v = entry<SRC>(a, m, r, col);
+                sum = fma(v, v, sum);
+            }
+    }
     sum = block_sum(sum);
     if (threadIdx.x == 0) a.part[m.part + k] = sum;
 }
 
-// Muon: m' = fma(mu, m, g), and the sums of squares of the update, one per
-// kSumChunk elements.
+// Muon: m' = fma(mu, m, g), and the sums of squares of the update, each of every
+// kSumMost-th chunk of kSumChunk elements.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
     const uint32_t k = blockIdx.x - m.begin;
-    const uint64_t n = (uint64_t)m.rows * m.cols, end = (uint64_t)(k + 1) * kSumChunk < n ? (uint64_t)(k + 1) * kSumChunk : n;
+    const uint64_t n = (uint64_t)m.rows * m.cols;
     double sum = 0.0;
-    for (uint64_t i = (uint64_t)k * kSumChunk + threadIdx.x; i < end; i += 256) {
-        const uint64_t e = m.ld_in + i;
-        const float g = grad_at<SRC>(a, e), mom = fmaf(a.mu, a.mom[e], g);
-        a.mom[e] = mom;
-        const double u = a.nesterov ? fmaf(a.mu, mom, g) : mom;
-        sum = fma(u, u, sum);
+    for (uint64_t i0 = (uint64_t)k * kSumChunk; i0 < n; i0 += (uint64_t)kSumMost * kSumChunk) {
+        const uint64_t end = min(i0 + kSumChunk, n);
+        for (uint64_t i = i0 + threadIdx.x; i < end; i += 256) {
+            const uint64_t e = m.ld_in + i;
+            const float g = grad_at<SRC>(a, e), mom = fmaf(a.mu, a.mom[e], g);
+            a.mom[e] = mom;
+            const double u = a.nesterov ? fmaf(a.mu, mom, g) : mom;
+            sum = fma(u, u, sum);
+        }
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) a.part[m.part + k] = sum;
@@ -209,39 +216,39 @@ constexpr uint32_t kTurnPitch = 36;  // words of a row of a block that is turned
 template <int OUT>
 __device__ inline void ns_result(const NsWork &m, const Sides &d, const NsArgs &a, uint32_t i, uint32_t j0, const f32x16 &acc) {
     const uint32_t lane = threadIdx.x & 63;
-            if (i >= d.s) return;
-            const uint64_t ld = OUT == kNsMuonF32 ? m.cols : m.ld_out;
-            const uint64_t step = d.tall ? ld : 1;  // from column j to the next
-    #pragma unroll
-            for (uint32_t g = 0; g < 4; g++) {
-                const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
-                if (j >= d.l) break;
-                const uint32_t n = min(4u, d.l - j);
-                const uint64_t at = d.tall ? j * ld + i : i * ld + j;
-                float v[4];
-                for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (1.0f / (kAScale * kXScale));
-                if constexpr (OUT == kNsMuonF32) {
-                    float *x = a.x + m.ld_out + at;
-                    const float keep = (m.op >> 16 & 1) ? a.keep : 1.0f;
-                    if (!d.tall && n == 4) {
-                        Vec<4, float> q = *(const Vec<4, float> *)x;
-                        for (int e = 0; e < 4; e++) q.v[e] = fmaf(-m.unit, v[e], keep * q.v[e]);
-                        *(Vec<4, float> *)x = q;
-                    } else {
-                        for (uint32_t e = 0; e < n; e++) x[e * step] = fmaf(-m.unit, v[e], keep * x[e * step]);
-                    }
-                } else {
-                    typedef std::conditional_t<OUT == kNsF32, float, std::conditional_t<OUT == kNsFP16, _Float16, __bf16>> T;
-                    T *to = (T *)m.out + at;
-                    if (!d.tall && n == 4) {
-                        Vec<4, T> q;
-                        for (int e = 0; e < 4; e++) q.v[e] = (T)v[e];
-                        *(Vec<4, T> *)to = q;
-                    } else {
-                        for (uint32_t e = 0; e < n; e++) to[e * step] = (T)v[e];
-                    }
-                }
+    if (i >= d.s) return;
+    const uint64_t ld = OUT == kNsMuonF32 ? m.cols : m.ld_out;
+    const uint64_t step = d.tall ? ld : 1;  // from column j to the next
+#pragma unroll
+    for (uint32_t g = 0; g < 4; g++) {
+        const uint32_t j = j0 + 8 * g + 4 * (lane / 32);
+        if (j >= d.l) break;
+        const uint32_t n = min(4u, d.l - j);
+        const uint64_t at = d.tall ? j * ld + i : i * ld + j;
+        float v[4];
+        for (int e = 0; e < 4; e++) v[e] = acc[4 * g + e] * (1.0f / (kAScale * kXScale));
+        if constexpr (OUT == kNsMuonF32) {
+            float *x = a.x + m.ld_out + at;
+            const float keep = (m.op >> 16 & 1) ? a.keep : 1.0f;
+            if (!d.tall && n == 4) {
+                Vec<4, float> q = *(const Vec<4, float> *)x;
+                for (int e = 0; e < 4; e++) q.v[e] = fmaf(-m.unit, v[e], keep * q.v[e]);
+                *(Vec<4, float> *)x = q;
+            } else {
+                for (uint32_t e = 0; e < n; e++) x[e * step] = fmaf(-m.unit, v[e], keep * x[e * step]);
             }
+        } else {
+            typedef std::conditional_t<OUT == kNsF32, float, std::conditional_t<OUT == kNsFP16, _Float16, __bf16>> T;
+            T *to = (T *)m.out + at;
+            if (!d.tall && n == 4) {
+                Vec<4, T> q;
+                for (int e = 0; e < 4; e++) q.v[e] = (T)v[e];
+                *(Vec<4, T> *)to = q;
+            } else {
+                for (uint32_t e = 0; e < n; e++) to[e * step] = (T)v[e];
+            }
+        }
+    }
 }
 
 // What a block of 32 x 32 (rows i0, columns j0 on) of a product becomes.  The lane's
@@ -392,7 +399,7 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
     constexpr uint32_t kLoads = 2 * T / 8 / NW;
     const uint32_t from = wave * 1024 + (lane / 8) * 128 + ((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16;
     const uint64_t left_panel = (uint64_t)left_rows * 128, right_panel = (uint64_t)right_rows * 128;
-    const uint32_t left_end = (left_rows - i0) * 128, right_end = (right_rows - j0) * 128;
+    const uint32_t left_end = min(left_rows - i0, T) * 128, right_end = min(right_rows - j0, T) * 128;
     const uint32_t first = (uint64_t)(K / 32) * tile.piece / m.pieces;
     const uint32_t panels = (uint32_t)((uint64_t)(K / 32) * (tile.piece + 1) / m.pieces) - first;
     left += (uint64_t)i0 * 128 + first * left_panel;

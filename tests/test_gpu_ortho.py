@@ -267,3 +267,81 @@ def test_muon_other_stream_and_graph():
     for how in ("stream", "graph"):
         for (x, m), (wx, wm) in zip(steps(4, how), want):
             assert torch.equal(x, wx) and torch.equal(m, wm)
+
+
+@pytest.mark.parametrize("shapes", [[(128, 96), (100, 300)], [(200, 300), (130, 70)], [(256, 1400), (80, 500)]],
+                         ids=["narrow", "products", "blocks"])
+def test_orthogonalize_in_a_graph(shapes):
+    """Every replay on new input equals the call, for each way a batch is worked on."""
+    gs = [up(matrix(r, c, 3 + i), torch.float32) for i, (r, c) in enumerate(shapes)]
+    outs = [torch.empty_like(g) for g in gs]
+    call = D.OrthogonalizeCall(gs, outs)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for turn in range(4):
+        for i, g in enumerate(gs):
+            g.copy_(torch.from_numpy(matrix(*g.shape, 10 * turn + i)).float())
+        for o in outs:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, o in zip(gs, outs):
+            check(o, g)
+            (o * 2).sum().item()  # eager work between the replays
+        got = [o.clone() for o in outs]
+        call()
+        assert all(torch.equal(a, o) for a, o in zip(got, outs))
+
+
+@pytest.mark.parametrize("tall", [False, True])
+def test_more_columns_than_a_32_bit_panel(tall):
+    """A panel of X^T, 128 bytes a column, passes 2^32 bytes; the definition on the device, in 64 bits."""
+    l = (1 << 25) + 40
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    g = torch.randn(2, l, generator=gen, device=DEV)
+    g[1] += 0.5 * g[0]
+    if tall:
+        g = g.t().contiguous()
+    out = torch.empty_like(g)
+    D.dedloc_orthogonalize([g], [out], D.ortho_cfg(steps=2))
+    x = (g.t() if tall else g).double()
+    norm = torch.sqrt((x * x).sum())
+    x /= norm + 1e-7
+    a, b, c = ABC
+    tol = 0.0
+    for _ in range(2):
+        tol = 4 * tol + 2.0 ** -20 * (abs(a) + 2 * abs(b) + 4 * abs(c)) * float(torch.sqrt((x * x).sum()))
+        A = torch.stack([torch.stack([(x[i] * x[j]).sum() for j in range(2)]) for i in range(2)])
+        M = b * A + c * torch.stack([torch.stack([(A[i] * A[j]).sum() for j in range(2)]) for i in range(2)])
+        M += a * torch.eye(2, device=DEV, dtype=torch.float64)
+        x = torch.stack([M[i, 0] * x[0] + M[i, 1] * x[1] for i in range(2)])
+    x -= out.t() if tall else out
+    err = float(torch.sqrt((x * x).sum()))
+    print(f"error {err:.3g} of {tol:.3g}")
+    assert err <= tol + 2.0 ** -24 * 2
+
+
+@pytest.mark.parametrize("shape", [(64, 140100), (66000, 130)])
+def test_more_sums_than_the_next_pass_adds_up(shape):
+    """Sums of squares over more than 2048 blocks, with most of the norm in the last of them."""
+    g = matrix(*shape, 11)
+    g[-40:, -40:] *= 50
+    g = up(g, torch.float32)
+    check(D.dedloc_orthogonalize([g], cfg=D.ortho_cfg(steps=3))[0], g, steps=3)
+
+
+def test_muon_on_more_chunks_than_the_next_pass_adds_up():
+    """Momentum 0 and no decay: m' is the gradient, x' the orthogonalised gradient times the rate."""
+    shape = (65, 270000)  # 2143 chunks
+    n = shape[0] * shape[1]
+    g = matrix(*shape, 12)
+    g[-1, -9000:] *= 50
+    g = torch.from_numpy(g).float().to(DEV)
+    x, m = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    cfg = D.muon_cfg(lr=1.0, momentum=0.0, weight_decay=0.0, nesterov=False)
+    D.dedloc_muon_step(x, m, g.reshape(-1), [0, n], [shape], [0], cfg)
+    assert torch.equal(m, g.reshape(-1))
+    check(-x.view(shape), g)
