@@ -17,10 +17,6 @@ namespace dedloc {
 
 namespace {
 
-__device__ inline float load1(const float *p) { return *p; }
-__device__ inline float load1(const _Float16 *p) { return (float)*p; }
-__device__ inline float load1(const __bf16 *p) { return (float)*p; }
-
 // N elements at any alignment of the element, as floats and back.
 template <int N, typename T>
 struct Vec {
@@ -79,39 +75,27 @@ __device__ inline uint32_t token(const void *ids, int wide, uint32_t vocab, uint
 }  // namespace
 
 // A row of threads (tx of them, a power of two) per position, N elements per
-// thread and turn; ROWS positions at a time, whose loads are all on their way
-// before the first is scaled.
-template <typename TI, typename TO, int N, int ROWS>
+// thread and turn.  Bound by memory once there is enough to move: 131072 x 1024 bf16
+// 75 us, 7.1 TB/s read and written, 32768 x 1024 21 us, 6.4 TB/s (a plain copy of 2 GB: 5.0);
+// below 16 MB by the launch, 6 us.  Four positions per row of threads, all loaded before the
+// first is stored, took the same times within 3 %.
+template <typename TI, typename TO, int N>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {
     const uint32_t x = threadIdx.x & (tx - 1), rows = 256 / tx;
-    const uint64_t row0 = (uint64_t)blockIdx.x * (rows * ROWS) + threadIdx.x / tx;
-    uint32_t tok[ROWS];
-#pragma unroll
-    for (int k = 0; k < ROWS; k++) {
-        const uint64_t row = row0 + k * rows;
-        tok[k] = row < a.n ? token(a.ids, a.wide_ids, a.vocab, (uint32_t)row) : a.vocab;
-    }
+    const uint64_t row = (uint64_t)blockIdx.x * rows + threadIdx.x / tx;
+    if (row >= a.n) return;
+    const uint32_t tok = token(a.ids, a.wide_ids, a.vocab, (uint32_t)row);
+    const bool named = tok < a.vocab;
+    const TI *from = (const TI *)a.table + (uint64_t)tok * a.ld_table;  // read only if named
+    TO *to = (TO *)a.out + row * a.ld_out;
     for (uint32_t c = x * N; c < a.width; c += tx * N) {
-        const bool whole = c + N <= a.width;
-        float v[ROWS][N] = {};
-        if (whole) {
-#pragma unroll
-            for (int k = 0; k < ROWS; k++)
-                if (tok[k] < a.vocab) load<N>((const TI *)a.table + (uint64_t)tok[k] * a.ld_table + c, v[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < ROWS; k++) {
-            const uint64_t row = row0 + k * rows;
-            if (row >= a.n) break;
-            const bool named = tok[k] < a.vocab;
-            TO *to = (TO *)a.out + row * a.ld_out;
-            if (whole) {
-                for (int i = 0; i < N; i++) v[k][i] = named ? times(v[k][i], a.scale) : 0.0f;
-                store_stream<N>(to + c, v[k]);
-            } else {
-                const TI *from = (const TI *)a.table + (uint64_t)tok[k] * a.ld_table;
-                for (uint32_t i = c; i < a.width; i++) to[i] = (TO)(named ? times(load1(from + i), a.scale) : 0.0f);
-            }
+        if (c + N <= a.width) {
+            float v[N] = {};
+            if (named) load<N>(from + c, v);
+            for (int i = 0; i < N; i++) v[i] = named ? times(v[i], a.scale) : 0.0f;
+            store_stream<N>(to + c, v);
+        } else {
+            for (uint32_t i = c; i < a.width; i++) to[i] = (TO)(named ? times((float)from[i], a.scale) : 0.0f);
         }
     }
 }
@@ -383,28 +367,37 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a, const u
     }
 }
 
-// The runs that leave the chunk they began in: their parts, a quarter per wave, in
-// ascending order.  A workgroup looks after 256 columns of the run that leaves one
-// chunk (four chunks each: 5 us more at 131072 x 1024, 1 us more at 8192 x 128).
+// The runs that leave the chunk they began in: their parts, an equal share of them per wave,
+// in ascending order.  A workgroup looks after 256 columns of the run that leaves one
+// chunk (four chunks each: 5 us more at 131072 x 1024, 1 us more at 8192 x 128).  Most runs
+// have a part or two and cost the workgroup's start and the look ahead; a token that many positions
+// share is bound by its few workgroups' loads.
+constexpr uint32_t kJoinBatch = 8;  // parts whose loads are on their way at a time
 
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const uint2 *pairs) {
+template <uint32_t WAVES>
+__global__ __launch_bounds__(64 * WAVES) void embed_join_kernel(EmbedGradArgs a, const uint2 *pairs) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (a.n + a.run - 1) / a.run;
     const uint32_t c = (blockIdx.y * 64 + lane) * 4, live = c < a.width ? min(4u, a.width - c) : 0;
-    __shared__ float part[3][64][4];
-    const uint32_t chunk = blockIdx.x;
+    __shared__ float part[WAVES][64][4];
+    const uint32_t chunk = blockIdx.z * gridDim.x + blockIdx.x;
     const uint64_t i1 = (uint64_t)(chunk + 1) * a.run, i0 = i1 - a.run;
     if (i1 >= a.n) return;
     const uint32_t tok = pairs[i1 - 1].x;
     if (tok >= a.vocab || pairs[i1].x != tok) return;                      // it ends here
     if (i0 > 0 && pairs[i0].x == tok && pairs[i0 - 1].x == tok) return;  // it began earlier
-    // the chunks after this one that begin with the run
-    uint32_t more = 0;
-    for (;; more += 64) {
-        const uint32_t k = chunk + 1 + more + lane;
-        const unsigned long long m = __ballot(k < chunks && pairs[(uint64_t)k * a.run].x == tok);
-        if (m != ~0ull) {
-            more += (uint32_t)__builtin_ctzll(~m);
-            break;
+    // the chunks after this one that begin with the run: 64 looked at first, then 512 at a time
+    auto begins = [&](uint32_t k) { return k < chunks && pairs[(uint64_t)k * a.run].x == tok; };
+    const unsigned long long first = __ballot(begins(chunk + 1 + lane));
+    uint32_t more = first == ~0ull ? 64 : (uint32_t)__builtin_ctzll(~first);
+    for (bool on = first == ~0ull; on;) {
+        bool in[8];
+#pragma unroll
+        for (uint32_t q = 0; q < 8; q++) in[q] = begins(chunk + 1 + more + q * 64 + lane);
+#pragma unroll
+        for (uint32_t q = 0; q < 8; q++) {
+            const unsigned long long m = __ballot(in[q]);
+            if (on) more += m == ~0ull ? 64 : (uint32_t)__builtin_ctzll(~m);
+            on = on && m == ~0ull;
         }
     }
     float sum[4] = {};
@@ -414,12 +407,12 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const 
         for (uint32_t e = 0; e < 4; e++)
             if (e < live) sum[e] = from[e];
     }
-    const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / 4);
-    uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / 4);
-    for (; k < k1; k += 8) {
-        float v[8][4] = {};
+    const uint32_t k1 = chunk + 1 + (uint32_t)((uint64_t)more * (wave + 1) / WAVES);
+    uint32_t k = chunk + 1 + (uint32_t)((uint64_t)more * wave / WAVES);
+    for (; k < k1; k += kJoinBatch) {
+        float v[kJoinBatch][4] = {};
 #pragma unroll
-        for (uint32_t b = 0; b < 8; b++) {
+        for (uint32_t b = 0; b < kJoinBatch; b++) {
             const float *from = a.cut + (uint64_t)(k + b) * 2 * a.width + c;
             if (k + b < k1 && live == 4) load<4>(from, v[b]);
             if (k + b < k1 && live < 4)
@@ -428,26 +421,27 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a, const 
                     if (e < live) v[b][e] = from[e];
         }
 #pragma unroll
-        for (uint32_t b = 0; b < 8; b++)
+        for (uint32_t b = 0; b < kJoinBatch; b++)
             for (int e = 0; e < 4; e++) sum[e] += v[b][e];
     }
-    if (wave > 0)
-        for (int e = 0; e < 4; e++) part[wave - 1][lane][e] = sum[e];
+    for (int e = 0; e < 4; e++) part[wave][lane][e] = sum[e];
     __syncthreads();
     if (wave > 0) return;
+    for (uint32_t w = 1; w < WAVES; w++)
+        for (int e = 0; e < 4; e++) sum[e] += part[w][lane][e];
     float *to = a.grad + (uint64_t)tok * a.ld_grad + c;
 #pragma unroll
     for (uint32_t e = 0; e < 4; e++)
-        if (e < live) to[e] = fmaf(a.factor, (sum[e] + part[0][lane][e]) + (part[1][lane][e] + part[2][lane][e]), to[e]);
+        if (e < live) to[e] = fmaf(a.factor, sum[e], to[e]);
 }
 
 // ---------------------------------------------------------------- launchers
 
 namespace {
 
-// Threads per row: the power of two that covers `units`, at most 256.
-constexpr uint64_t kEmbedManyThreads = 1ull << 20;
+constexpr uint32_t kGridMost = 1u << 23;  // workgroups along one side of a grid: 2^32 threads are too many
 
+// Threads per row: the power of two that covers `units`, at most 256.
 uint32_t row_threads(uint32_t units) {
     uint32_t tx = 1;
     while (tx < units && tx < 256) tx *= 2;
@@ -458,10 +452,14 @@ template <typename TI, typename TO>
 void embed(const EmbedArgs &a, hipStream_t s) {
     constexpr int N = 16 / (sizeof(TI) > sizeof(TO) ? sizeof(TI) : sizeof(TO));
     const uint32_t tx = row_threads((a.width + N - 1) / N), rows = 256 / tx;
-    if ((uint64_t)a.n * tx >= kEmbedManyThreads)
-        embed_kernel<TI, TO, N, 4><<<(a.n + 4 * rows - 1) / (4 * rows), 256, 0, s>>>(a, tx);
-    else
-        embed_kernel<TI, TO, N, 1><<<(a.n + rows - 1) / rows, 256, 0, s>>>(a, tx);
+    const uint64_t most = (uint64_t)kGridMost * rows;  // positions of a launch
+    for (uint64_t i = 0; i < a.n; i += most) {
+        EmbedArgs b = a;
+        b.ids = (const char *)a.ids + i * (a.wide_ids ? 8 : 4);
+        b.out = (TO *)a.out + i * a.ld_out;
+        b.n = (uint32_t)std::min(a.n - i, most);
+        embed_kernel<TI, TO, N><<<(b.n + rows - 1) / rows, 256, 0, s>>>(b, tx);
+    }
 }
 template <typename TI>
 void embed(int out, const EmbedArgs &a, hipStream_t s) {
@@ -536,8 +534,12 @@ hipError_t launch_embed_sum(int dy, const EmbedGradArgs &a, int sorted, hipStrea
 }
 
 hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s) {
-    const dim3 grid(run_chunks(a), (a.width + 255) / 256);
-    embed_join_kernel<<<grid, 256, 0, s>>>(a, a.pairs[sorted]);
+    const uint32_t chunks = run_chunks(a), x = std::min(chunks, kGridMost);
+    const dim3 grid(x, (a.width + 255) / 256, (chunks + x - 1) / x);
+    // 8 or 4 waves, the whole gradient, us: with tokens at random 21.3, 21.2 (8192 x 128, 1024 workgroups), 42, 41 (16384 x 768,
+    // 3072), 183, 168 (131072 x 1024, 16384); with half of the positions one token 30, 36, 48, 52 and 222, 231
+    if ((uint64_t)chunks * grid.y <= 4096) embed_join_kernel<8><<<grid, 512, 0, s>>>(a, a.pairs[sorted]);
+    else embed_join_kernel<4><<<grid, 256, 0, s>>>(a, a.pairs[sorted]);
     return hipGetLastError();
 }
 

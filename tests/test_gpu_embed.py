@@ -207,3 +207,29 @@ def test_embed_graph_and_stream():
         s.synchronize()
         assert torch.equal(out, o) and torch.equal(acc, g)
         torch.cuda.synchronize()
+
+
+def test_lookup_of_more_rows_than_a_grid_takes():
+    """2^23 rows of 256 threads make 2^31 threads; the rows after them, and 16 GiB of output."""
+    n, vocab, width = (1 << 23) + 5, 300, 1021
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    table = torch.randn(vocab, width, generator=gen, device=DEV)
+    ids = torch.randint(-1, vocab, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    out = D.dedloc_embed(table, ids, 0.5, out_dtype=torch.bfloat16)
+    rows = torch.cat([0.5 * table, torch.zeros(1, width, device=DEV)]).to(torch.bfloat16)  # row -1: zeros
+    for i in range(0, n, 1 << 20):
+        assert torch.equal(out[i:i + (1 << 20)], rows[ids[i:i + (1 << 20)].long()])
+
+
+def test_gradient_of_more_chunks_than_a_grid_takes():
+    """2^24 + 31 chunks of 32 positions.  Sums of ones below 2^24 are exact in fp32, whatever their order."""
+    n, vocab = (1 << 29) + 1000, 1 << 20
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    ids = torch.randint(0, vocab, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    ids[:1 << 22] = 5
+    acc = torch.zeros(vocab, 1, device=DEV)
+    D.dedloc_embed_grad(acc, ids, torch.ones(n, 1, dtype=torch.float16, device=DEV), 2.0, 3.0)
+    want = torch.zeros(vocab, dtype=torch.int64, device=DEV)
+    for i in range(0, n, 1 << 26):
+        want += torch.bincount(ids[i:i + (1 << 26)], minlength=vocab)
+    assert int(want.max()) < 1 << 24 and torch.equal(acc[:, 0].double(), 6.0 * want.double())
