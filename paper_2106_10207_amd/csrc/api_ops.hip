@@ -214,6 +214,7 @@ void works_of(const Batch &b, const Program p[2], uint32_t k, NsWorks &t) {
             }
     }
     std::sort(t.w, t.w + t.n, [](const NsWork &x, const NsWork &y) { return panels_of(x) > panels_of(y); });
+    t.mixed = t.n > 1 && panels_of(t.w[0]) != panels_of(t.w[t.n - 1]);
 }
 
 // Sets every work's pieces and first item: the launch's items, the tiles that are cut and the items that these have.

@@ -72,6 +72,7 @@ template <int N>
 struct NsList {
     NsWork w[N];
     uint32_t n;
+    uint32_t mixed;  // products: whether their summed indexes differ in length
 };
 typedef NsList<kNsWorks> NsWorks;
 
