@@ -164,14 +164,14 @@ struct Cut {
 // more than `room` bytes.  W turns of 32 of the summed index, in `items` tiles of which
 // `full` are not symmetric (and written twice), the longest of `longest` turns: bound by
 // one workgroup alone on its CU, or by 256 CUs that hold two each; the join
-// reads its pieces back.  Fitted to 672 launches (the products of 14 calls of 1 to 54
+// reads its pieces back.  Fitted to 684 launches (the products of 14 calls of 1 to 54
 // matrices, sides of 1 to 8192) timed in tiles of 128 and 64, uncut and in pieces of at most 64,
 // 32, 16 and 8 panels: the choice by this estimate takes 1.02 of the best times' sum, always 128
-// uncut 1.37, always 64 uncut 1.33.
+// uncut 1.35, always 64 uncut 1.26.
 double cost_of(const NsWorks &t, Cut c, size_t room) {
     const bool big = c.edge == 128;
-    const double alone = big ? 0.78 : 0.17, once = big ? 6.8 : 5.4, busy = big ? 0.63 : 0.21, item = big ? 2.0 : 1.6,
-                 twice = big ? 4.3 : 2.0;
+    const double alone = big ? 0.54 : 0.17, once = big ? 9.1 : 5.0, busy = big ? 0.56 : 0.18, item = big ? 4.2 : 2.1,
+                 twice = big ? 6.2 : 1.9;
     double W = 0, items = 0, full = 0, cut = 0;
     uint32_t longest = 0;
     for (uint32_t k = 0; k < t.n; k++) {
@@ -184,8 +184,8 @@ double cost_of(const NsWorks &t, Cut c, size_t room) {
         longest = std::max(longest, blocks(P, z));
     }
     if (cut > (double)room) return -1.0;
-    const double filled = (W * busy + items * item + full * twice) / 256 + 0.7 * busy * longest + 5.5;
-    return std::max(longest * alone + once, filled) + (cut > 0 ? 3.9 + cut * 0.27e-6 : 0);
+    const double filled = (W * busy + items * item + full * twice) / 256 + 0.35 * busy * longest + 5.0;
+    return std::max(longest * alone + once, filled) + (cut > 0 ? 3.2 + cut * 0.29e-6 : 0);
 }
 
 Cut choose_cut(const NsWorks &t, size_t room) {
