@@ -95,6 +95,22 @@ __device__ inline float grad_at(const NsArgs &a, uint64_t e) {
     return (float)((const int8_t *)a.grad)[e] * a.scales[e >> 10];
 }
 
+// Four of them; e is a multiple of 4, so they share a block of the int8 codec.
+template <int SRC>
+__device__ inline void grads_at(const NsArgs &a, uint64_t e, float *g) {
+    if constexpr (SRC == kNsMuonF32) {
+        *(f32x4 *)g = *(const f32x4 *)((const float *)a.grad + e);
+    } else if constexpr (SRC == kNsMuonFP16) {
+        const f16x4 v = *(const f16x4 *)((const _Float16 *)a.grad + e);
+        for (int q = 0; q < 4; q++) g[q] = (float)v[q];
+    } else {
+        typedef int8_t i8x4 __attribute__((ext_vector_type(4)));
+        const i8x4 v = *(const i8x4 *)((const int8_t *)a.grad + e);
+        const float scale = a.scales[e >> 10];
+        for (int q = 0; q < 4; q++) g[q] = (float)v[q] * scale;
+    }
+}
+
 template <int SRC>
 __device__ inline float entry(const NsArgs &a, const NsMat &m, uint32_t row, uint32_t col) {
     if (SRC >= kNsMuonF32) {
@@ -120,6 +136,17 @@ __device__ inline double block_sum(double v) {
 
 }  // namespace
 
+// A thread's entries of the block of kNsTile rows and columns at (r0, c0): column threadIdx.x % 64,
+// rows threadIdx.x / 64 + 4 k.  All loads are on their way before the first is used.
+constexpr uint32_t kBlockEntries = kNsTile * kNsTile / 256;
+template <int SRC>
+__device__ inline void block_entries(const NsArgs &a, const NsMat &m, uint32_t r0, uint32_t c0, float *v) {
+    const uint32_t row = r0 + threadIdx.x / kNsTile, col = c0 + threadIdx.x % kNsTile;
+#pragma unroll
+    for (uint32_t k = 0; k < kBlockEntries; k++)
+        v[k] = row + 4 * k < m.rows && col < m.cols ? entry<SRC>(a, m, row + 4 * k, col) : 0.0f;
+}
+
 // Sums of squares in 64 bits, each of every kSumMost-th block of kNsTile rows and
 // columns: one block for most matrices.
 template <int SRC, int N>
@@ -129,12 +156,10 @@ __global__ __launch_bounds__(256) void ns_sum_kernel(NsMats<N> t, NsArgs a) {
     const uint32_t blocks = across * ((m.rows + kNsTile - 1) / kNsTile);
     double sum = 0.0;
     for (uint32_t b = k; b < blocks; b += kSumMost) {
-        const uint32_t r0 = b / across * kNsTile, col = b % across * kNsTile + threadIdx.x % kNsTile;
-        if (col < m.cols)
-            for (uint32_t r = r0 + threadIdx.x / kNsTile; r < r0 + kNsTile && r < m.rows; r += 256 / kNsTile) {
-                const double v = entry<SRC>(a, m, r, col);
-                sum = fma(v, v, sum);
-            }
+        float v[kBlockEntries];
+        block_entries<SRC>(a, m, b / across * kNsTile, b % across * kNsTile, v);
+#pragma unroll
+        for (uint32_t i = 0; i < kBlockEntries; i++) sum = fma((double)v[i], (double)v[i], sum);
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) a.part[m.part + k] = sum;
@@ -150,12 +175,29 @@ __global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
     double sum = 0.0;
     for (uint64_t i0 = (uint64_t)k * kSumChunk; i0 < n; i0 += (uint64_t)kSumMost * kSumChunk) {
         const uint64_t end = min(i0 + kSumChunk, n);
-        for (uint64_t i = i0 + threadIdx.x; i < end; i += 256) {
-            const uint64_t e = m.ld_in + i;
-            const float g = grad_at<SRC>(a, e), mom = fmaf(a.mu, a.mom[e], g);
-            a.mom[e] = mom;
-            const double u = a.nesterov ? fmaf(a.mu, mom, g) : mom;
-            sum = fma(u, u, sum);
+        for (uint64_t i = i0 + threadIdx.x * 4; i < end; i += 256 * 4) {
+            const uint64_t e = m.ld_in + i;  // a multiple of 4
+            alignas(16) float g[4], mom[4];
+            const bool whole = i + 4 <= end;
+            if (whole) {
+                grads_at<SRC>(a, e, g);
+                *(f32x4 *)mom = *(const f32x4 *)(a.mom + e);
+            } else {
+                for (uint32_t q = 0; q < 4; q++) {
+                    g[q] = i + q < end ? grad_at<SRC>(a, e + q) : 0.0f;
+                    mom[q] = i + q < end ? a.mom[e + q] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (uint32_t q = 0; q < 4; q++) {
+                mom[q] = fmaf(a.mu, mom[q], g[q]);
+                const double u = a.nesterov ? fmaf(a.mu, mom[q], g[q]) : mom[q];
+                sum = fma(u, u, sum);
+            }
+            if (whole) *(f32x4 *)(a.mom + e) = *(const f32x4 *)mom;
+            else
+                for (uint32_t q = 0; q < 4; q++)
+                    if (i + q < end) a.mom[e + q] = mom[q];
         }
     }
     sum = block_sum(sum);
@@ -169,34 +211,47 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) 
     const uint32_t q = find(t.m, t.n, blockIdx.x);
     const NsMat &m = t.m[q];
     const Sides d = sides(m.rows, m.cols);
+    const uint32_t k = blockIdx.x - m.begin;
+    const uint32_t across = (d.tall ? d.S : d.L) / 64, r0 = k / across * 64, c0 = k % across * 64;
+    float v[kBlockEntries];
+    block_entries<SRC>(a, m, r0, c0, v);
     double sum = 0.0;
     const uint32_t end = q + 1 < t.n ? t.m[q + 1].part : t.parts;
     for (uint32_t i = m.part + threadIdx.x; i < end; i += 256) sum += a.part[i];
     sum = block_sum(sum);
     const float scale = (float)((double)kXScale / (sqrt(sum) + (double)a.eps));
     __shared__ float tile[64][65];
-    const uint32_t k = blockIdx.x - m.begin;
-    const uint32_t across = (d.tall ? d.S : d.L) / 64, r0 = k / across * 64, c0 = k % across * 64;
-    const uint32_t tc = threadIdx.x % 64;
-    for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
-        float v = 0.0f;
-        if (r0 + r < m.rows && c0 + tc < m.cols) v = entry<SRC>(a, m, r0 + r, c0 + tc) * scale;
-        tile[r][tc] = v;
-    }
+#pragma unroll
+    for (uint32_t i = 0; i < kBlockEntries; i++) tile[threadIdx.x / 64 + 4 * i][threadIdx.x % 64] = v[i] * scale;
     __syncthreads();
-    // the block as stored goes to X (wide) or X^T (tall), its transpose to the other
+    // The block as stored goes to X (wide) or X^T (tall), its transpose to the other, 8 entries of a row
+    // at a time: 16 bytes of each plane, from 64 banks.
     char *straight = buffer(a, m.base, d, d.tall), *turned = buffer(a, m.base, d, !d.tall);
     const uint32_t h_straight = d.tall ? d.L : d.S, h_turned = d.tall ? d.S : d.L;
-    for (uint32_t r = threadIdx.x / 64; r < 64; r += 4) {
-        _Float16 hi, lo;
-        split(tile[r][tc], hi, lo);
-        _Float16 *p = (_Float16 *)(straight + at_planes(r0 + r, c0 + tc, h_straight));
-        p[0] = hi;
-        p[32] = lo;
-        split(tile[tc][r], hi, lo);
-        p = (_Float16 *)(turned + at_planes(c0 + r, r0 + tc, h_turned));
-        p[0] = hi;
-        p[32] = lo;
+    const uint32_t e0 = threadIdx.x % 8 * 8;
+#pragma unroll
+    for (uint32_t r = threadIdx.x / 8; r < 64; r += 32) {
+        f16x8 hi, lo;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e++) {
+            _Float16 h, w;
+            split(tile[r][e0 + e], h, w);
+            hi[e] = h;
+            lo[e] = w;
+        }
+        char *p = straight + at_planes(r0 + r, c0 + e0, h_straight);
+        *(f16x8 *)p = hi;
+        *(f16x8 *)(p + 64) = lo;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; e++) {
+            _Float16 h, w;
+            split(tile[e0 + e][r], h, w);
+            hi[e] = h;
+            lo[e] = w;
+        }
+        p = turned + at_planes(c0 + r, r0 + e0, h_turned);
+        *(f16x8 *)p = hi;
+        *(f16x8 *)(p + 64) = lo;
     }
 }
 
