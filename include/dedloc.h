@@ -402,15 +402,18 @@ typedef struct {
  * The norm is summed in fp64.  Every factor of a product is held as a pair of
  * fp16 numbers (22 bits) and the products are summed in fp32, so that an fp32
  * result is as near to the formula as fp32 products make it; 16-bit results
- * are rounded once, at the end.  The arithmetic takes |X|, |A| and |B| up to 15,
- * 63 and 63: coefficients that leave that range give infinities or NaN.  A zero
+ * are rounded once, at the end.  The arithmetic takes entries of X up to 15 and of
+ * its symmetric factors (A, a I + B and products of them over up to three steps)
+ * up to 255: coefficients that leave that range give infinities or NaN.  A zero
  * matrix gives zeros; one that holds an infinity or NaN gives NaN throughout.
  * Equal calls give equal bits; beside other matrices a matrix' sums may be
  * taken in other pieces, and so differ in their last bits.
  * ws: dedloc_orthogonalize_workspace_bytes (0 for invalid arguments; it looks
  * at the sides and their limits only), 256-byte aligned, contents arbitrary.
- * About 12 bytes an element and 8 a square of the shorter side; calls that
- * share one workspace must not overlap in time.
+ * With both sides rounded up to multiples of 64, 12 bytes an element and 8 (24 for
+ * long or large matrices) a square of the shorter side, half as much again or 4 MiB
+ * for cut sums, for the largest group of matrices that share their launches; calls
+ * that share one workspace must not overlap in time.
  * Errors: mats or cfg NULL, n == 0, an unknown dtype, steps out of range, a
  * side above its limit, ld < cols, a NULL pointer of a non-empty matrix ->
  * INVALID_ARG; a pointer not aligned to the element -> ALIGN; ws NULL or too

@@ -103,7 +103,8 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {
 // ------------------------------------------------------------------ the sort
 
 // One pass orders the positions by a digit of their token, BITS bits, keeping the
-// order of equal ones.  Chunk k counts its digits into counts[k][2^BITS].
+// order of equal ones.  Chunk k counts its digits into counts[k][2^BITS].  A pass over 131072 positions takes
+// 5.3 us to count and 8.2 to scatter, both near a launch that reads its chunk and the table of counts.
 template <bool FIRST>
 __device__ inline uint2 pair_at(const EmbedGradArgs &a, const uint2 *from, uint32_t i) {
     if (FIRST) return make_uint2(token(a.ids, a.wide_ids, a.vocab, i), i);
@@ -220,7 +221,8 @@ __global__ __launch_bounds__(256) void embed_scatter_kernel(EmbedGradArgs a, con
 }
 
 // A chunk of 1024 positions sorted by one workgroup, every pass at once, the pairs in
-// LDS between the passes.
+// LDS between the passes: 6.6 us for 8192 positions in two passes of 8 bits, bound by the barriers between their steps.  (All 8192
+// in one workgroup took 18.5 us; counting the smaller tokens of each, n^2, 21.6.)
 __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2 *to) {
     __shared__ uint2 pairs[1024];
     __shared__ uint32_t at[16][256];
@@ -256,7 +258,8 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2
 // Up to kSortOne positions: the sorted chunks merged.  A pair goes to its place in
 // its chunk plus, for every other chunk, the number of pairs that come before it, which
 // a binary search finds: those of a smaller token, and in earlier chunks those of its own too.
-// Eight lanes share a pair's searches; all tokens lie in LDS.
+// Eight lanes share a pair's searches; all tokens lie in LDS.  5.5 us for 8192 positions, bound by the reads that
+// fill the LDS and the ten dependent steps of a search.
 __global__ __launch_bounds__(512) void embed_merge_kernel(EmbedGradArgs a, const uint2 *from, uint2 *to) {
     extern __shared__ __align__(16) uint32_t tok[];
     const uint32_t chunks = (a.n + 1023) / 1024;
@@ -298,7 +301,8 @@ __global__ __launch_bounds__(512) void embed_merge_kernel(EmbedGradArgs a, const
 // ------------------------------------------------------------------ the sums
 
 // A row of tx threads sums one chunk of a.run sorted positions, N columns per
-// thread, kBatch rows of dy (and the accumulator's rows that they end) on their way at a time.
+// thread, kBatch rows of dy (and the accumulator's rows that they end) on their way at a time.  Bound by memory:
+// 131072 x 1024 bf16 over 30000 tokens 106 us, 3.8 TB/s of dy and of the accumulator's rows read and written.
 constexpr uint32_t kBatch = 4;  // 131072 x 1024 bf16: 2 112 us, 4 107, 8 155
 
 template <typename T, int N>

@@ -148,7 +148,8 @@ __device__ inline void block_entries(const NsArgs &a, const NsMat &m, uint32_t r
 }
 
 // Sums of squares in 64 bits, each of every kSumMost-th block of kNsTile rows and
-// columns: one block for most matrices.
+// columns: one block for most matrices.  13.8M fp32 elements of 8 matrices 25 us, 2.2 TB/s;
+// blocks of 16 x 256 took as long.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void ns_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
@@ -166,7 +167,8 @@ __global__ __launch_bounds__(256) void ns_sum_kernel(NsMats<N> t, NsArgs a) {
 }
 
 // Muon: m' = fma(mu, m, g), and the sums of squares of the update, each of every
-// kSumMost-th chunk of kSumChunk elements.
+// kSumMost-th chunk of kSumChunk elements.  Bound by memory: 54.8M elements with an int8
+// gradient (9 bytes each) 75 us, 6.6 TB/s.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
     const NsMat &m = t.m[find(t.m, t.n, blockIdx.x)];
@@ -205,7 +207,8 @@ __global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
 }
 
 // X0 and its transpose in two planes, zeros in the padding: one workgroup per
-// block of 64 x 64 of the matrix as it is stored.
+// block of 64 x 64 of the matrix as it is stored.  Bound by memory: the same elements
+// (12 bytes each without Nesterov's momentum) 126 us, 5.2 TB/s.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) {
     const uint32_t q = find(t.m, t.n, blockIdx.x);
@@ -462,6 +465,11 @@ typedef Shape<64, 1, 1, 4, 2> Little;
 // lanes of a read, one row each, meet all 64 banks (with r % 8 two rows met in a bank
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
+//
+// Large products are bound by the card's power: those of 8 matrices up to 8192 x 2048 (17 launches, 4.78 ms)
+// run at 0.95 PFLOP/s, three fp16 products for one, the clock between 1.75 and 1.9 GHz (these instructions alone, on random operands, reach
+// 1.6 to 1.7 PFLOP/s, with the loop's loads and reads 1.40; a large library product of fp16 1.20).
+// Small ones are bound by the launch: 4.5 us, and 5.3 for tiles of 64 with 4 turns.
 template <int OUT, typename C, int N>
 __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(NsList<N> t, NsArgs a) {
     constexpr uint32_t T = C::edge, NW = C::waves, WI = C::wi, WJ = C::wj, NS = C::stages;
@@ -582,7 +590,8 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
 }
 
 // A block of 32 x 32 of a product whose summed index was cut: a workgroup adds up its pieces, a quarter of them
-// per wave, in an order that only their number decides.  One workgroup per block of each tile.
+// per wave, in an order that only their number decides.  One workgroup per block of each tile.  4.2 us for
+// 640 KB of pieces, which is the launch; 0.29 us more per MB.
 template <int OUT, typename C, int N>
 __global__ __launch_bounds__(256) void ns_join_kernel(NsList<N> t, NsArgs a) {
     constexpr uint32_t T = C::edge, WI = C::wi, WJ = C::wj, kBlocks = T * T / 1024;
