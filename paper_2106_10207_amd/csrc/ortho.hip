@@ -902,6 +902,19 @@ void join(int out, const NsList<N> &t, const NsArgs &a, uint32_t tiles, hipStrea
     }
 }
 
+template <int OUT, int N>
+hipError_t narrow(const NsList<N> &t, const NsArgs &a, const float *from, float *to, bool first, bool last, uint32_t groups,
+                  uint32_t widest, hipStream_t s) {
+    const uint32_t lds = widest * widest * 4 + 2 * kNarrowCols * widest * 4;
+    if (lds > 65536) {  // beyond the default of 64 KB; at every launch, since it belongs to the current device
+        const hipError_t e = hipFuncSetAttribute((const void *)ns_narrow_kernel<OUT, N>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    ns_narrow_kernel<OUT><<<groups, 512, lds, s>>>(t, a, from, to, narrow_part(widest), first, last);
+    return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_ns_sum(int src, const NsTable &t, const NsArgs &a, uint32_t groups, hipStream_t s) {
@@ -932,21 +945,13 @@ hipError_t launch_ns_join(int out, uint32_t edge, const NsWorks &t, const NsArgs
 
 hipError_t launch_ns_narrow(int out, const NsWorks &t, const NsArgs &a, const float *from, float *to, bool first, bool last,
                             uint32_t groups, uint32_t widest, hipStream_t s) {
-    const uint32_t lds = widest * widest * 4 + 2 * kNarrowCols * widest * 4;
     hipError_t e = hipSuccess;
     with_table(t, [&](const auto &q) {
-        auto go = [&](auto kernel) {
-            // beyond the default of 64 KB; at every launch, since it belongs to the current device
-            if (lds > 65536)
-                e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (e == hipSuccess) kernel<<<groups, 512, lds, s>>>(q, a, from, to, narrow_part(widest), first, last);
-        };
-        constexpr int N = sizeof(q.w) / sizeof(q.w[0]);
         switch (out) {
-            case kNsF32: go(ns_narrow_kernel<kNsF32, N>); break;
-            case kNsFP16: go(ns_narrow_kernel<kNsFP16, N>); break;
-            case kNsBF16: go(ns_narrow_kernel<kNsBF16, N>); break;
-            default: go(ns_narrow_kernel<kNsMuonF32, N>); break;
+            case kNsF32: e = narrow<kNsF32>(q, a, from, to, first, last, groups, widest, s); break;
+            case kNsFP16: e = narrow<kNsFP16>(q, a, from, to, first, last, groups, widest, s); break;
+            case kNsBF16: e = narrow<kNsBF16>(q, a, from, to, first, last, groups, widest, s); break;
+            default: e = narrow<kNsMuonF32>(q, a, from, to, first, last, groups, widest, s); break;
         }
     });
     return e != hipSuccess ? e : hipGetLastError();
