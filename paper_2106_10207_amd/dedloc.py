@@ -9,6 +9,7 @@ missing or unloadable library raises.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -686,6 +687,16 @@ def _rows(t, name: str):
     return t.data_ptr(), (sr if r > 1 else c or 1), r, c
 
 
+def _allocating_on(stream):
+    """Where tensors that a call on `stream` makes for itself are allocated:
+    from that stream's memory, so that neither an earlier tensor's work on the
+    current stream nor a later tensor there meets the call's."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(stream)
+
+
 class OrthogonalizeCall:
     """Pre-marshalled arguments of one dedloc_orthogonalize call: `mats` and
     `out` are lists of 2-D tensors of one dtype with contiguous rows at any
@@ -727,9 +738,11 @@ def dedloc_orthogonalize(mats: Sequence, out: Optional[Sequence] = None, cfg: Op
     """Orthogonalise a list of matrices (out None: into new tensors); returns
     the results."""
     import torch
-    if out is None:
-        out = [torch.empty(m.shape, dtype=m.dtype, device=m.device) for m in mats]
-    return OrthogonalizeCall(mats, out, cfg, ws)(stream)
+    with _allocating_on(stream):
+        if out is None:
+            out = [torch.empty(m.shape, dtype=m.dtype, device=m.device) for m in mats]
+        call = OrthogonalizeCall(mats, out, cfg, ws)
+    return call(stream)
 
 
 def make_muon_workspace(shapes, device="cuda"):
@@ -770,7 +783,8 @@ class MuonCall:
 def dedloc_muon_step(x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, grad_codec: int = DEDLOC_CODEC_F32,
                      grad_scales=None, block: int = DEDLOC_I8_BLOCK, ws=None, stream=None):
     """One Muon step over the matrices of a flat vector; returns the workspace."""
-    call = MuonCall(x, m, grad, offsets, shapes, flags, cfg, grad_codec, grad_scales, block, ws)
+    with _allocating_on(stream):
+        call = MuonCall(x, m, grad, offsets, shapes, flags, cfg, grad_codec, grad_scales, block, ws)
     call(stream)
     return call.ws
 
@@ -797,7 +811,8 @@ def dedloc_embed(table, ids, scale: float = 1.0, out=None, out_dtype=None, strea
     tp, tl, vocab, width = _rows(table, "table")
     if out is None:
         import torch
-        out = torch.empty(n, width, dtype=out_dtype or table.dtype, device=table.device)
+        with _allocating_on(stream):
+            out = torch.empty(n, width, dtype=out_dtype or table.dtype, device=table.device)
     op, ol, r, c = _rows(out, "out")
     if r != n or c != width:
         raise ValueError(f"out: expected {n} rows of {width}, got {tuple(out.shape)}")
@@ -826,7 +841,8 @@ def dedloc_embed_grad(grad, ids, dy, scale: float = 1.0, batch_samples: float = 
     if r != n or c != width:
         raise ValueError(f"dy: expected {n} rows of {width}, got {tuple(dy.shape)}")
     if ws is None:
-        ws = make_embed_workspace(n, vocab, width, grad.device)
+        with _allocating_on(stream):
+            ws = make_embed_workspace(n, vocab, width, grad.device)
     _check(load().dedloc_embed_grad(gp, vocab, width, gl, p, size, n, dp, _dtype(dy, "dy"), dl, scale, batch_samples,
                                     _dev(ws, name="ws"), _nbytes(ws), _stream(stream)))
     return grad
