@@ -240,8 +240,8 @@ Items cut_works(NsWorks &t, Cut c) {
 // Whether a batch takes the narrow path, a launch per step: every shorter side at
 // most 128, few enough turns per workgroup, no more workgroups than the GPU takes at once.  Sets up
 // the works, the workgroups and the widest matrix.  Narrow against the products' path, us:
-// 64 x 64 48 / 81, 64 x 1024 (one turn) 61 / 113, 64 x 4096 (four) 102 / 115, 64 x 8192 (eight) 153 / 120;
-// 128 x 128 81 / 93, 128 x 1024 (two) 117 / 110, eight of them 138 / 160, 32 205 / 262.
+// 64 x 64 47 / 79, 64 x 1024 (one turn) 60 / 113, 64 x 4096 (four) 92 / 114, 64 x 8192 (eight) 134 / 120;
+// 128 x 128 79 / 91, 128 x 1024 (two) 103 / 112, eight of them 116 / 123, 32 168 / 182, 128 x 2048 (four) 137 / 112.
 struct Narrow {
     NsWorks t;
     uint32_t groups, widest;
@@ -255,7 +255,7 @@ bool narrow(const Batch &b, Narrow &n) {
         const uint32_t S = padded(std::min(w.rows, w.cols)), L = padded(std::max(w.rows, w.cols));
         if (S > kNarrowShort) return false;
         const uint32_t tiles = L / kNarrowCols, most = S == 64 ? 16 : 8, subs = blocks(tiles, most);
-        if (subs > (S == 64 ? 4u : b.t.n >= 4 ? 2u : 1u)) return false;
+        if (subs > (S == 64 ? 4u : 2u)) return false;
         w.pieces = blocks(tiles, subs);
         w.op |= subs << 20;
         w.begin = n.groups;

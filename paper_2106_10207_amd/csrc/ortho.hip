@@ -648,6 +648,7 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsList<N> t, NsArgs a) {
 // of X.  It adds up the parts of A = X X^T that all workgroups of its matrix left
 // at the launch before, forms M in LDS, takes its columns through X <- M X, and leaves
 // its part of the next A.  Each workgroup forms M for itself: 128^3 multiply-adds, three times, 1.5 us.
+// Bound by the dependent stages of a launch: 6 us a launch at 64 x 64, 12 at 128 x 128, 15 at 128 x 1024.
 //
 // LDS, two-plane panels as in memory with the product's swizzle: A and then M
 // [s][s], the columns' X^T [64][s], and X [s][64] for the next A.
@@ -731,6 +732,24 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
         bi = b < 1 ? 0 : b < 3 ? 1 : b < 6 ? 2 : 3;
         bj = b - bi * (bi + 1) / 2;
     };
+    // 16-byte pieces of X^T's rows (for X0: of X's columns), of a turn's 64 columns, loaded a turn ahead
+    char *const mem = buffer(a, m.base, d, first ? 0 : 1);
+    const uint32_t rows = first ? S : kNarrowCols, panels = first ? kNarrowCols / 32 : nb, in_turn = panels * rows * 8;
+    auto piece_at = [&](uint32_t k, uint32_t l0) {  // of piece k: its place in memory
+        const uint32_t p = k / (rows * 8), r = k / 8 % rows;
+        return mem + (first ? ((uint64_t)(l0 / 32 + p) * S + r) : ((uint64_t)p * d.L + l0 + r)) * 128 + k % 8 * 16;
+    };
+    auto swizzled = [&](uint32_t k) { return k / 8 * 128 + ((k % 8) ^ (k / 8 % rows / 2 % 8)) * 16; };
+    constexpr uint32_t kPieces = kNarrowShort / 32 * kNarrowCols * 8 / 512;  // of a thread, at most
+    u32x4 ahead[kPieces] = {};
+    auto fetch = [&](uint32_t sub) {
+        const uint32_t l0 = (wg * subs + sub) * kNarrowCols;
+        if (sub >= subs || l0 >= d.L) return;
+#pragma unroll
+        for (uint32_t q = 0; q < kPieces; q++)
+            if (threadIdx.x + 512 * q < in_turn) ahead[q] = *(const u32x4 *)piece_at(threadIdx.x + 512 * q, l0);
+    };
+    fetch(0);
     if (!first) {
         f32x16 v[2] = {};
 #pragma unroll
@@ -785,16 +804,10 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
     for (uint32_t sub = 0; sub < subs; sub++) {
         const uint32_t l0 = (wg * subs + sub) * kNarrowCols;
         if (l0 >= d.L) break;
-        // 16-byte pieces of X^T's rows l0 on (for X0: of X's columns), to their swizzled places
-        char *const mem = buffer(a, m.base, d, first ? 0 : 1);
-        const uint32_t rows = first ? S : kNarrowCols, panels = first ? kNarrowCols / 32 : nb;
-        auto piece_at = [&](uint32_t k) {  // of piece k: its place in memory
-            const uint32_t p = k / (rows * 8), r = k / 8 % rows;
-            return mem + (first ? ((uint64_t)(l0 / 32 + p) * S + r) : ((uint64_t)p * d.L + l0 + r)) * 128 + k % 8 * 16;
-        };
-        auto swizzled = [&](uint32_t k) { return k / 8 * 128 + ((k % 8) ^ (k / 8 % rows / 2 % 8)) * 16; };
-        for (uint32_t k = threadIdx.x; k < panels * rows * 8; k += 512)
-            *(u32x4 *)((first ? xg : xt) + swizzled(k)) = *(const u32x4 *)piece_at(k);
+#pragma unroll
+        for (uint32_t q = 0; q < kPieces; q++)
+            if (threadIdx.x + 512 * q < in_turn) *(u32x4 *)((first ? xg : xt) + swizzled(threadIdx.x + 512 * q)) = ahead[q];
+        fetch(sub + 1);
         __syncthreads();
         if (!first) {
             // blocks (bi, bj) of X' [s][64]: 2 nb of them, one per wave
@@ -813,8 +826,7 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
                 put_block(xt, kNarrowCols, bi * 32, bj * 32, true, value);
             }
             __syncthreads();
-            for (uint32_t k = threadIdx.x; k < panels * rows * 8; k += 512)
-                *(u32x4 *)piece_at(k) = *(const u32x4 *)(xt + swizzled(k));
+            for (uint32_t k = threadIdx.x; k < in_turn; k += 512) *(u32x4 *)piece_at(k, l0) = *(const u32x4 *)(xt + swizzled(k));
         }
 #pragma unroll
         for (uint32_t q = 0; q < 2; q++) {
