@@ -92,9 +92,11 @@ constexpr uint32_t kNarrowMost = 512;  // workgroups
 // Whether a matrix is worked on in blocks of steps.  Five steps as blocks of three and two
 // are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15: worth it from
 // 9 s^2 (l - s) = 6e8 on.
-bool blocked(uint32_t rows, uint32_t cols) {
+// The s x s side keeps A's own roundings, which a Gram matrix of a long X averages out: an fp32 result is
+// worked on in blocks only up to 4 times as long as wide.
+bool blocked(uint32_t rows, uint32_t cols, bool fp32) {
     const uint64_t s = std::min(rows, cols), l = std::max(rows, cols);
-    return s * s * (l - s) >= kNsBlocked;
+    return s * s * (l - s) >= kNsBlocked && !(fp32 && l > 4 * s);
 }
 
 // Matrices are worked on in batches, one after the other on the same workspace:
@@ -105,21 +107,21 @@ struct Batch {
     bool blocked_[kNsWorks];
     uint32_t works;
     uint64_t regions;
-    bool muon;
-    explicit Batch(bool muon_) : muon(muon_) { clear(); }
+    bool muon, fp32;  // fp32: orthogonalize's results
+    Batch(bool muon_, bool fp32_) : muon(muon_), fp32(fp32_) { clear(); }
     void clear() {
         memset(&t, 0, sizeof t);
         works = 0;
         regions = 0;
     }
-    bool fits(uint32_t rows, uint32_t cols) const { return works + 1 + blocked(rows, cols) <= (uint32_t)kNsWorks; }
+    bool fits(uint32_t rows, uint32_t cols) const { return works + 1 + blocked(rows, cols, fp32) <= (uint32_t)kNsWorks; }
     uint32_t sums(const NsMat &m) const {
         const uint32_t n = muon ? blocks((uint64_t)m.rows * m.cols, kSumChunk) : blocks(m.rows, kNsTile) * blocks(m.cols, kNsTile);
         return std::min(n, kSumMost);
     }
     void add(const void *in, uint64_t ld_in, void *out, uint64_t ld_out, uint32_t rows, uint32_t cols, uint32_t flags, float unit) {
         const uint64_t s = padded(std::min(rows, cols)), l = padded(std::max(rows, cols));
-        const bool b = blocked(rows, cols);
+        const bool b = blocked(rows, cols, fp32);
         NsMat &m = t.m[t.n];
         m = {regions, in, ld_in, rows, cols, t.parts, 0};
         t.parts += sums(m);
@@ -307,8 +309,8 @@ int run_batch(Batch &b, const Program p[2], uint32_t steps, int src, int out, Ns
 // Calls run(batch) on the matrices of a call in batches.  next(k, batch) adds
 // matrix k; sides(k, rows, cols) gives its sides.
 template <typename S, typename N, typename R>
-int in_batches(bool muon, uint32_t n, S sides, N next, R run) {
-    Batch b(muon);
+int in_batches(bool muon, bool fp32, uint32_t n, S sides, N next, R run) {
+    Batch b(muon, fp32);
     for (uint32_t k = 0; k < n; k++) {
         uint32_t rows = 0, cols = 0;
         sides(k, rows, cols);
@@ -330,7 +332,7 @@ int check_ws(const void *ws, size_t have, size_t need) {
     return DEDLOC_OK;
 }
 
-// Workspace of matrices given by their sides: the largest batch's.
+// Workspace of matrices given by their sides: the largest batch's, for results of any type.
 template <typename S>
 size_t batches_bytes(bool muon, uint32_t n, S sides) {
     for (uint32_t k = 0; k < n; k++) {
@@ -339,16 +341,19 @@ size_t batches_bytes(bool muon, uint32_t n, S sides) {
         if (check_sides(k, rows, cols)) return 0;
     }
     size_t most = 256;
-    in_batches(muon, n, sides,
-               [&](uint32_t k, Batch &b) {
-                   uint32_t rows = 0, cols = 0;
-                   sides(k, rows, cols);
-                   b.add(nullptr, 0, nullptr, 0, rows, cols, 0, 0.0f);
-               },
-               [&](Batch &b) {
-                   most = std::max(most, b.bytes());
-                   return DEDLOC_OK;
-               });
+    for (bool fp32 : {false, true}) {
+        if (muon && fp32) break;
+        in_batches(muon, fp32, n, sides,
+                   [&](uint32_t k, Batch &b) {
+                       uint32_t rows = 0, cols = 0;
+                       sides(k, rows, cols);
+                       b.add(nullptr, 0, nullptr, 0, rows, cols, 0, 0.0f);
+                   },
+                   [&](Batch &b) {
+                       most = std::max(most, b.bytes());
+                       return DEDLOC_OK;
+                   });
+    }
     return most;
 }
 
@@ -454,7 +459,7 @@ int dedloc_orthogonalize(const dedloc_matrix *mats, uint32_t n, int32_t dtype, c
     a.c = cfg->c;
     a.eps = cfg->eps;
     return in_batches(
-        false, n,
+        false, dtype == DEDLOC_DTYPE_F32, n,
         [&](uint32_t k, uint32_t &rows, uint32_t &cols) {
             rows = mats[k].rows;
             cols = mats[k].cols;
@@ -529,7 +534,7 @@ int dedloc_muon_step(float *x, float *m, const void *grad, const float *grad_sca
     a.keep = (float)(1.0 - (double)cfg->lr * (double)cfg->weight_decay);
     a.nesterov = cfg->nesterov;
     return in_batches(
-        true, n_tensors,
+        true, false, n_tensors,
         [&](uint32_t k, uint32_t &r, uint32_t &c) {
             r = rows[k];
             c = cols[k];

@@ -44,6 +44,10 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
+// fp16 products for one: lo lo' too where the result keeps its 24 bits.
+template <int OUT>
+constexpr uint32_t kProducts = OUT == kNsF32 ? 4 : 3;
+
 constexpr float kXScale = 4096.0f;  // of X
 constexpr float kAScale = 256.0f;   // of the symmetric matrices
 
@@ -258,6 +262,12 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) 
     }
 }
 
+// An entry of a I + b A + c A^2, all times kAScale.  In 64 bits: where A is near 1 the terms are nine times
+// their sum.
+__device__ inline float polynomial(const NsArgs &a, float A, double A2, bool diagonal) {
+    return (float)fma((double)a.b, (double)A, fma((double)a.c, A2, diagonal ? (double)a.a * (double)kAScale : 0.0));
+}
+
 // Orders what one lane of a wave wrote to LDS before what another reads.
 __device__ inline void wave_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -334,10 +344,8 @@ __device__ inline void ns_finish(const NsWork &m, const Sides &d, const NsArgs &
         if (kind == kNsSquare) {
             hi = *(const f16x4 *)(old + jl * 2);
             lo = *(const f16x4 *)(old + jl * 2 + 64);
-            for (int e = 0; e < 4; e++) {
-                v[e] = fmaf(a.b, (float)hi[e] + (float)lo[e], a.c * v[e]);
-                if (i == j0 + jl + e) v[e] = fmaf(a.a, kAScale, v[e]);
-            }
+            for (int e = 0; e < 4; e++)
+                v[e] = polynomial(a, (float)hi[e] + (float)lo[e], v[e], i == j0 + jl + e);
         }
         for (int e = 0; e < 4; e++) {
             _Float16 h, w;
@@ -524,20 +532,20 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
     };
     auto multiply = [&](uint32_t h) {
 #pragma unroll
-        for (uint32_t p = 0; p < 3; p++)  // lo hi', hi lo', hi hi'
+        for (uint32_t p = 4 - kProducts<OUT>; p < 4; p++)  // lo lo', lo hi', hi lo', hi hi'
 #pragma unroll
             for (uint32_t i = 0; i < WI; i++)
 #pragma unroll
                 for (uint32_t j = 0; j < WJ; j++)
                     // the right factor's rows first: a lane then holds four consecutive columns of one row
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[h][j][p == 1], l[h][i][p == 0], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(r[h][j][p % 2 == 0], l[h][i][p < 2], acc[i][j], 0, 0, 0);
     };
 #pragma unroll
     for (uint32_t k = 0; k < NS; k++) fetch(stage(k), k);
     arrived<(NS - 1) * kLoads>();
     read(stage(0), 0);
     auto turn = [&](uint32_t k, uint32_t panel) {
-        constexpr uint32_t kRead = 2 * (WI + WJ), kEach = 3 * WI * WJ > kRead ? 3 * WI * WJ / kRead : 1;
+        constexpr uint32_t kRead = 2 * (WI + WJ), kMfma = kProducts<OUT> * WI * WJ, kEach = kMfma > kRead ? kMfma / kRead : 1;
         static_assert(kLoads <= kRead, "");
         read(stage(k), 1);
         multiply(0);
@@ -690,9 +698,10 @@ __device__ inline void get_entries(const char *lds, uint32_t rows, uint32_t i, u
 #pragma unroll
     for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
 }
-// acc += rows i0 on of `left` times rows j0 on of `right`, over `panels` panels.
+// Rows i0 on of `left` times rows j0 on of `right`, over `panels` panels: hi hi' is added to acc, the rest to small.
+template <uint32_t PRODUCTS>
 __device__ inline void multiply_blocks(const char *left, uint32_t left_rows, uint32_t i0, const char *right, uint32_t right_rows,
-                                       uint32_t j0, uint32_t panels, f32x16 &acc) {
+                                       uint32_t j0, uint32_t panels, f32x16 &acc, f32x16 &small) {
     const uint32_t lane = threadIdx.x & 63, i = i0 + lane % 32, j = j0 + lane % 32;
     for (uint32_t p = 0; p < panels; p += 2) {  // a multiple of two: every read of two panels before their products
         f16x8 lh[4], ll[4], rh[4], rl[4];
@@ -707,8 +716,9 @@ __device__ inline void multiply_blocks(const char *left, uint32_t left_rows, uin
         }
 #pragma unroll
         for (uint32_t h = 0; h < 4; h++) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], lh[h], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], ll[h], acc, 0, 0, 0);
+            if constexpr (PRODUCTS == 4) small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], ll[h], small, 0, 0, 0);
+            small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], lh[h], small, 0, 0, 0);
+            small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], ll[h], small, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], lh[h], acc, 0, 0, 0);
         }
     }
@@ -774,8 +784,8 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
             if (b >= lower) continue;
             uint32_t bi, bj;
             block_of(b, bi, bj);
-            f32x16 acc = {};
-            multiply_blocks(sq, S, bi * 32, sq, S, bj * 32, nb, acc);
+            f32x16 acc = {}, small = {};
+            multiply_blocks<kProducts<OUT>>(sq, S, bi * 32, sq, S, bj * 32, nb, acc, small);
 #pragma unroll
             for (uint32_t g = 0; g < 4; g++) {
                 const uint32_t i = bi * 32 + lane % 32, j = bj * 32 + 8 * g + 4 * (lane / 32);
@@ -783,8 +793,8 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
                 get_entries(sq, S, i, j, old);
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    const float x = fmaf(a.b, old[e], a.c * (acc[4 * g + e] * (1.0f / kAScale)));
-                    v[q][4 * g + e] = i == j + e ? fmaf(a.a, kAScale, x) : x;
+                    const double square = ((double)acc[4 * g + e] + (double)small[4 * g + e]) * (1.0 / kAScale);
+                    v[q][4 * g + e] = polynomial(a, old[e], square, i == j + e);
                 }
             }
         }
@@ -812,8 +822,9 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
         if (!first) {
             // blocks (bi, bj) of X' [s][64]: 2 nb of them, one per wave
             const uint32_t bi = wave / 2, bj = wave % 2;
-            f32x16 acc = {};
-            if (bi < nb) multiply_blocks(sq, S, bi * 32, xt, kNarrowCols, bj * 32, nb, acc);
+            f32x16 acc = {}, small = {};
+            if (bi < nb) multiply_blocks<kProducts<OUT>>(sq, S, bi * 32, xt, kNarrowCols, bj * 32, nb, acc, small);
+            acc += small;
             if (last) {
                 if (bi < nb) ns_result<OUT>(m, d, a, bi * 32 + lane % 32, l0 + bj * 32, acc);
                 __syncthreads();
@@ -834,7 +845,7 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
             if (b >= lower) continue;
             uint32_t bi, bj;
             block_of(b, bi, bj);
-            multiply_blocks(xg, S, bi * 32, xg, S, bj * 32, kNarrowCols / 32, gram[q]);
+            multiply_blocks<kProducts<OUT>>(xg, S, bi * 32, xg, S, bj * 32, kNarrowCols / 32, gram[q], gram[q]);
         }
         __syncthreads();
     }
