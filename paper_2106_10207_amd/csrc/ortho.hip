@@ -568,14 +568,31 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
             if (q < kLoads) __builtin_amdgcn_sched_group_barrier(kSchedLoad, 1, 0);
         }
     };
+    // A matrix instruction cuts its sum off instead of rounding it: of the sums of many positive terms, a bit less each
+    // time.  fp32 results take two turns' sums to a total that is rounded.
+    f32x16 total[WI][WJ] = {};
+    auto to_total = [&] {
+        if constexpr (kProducts<OUT> == 4)
+#pragma unroll
+            for (uint32_t b = 0; b < WI * WJ; b++) {
+                total[b / WJ][b % WJ] += acc[b / WJ][b % WJ];
+                acc[b / WJ][b % WJ] = f32x16{};
+            }
+    };
     uint32_t panel = 0;
     for (; panel + NS <= panels; panel += NS)  // whole rounds of the stages, without a way out: the compiler counts the loads
 #pragma unroll
-        for (uint32_t k = 0; k < NS; k++) turn(k, panel + k);
+        for (uint32_t k = 0; k < NS; k++) {
+            turn(k, panel + k);
+            if (k % 2 == 1) to_total();
+        }
 #pragma unroll
     for (uint32_t k = 0; k + 1 < NS; k++)
         if (panel + k < panels) turn(k, panel + k);
     arrived<0>();  // no load may arrive in LDS that another workgroup has by then
+    if constexpr (kProducts<OUT> == 4)
+#pragma unroll
+        for (uint32_t b = 0; b < WI * WJ; b++) acc[b / WJ][b % WJ] += total[b / WJ][b % WJ];
     if (m.pieces > 1) {  // the sums of the piece, joined by the next launch
         float *to = a.pieces + (uint64_t)wg * (T * T) + wave * (T * T / NW) + lane * 4;
 #pragma unroll
