@@ -44,9 +44,11 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
-// fp16 products for one: lo lo' too where the result keeps its 24 bits.
+// An fp32 result keeps what its type holds: sums that no truncation biases and, where they have few
+// terms (a shorter side up to kFourProducts), lo lo' too.
 template <int OUT>
-constexpr uint32_t kProducts = OUT == kNsF32 ? 4 : 3;
+constexpr bool kFine = OUT == kNsF32;
+constexpr uint32_t kFourProducts = 64;
 
 constexpr float kXScale = 4096.0f;  // of X
 constexpr float kAScale = 256.0f;   // of the symmetric matrices
@@ -530,9 +532,9 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
             for (uint32_t b = 0; b < WJ; b++) r[h][b][p] = one(T + wj + b * 32 + lane % 32, p);
         }
     };
-    auto multiply = [&](uint32_t h) {
+    auto multiply = [&](uint32_t h, auto products) {
 #pragma unroll
-        for (uint32_t p = 4 - kProducts<OUT>; p < 4; p++)  // lo lo', lo hi', hi lo', hi hi'
+        for (uint32_t p = 4 - products.value; p < 4; p++)  // lo lo', lo hi', hi lo', hi hi'
 #pragma unroll
             for (uint32_t i = 0; i < WI; i++)
 #pragma unroll
@@ -544,11 +546,11 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
     for (uint32_t k = 0; k < NS; k++) fetch(stage(k), k);
     arrived<(NS - 1) * kLoads>();
     read(stage(0), 0);
-    auto turn = [&](uint32_t k, uint32_t panel) {
-        constexpr uint32_t kRead = 2 * (WI + WJ), kMfma = kProducts<OUT> * WI * WJ, kEach = kMfma > kRead ? kMfma / kRead : 1;
+    auto turn = [&](uint32_t k, uint32_t panel, auto products) {
+        constexpr uint32_t kRead = 2 * (WI + WJ), kMfma = decltype(products)::value * WI * WJ, kEach = kMfma > kRead ? kMfma / kRead : 1;
         static_assert(kLoads <= kRead, "");
         read(stage(k), 1);
-        multiply(0);
+        multiply(0, products);
 #pragma unroll
         for (uint32_t q = 0; q < kRead; q++) {
             __builtin_amdgcn_sched_group_barrier(kSchedMfma, kEach, 0);
@@ -560,7 +562,7 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
         __builtin_amdgcn_sched_barrier(0);
         read(stage((k + 1) % NS), 0);
         fetch(stage(k), panel + NS);
-        multiply(1);
+        multiply(1, products);
 #pragma unroll
         for (uint32_t q = 0; q < kRead; q++) {
             __builtin_amdgcn_sched_group_barrier(kSchedMfma, kEach, 0);
@@ -569,28 +571,38 @@ __global__ __launch_bounds__(64 * C::waves, C::per_simd) void ns_product_kernel(
         }
     };
     // A matrix instruction cuts its sum off instead of rounding it: of the sums of many positive terms, a bit less each
-    // time.  fp32 results take two turns' sums to a total that is rounded.
+    // time (at 1433 of them 3e-6 of the result).  Fine results take two turns' sums to a total that is rounded.
     f32x16 total[WI][WJ] = {};
     auto to_total = [&] {
-        if constexpr (kProducts<OUT> == 4)
+        if constexpr (kFine<OUT>)
 #pragma unroll
             for (uint32_t b = 0; b < WI * WJ; b++) {
                 total[b / WJ][b % WJ] += acc[b / WJ][b % WJ];
                 acc[b / WJ][b % WJ] = f32x16{};
             }
     };
-    uint32_t panel = 0;
-    for (; panel + NS <= panels; panel += NS)  // whole rounds of the stages, without a way out: the compiler counts the loads
+    auto loop = [&](auto products) {
+        uint32_t panel = 0;
+        for (; panel + NS <= panels; panel += NS)  // whole rounds of the stages, without a way out: the compiler counts the loads
 #pragma unroll
-        for (uint32_t k = 0; k < NS; k++) {
-            turn(k, panel + k);
-            if (k % 2 == 1) to_total();
-        }
+            for (uint32_t k = 0; k < NS; k++) {
+                turn(k, panel + k, products);
+                if (k % 2 == 1) to_total();
+            }
 #pragma unroll
-    for (uint32_t k = 0; k + 1 < NS; k++)
-        if (panel + k < panels) turn(k, panel + k);
+        for (uint32_t k = 0; k + 1 < NS; k++)
+            if (panel + k < panels) turn(k, panel + k, products);
+    };
+    typedef std::integral_constant<uint32_t, 3> Three;
+    typedef std::integral_constant<uint32_t, 4> Four;
+    if constexpr (kFine<OUT>) {
+        if (d.s <= kFourProducts) loop(Four{});
+        else loop(Three{});
+    } else {
+        loop(Three{});
+    }
     arrived<0>();  // no load may arrive in LDS that another workgroup has by then
-    if constexpr (kProducts<OUT> == 4)
+    if constexpr (kFine<OUT>)
 #pragma unroll
         for (uint32_t b = 0; b < WI * WJ; b++) acc[b / WJ][b % WJ] += total[b / WJ][b % WJ];
     if (m.pieces > 1) {  // the sums of the piece, joined by the next launch
@@ -802,7 +814,7 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
             uint32_t bi, bj;
             block_of(b, bi, bj);
             f32x16 acc = {}, small = {};
-            multiply_blocks<kProducts<OUT>>(sq, S, bi * 32, sq, S, bj * 32, nb, acc, small);
+            multiply_blocks<kFine<OUT> ? 4 : 3>(sq, S, bi * 32, sq, S, bj * 32, nb, acc, small);
 #pragma unroll
             for (uint32_t g = 0; g < 4; g++) {
                 const uint32_t i = bi * 32 + lane % 32, j = bj * 32 + 8 * g + 4 * (lane / 32);
@@ -840,7 +852,7 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
             // blocks (bi, bj) of X' [s][64]: 2 nb of them, one per wave
             const uint32_t bi = wave / 2, bj = wave % 2;
             f32x16 acc = {}, small = {};
-            if (bi < nb) multiply_blocks<kProducts<OUT>>(sq, S, bi * 32, xt, kNarrowCols, bj * 32, nb, acc, small);
+            if (bi < nb) multiply_blocks<kFine<OUT> ? 4 : 3>(sq, S, bi * 32, xt, kNarrowCols, bj * 32, nb, acc, small);
             acc += small;
             if (last) {
                 if (bi < nb) ns_result<OUT>(m, d, a, bi * 32 + lane % 32, l0 + bj * 32, acc);
@@ -862,7 +874,7 @@ __global__ __launch_bounds__(512) void ns_narrow_kernel(NsList<N> t, NsArgs a, c
             if (b >= lower) continue;
             uint32_t bi, bj;
             block_of(b, bi, bj);
-            multiply_blocks<kProducts<OUT>>(xg, S, bi * 32, xg, S, bj * 32, kNarrowCols / 32, gram[q], gram[q]);
+            multiply_blocks<kFine<OUT> ? 4 : 3>(xg, S, bi * 32, xg, S, bj * 32, kNarrowCols / 32, gram[q], gram[q]);
         }
         __syncthreads();
     }
