@@ -242,8 +242,9 @@ Items cut_works(NsWorks &t, Cut c) {
 // Whether a batch takes the narrow path, a launch per step: every shorter side at
 // most 128, few enough turns per workgroup, no more workgroups than the GPU takes at once.  Sets up
 // the works, the workgroups and the widest matrix.  Narrow against the products' path, us:
-// 64 x 64 47 / 79, 64 x 1024 (one turn) 60 / 113, 64 x 4096 (four) 92 / 114, 64 x 8192 (eight) 134 / 120;
-// 128 x 128 79 / 91, 128 x 1024 (two) 103 / 112, eight of them 116 / 123, 32 168 / 182, 128 x 2048 (four) 137 / 112.
+// 64 x 64 47 / 79, 64 x 1024 (one turn) 60 / 113, 64 x 4096 (four) 93 / 114, 64 x 8192 (eight) 134 / 122; 128 x 128
+// 79 to 82 / 91, 128 x 1024 (two) 103 to 107 / 112, eight of them 116 to 122 / 123, 32 168 to 176 / 182, 128 x 2048 (four) 137 / 115
+// (the larger of two: fp32, with a fourth product).
 struct Narrow {
     NsWorks t;
     uint32_t groups, widest;

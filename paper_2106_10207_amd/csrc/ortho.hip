@@ -15,9 +15,10 @@
 // gradient, 8 bits (bf16) 1e-1.  So every operand is held in two fp16 planes,
 // hi + lo, 22 bits, and a product takes three of them,
 //   hi hi' + hi lo' + lo hi'
-// in fp32 accumulators, which leaves errors of 5e-7 to 2e-6 of the result (fp32 products:
-// 1e-6 to 4e-6).  An error of A grows by a^2 in a step on the s x s side: three
-// steps from X0 and two from later X keep that; five lose it altogether.
+// in fp32 accumulators.  An error of A grows by a^2 in a step on the s x s side: three
+// steps from X0 and two from later X keep it small; five lose it altogether.  Fine (fp32) results
+// also round their sums every two turns, take lo lo' where sums are short, and leave long matrices out
+// of the blocks: errors of 3e-7 to 2e-6 of the result, about half of those of fp32 products.
 // X is stored times 2^12, the symmetric matrices times 2^8: |X| stays below 1.3 and
 // |Q| below a^3 = 41, and the low planes of entries of the usual size (1 / sqrt(s l))
 // stay in fp16's normal range.
@@ -727,7 +728,8 @@ __device__ inline void get_entries(const char *lds, uint32_t rows, uint32_t i, u
 #pragma unroll
     for (int e = 0; e < 4; e++) v[e] = (float)hi[e] + (float)lo[e];
 }
-// Rows i0 on of `left` times rows j0 on of `right`, over `panels` panels: hi hi' is added to acc, the rest to small.
+// Rows i0 on of `left` times rows j0 on of `right`, over `panels` panels: hi hi' is added to acc, the rest, before it,
+// to small (which may be acc).
 template <uint32_t PRODUCTS>
 __device__ inline void multiply_blocks(const char *left, uint32_t left_rows, uint32_t i0, const char *right, uint32_t right_rows,
                                        uint32_t j0, uint32_t panels, f32x16 &acc, f32x16 &small) {
@@ -748,8 +750,9 @@ __device__ inline void multiply_blocks(const char *left, uint32_t left_rows, uin
             if constexpr (PRODUCTS == 4) small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], ll[h], small, 0, 0, 0);
             small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rl[h], lh[h], small, 0, 0, 0);
             small = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], ll[h], small, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], lh[h], acc, 0, 0, 0);
         }
+#pragma unroll
+        for (uint32_t h = 0; h < 4; h++) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(rh[h], lh[h], acc, 0, 0, 0);
     }
 }
 

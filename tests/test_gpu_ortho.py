@@ -345,3 +345,23 @@ def test_muon_on_more_chunks_than_the_next_pass_adds_up():
     D.dedloc_muon_step(x, m, g.reshape(-1), [0, n], [shape], [0], cfg)
     assert torch.equal(m, g.reshape(-1))
     check(-x.view(shape), g)
+
+
+@pytest.mark.parametrize("shapes", [[(1433, 1), (2048, 1536)], [(192, 2368), (211, 2988)], [(64, 3584)], [(3, 5000), (1, 700)],
+                                    [(1024, 1024), (4096, 512)]])
+def test_fp32_results_as_near_as_fp32_products(shapes):
+    """Against the same formula in torch's fp32 products: at most twice their error, and 1e-6 for where both are small."""
+    g = [up(matrix(*s, seed=20 + k), torch.float32) for k, s in enumerate(shapes)]
+    a, b, c = ABC
+    for o, m in zip(D.dedloc_orthogonalize(g), g):
+        tall = m.shape[0] > m.shape[1]
+        x = (m.t() if tall else m).contiguous()
+        x = x / (x.norm() + 1e-7)
+        for _ in range(5):
+            A = x @ x.t()
+            x = a * x + (b * A + c * (A @ A)) @ x
+        plain = (x.t() if tall else x).double().cpu().numpy()
+        want, _ = exact(m.double().cpu().numpy())
+        err, of = (np.linalg.norm(v - want) / np.linalg.norm(want) for v in (o.double().cpu().numpy(), plain))
+        print(tuple(m.shape), f"error {err:.3g}, fp32 products {of:.3g}")
+        assert err <= 2 * of + 1e-6
