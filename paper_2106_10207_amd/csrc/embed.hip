@@ -541,7 +541,7 @@ hipError_t launch_embed_join(const EmbedGradArgs &a, int sorted, hipStream_t s) 
     const uint32_t chunks = run_chunks(a), x = std::min(chunks, kGridMost);
     const dim3 grid(x, (a.width + 255) / 256, (chunks + x - 1) / x);
     // 8 or 4 waves, the whole gradient, us: with tokens at random 21.3, 21.2 (8192 x 128, 1024 workgroups), 42, 41 (16384 x 768,
-    // 3072), 183, 168 (131072 x 1024, 16384); with half of the positions one token 30, 36, 48, 52 and 222, 231
+    // 3 x 1024), 183, 168 (131072 x 1024, 16384); with half of the positions one token 30, 36, 48, 52 and 222, 231
     if ((uint64_t)chunks * grid.y <= 4096) embed_join_kernel<8><<<grid, 512, 0, s>>>(a, a.pairs[sorted]);
     else embed_join_kernel<4><<<grid, 256, 0, s>>>(a, a.pairs[sorted]);
     return hipGetLastError();

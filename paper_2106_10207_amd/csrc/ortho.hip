@@ -477,8 +477,8 @@ typedef Shape<64, 1, 1, 4, 2> Little;
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
 //
-// Large products are bound by the card's power: those of 8 matrices up to 8192 x 2048 (17 launches, 4.78 ms)
-// run at 0.95 PFLOP/s, three fp16 products for one, the clock between 1.75 and 1.9 GHz (these instructions alone, on random operands, reach
+// Large products are bound by the card's power: those of 8 matrices up to 8192 x 2048 (17 launches, 4.74 ms)
+// run at 0.96 PFLOP/s, three fp16 products for one, the clock between 1.75 and 1.9 GHz (these instructions alone, on random operands, reach
 // 1.6 to 1.7 PFLOP/s, with the loop's loads and reads 1.40; a large library product of fp16 1.20).
 // Small ones are bound by the launch: 4.5 us, and 5.3 for tiles of 64 with 4 turns.
 template <int OUT, typename C, int N>
@@ -686,7 +686,7 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsList<N> t, NsArgs a) {
 // of X.  It adds up the parts of A = X X^T that all workgroups of its matrix left
 // at the launch before, forms M in LDS, takes its columns through X <- M X, and leaves
 // its part of the next A.  Each workgroup forms M for itself: 128^3 multiply-adds, three times, 1.5 us.
-// Bound by the dependent stages of a launch: 6 us a launch at 64 x 64, 12 at 128 x 128, 15 at 128 x 1024.
+// Bound by the dependent stages of a launch: 6 us a launch at 64 x 64, 12 at 128 x 128, 16 at 128 x 1024.
 //
 // LDS, two-plane panels as in memory with the product's swizzle: A and then M
 // [s][s], the columns' X^T [64][s], and X [s][64] for the next A.
