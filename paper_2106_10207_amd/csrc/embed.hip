@@ -230,7 +230,8 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(EmbedGradArgs a, uint2
     const uint32_t t = threadIdx.x, wave = t >> 6, i0 = blockIdx.x * 1024, n = min(1024u, a.n - i0);
     const uint32_t left = wave * 64 < n ? n - wave * 64 : 0;
     uint2 p = t < n ? pair_at<true>(a, nullptr, i0 + t) : make_uint2(0xffffffffu, 0u);
-    for (uint32_t shift = 0; shift == 0 || a.vocab >> shift; shift += 8) {
+    // as many digits as hold `vocab`; a shift of 32 would be one of 0 (a vocab from 2^24 on has all four)
+    for (uint32_t shift = 0; shift < 32 && (shift == 0 || a.vocab >> shift); shift += 8) {
         for (uint32_t k = t; k < 16 * 256; k += 1024) (&at[0][0])[k] = 0;
         __syncthreads();
         uint16_t rank;

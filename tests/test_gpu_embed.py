@@ -233,3 +233,24 @@ def test_gradient_of_more_chunks_than_a_grid_takes():
     for i in range(0, n, 1 << 26):
         want += torch.bincount(ids[i:i + (1 << 26)], minlength=vocab)
     assert int(want.max()) < 1 << 24 and torch.equal(acc[:, 0].double(), 6.0 * want.double())
+
+
+@pytest.mark.parametrize("vocab", [(1 << 24) - 1, 1 << 24, (1 << 24) + 5, 1 << 30])
+@pytest.mark.parametrize("n", [1, 100, 3000, 16384, 17000])
+def test_embed_grad_of_tokens_past_24_bits(n, vocab):
+    """Three or four digits of 8 bits in the short sorts, of 8 or 9 in the long one.  Sums of small integers are exact in
+    fp32, whatever their order."""
+    rng = np.random.default_rng(n)
+    ends = np.concatenate([np.arange(5), vocab - 1 - np.arange(5), [vocab // 2, (1 << 24) - 1, (1 << 16), 255, 256]])
+    ids = np.where(rng.random(n) < 0.5, rng.choice(ends, n), rng.integers(0, vocab, n))
+    ids = np.where(rng.random(n) < 0.1, rng.choice([-1, vocab, vocab + 3, -vocab], n), ids)
+    if n == 1:
+        ids[:] = vocab - 1
+    dy = rng.integers(-3, 4, (n, 1))
+    acc = torch.zeros(vocab, 1, device=DEV)
+    D.dedloc_embed_grad(acc, torch.from_numpy(ids).to(DEV), torch.from_numpy(dy).half().to(DEV), 2.0, 3.0)
+    ok = (ids >= 0) & (ids < vocab)
+    named, place = np.unique(ids[ok], return_inverse=True)
+    want = 6.0 * np.bincount(place, dy[ok, 0], len(named))
+    assert np.array_equal(acc[torch.from_numpy(named).to(DEV), 0].double().cpu().numpy(), want)
+    assert int(torch.count_nonzero(acc)) == np.count_nonzero(want)
