@@ -697,11 +697,39 @@ def _allocating_on(stream):
     return torch.cuda.stream(stream)
 
 
+class _Workspaces:
+    """The workspace of a call object on the stream that calls.  One that the
+    caller gave serves every call as it is.  Otherwise every stream has its
+    own from its own memory: another stream's would be written by work that
+    still waits there, and be given away there while this one still waits."""
+
+    def __init__(self, given, make):
+        self.given = given is not None
+        self.make = make
+        self.first = given if self.given else make()
+        self.args = _dev(self.first, name="ws"), _nbytes(self.first)
+        # by the stream's handle; kept with the tensor that holds the memory
+        self.of = {} if self.given else {_current_stream()(): (self.args, self.first)}
+
+    def on(self, stream, handle):
+        """(address, bytes) for a call on `stream`, whose handle this is."""
+        if self.given:
+            return self.args
+        got = self.of.get(handle)
+        if got is None:
+            with _allocating_on(stream):
+                ws = self.make()
+            got = self.of[handle] = (_dev(ws, name="ws"), _nbytes(ws)), ws
+        return got[0]
+
+
 class OrthogonalizeCall:
     """Pre-marshalled arguments of one dedloc_orthogonalize call: `mats` and
     `out` are lists of 2-D tensors of one dtype with contiguous rows at any
     stride (out None: in place).  Every call orthogonalises what `mats` then
-    hold."""
+    hold.  ws None: a workspace of its own for every stream that calls, the
+    current one's made at once; a workspace that is given is used on all of
+    them, so their calls must not overlap in time."""
 
     def __init__(self, mats: Sequence, out: Optional[Sequence] = None, cfg: Optional[dedloc_ortho_cfg] = None, ws=None):
         import torch
@@ -721,15 +749,16 @@ class OrthogonalizeCall:
         need = load().dedloc_orthogonalize_workspace_bytes(self.mats, len(mats))
         if need == 0:
             raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
-        self.ws = torch.empty(need, dtype=torch.uint8, device=mats[0].device) if ws is None else ws
-        self._ws = _dev(self.ws, name="ws")
-        self._ws_bytes = _nbytes(self.ws)
+        device = mats[0].device
+        self._ws = _Workspaces(ws, lambda: torch.empty(need, dtype=torch.uint8, device=device))
+        self.ws = self._ws.first
         self._keep = (list(mats), list(out))
         self._cfg = ctypes.byref(self.cfg)
 
     def __call__(self, stream=None):
-        _check(load().dedloc_orthogonalize(self.mats, len(self.mats), self.dtype, self._cfg, self._ws, self._ws_bytes,
-                                           _stream(stream)))
+        handle = _stream(stream)
+        _check(load().dedloc_orthogonalize(self.mats, len(self.mats), self.dtype, self._cfg, *self._ws.on(stream, handle),
+                                           handle))
         return self._keep[1]
 
 
@@ -757,7 +786,8 @@ def make_muon_workspace(shapes, device="cuda"):
 
 class MuonCall:
     """Pre-marshalled arguments of one dedloc_muon_step call.  shapes: (rows,
-    cols) per tensor, (0, 0) for one that is not a matrix and is left alone."""
+    cols) per tensor, (0, 0) for one that is not a matrix and is left alone.
+    ws: as for OrthogonalizeCall."""
 
     def __init__(self, x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, grad_codec: int = DEDLOC_CODEC_F32,
                  grad_scales=None, block: int = DEDLOC_I8_BLOCK, ws=None):
@@ -768,16 +798,18 @@ class MuonCall:
         if not len(self.off) - 1 == len(self.rows) == len(self.fl):
             raise ValueError("offsets, shapes and flags describe different numbers of tensors")
         self.cfg = cfg
-        self.ws = make_muon_workspace(shapes, x.device) if ws is None else ws
+        device, shapes = x.device, list(shapes)
+        self._ws = _Workspaces(ws, lambda: make_muon_workspace(shapes, device))
+        self.ws = self._ws.first
         self._keep = (x, m, grad, grad_scales)
         self.args = (_dev(x, 4 * P, "x", f32=True), _dev(m, 4 * P, "m", f32=True),
                      _dev(grad, _code_bytes(grad_codec, P), "grad"),
                      _dev(grad_scales, _scale_bytes(grad_codec, P, block), "grad_scales"), grad_codec, block, P)
-        self._ws = (_dev(self.ws, name="ws"), _nbytes(self.ws))
 
     def __call__(self, stream=None):
+        handle = _stream(stream)
         _check(load().dedloc_muon_step(*self.args, _ptr(self.off), _ptr(self.rows), _ptr(self.cols), _ptr(self.fl),
-                                       len(self.fl), ctypes.byref(self.cfg), *self._ws, _stream(stream)))
+                                       len(self.fl), ctypes.byref(self.cfg), *self._ws.on(stream, handle), handle))
 
 
 def dedloc_muon_step(x, m, grad, offsets, shapes, flags, cfg: dedloc_muon_cfg, grad_codec: int = DEDLOC_CODEC_F32,

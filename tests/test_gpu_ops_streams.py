@@ -51,3 +51,77 @@ def test_waiting_call_keeps_its_memory(make):
     torch.cuda.current_stream().synchronize()  # the call still waits here
     side.synchronize()
     assert torch.equal(got, want) and all(int(o.max()) == 0 for o in others)
+
+
+def orthogonalize_object():
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    g = torch.randn(200, 300, generator=gen, device=DEV)
+    out = torch.empty_like(g)
+    return out, lambda: D.OrthogonalizeCall([g], [out])
+
+
+def muon_object():
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    x, m, g = torch.randn(3, 256 * 512, generator=gen, device=DEV)
+    return x, lambda: D.MuonCall(x, m, g, [0, 256 * 512], [(256, 512)], [3], D.muon_cfg())
+
+
+@pytest.mark.parametrize("make", [orthogonalize_object, muon_object])
+def test_call_object_on_a_stream_beside_the_one_that_made_it(make):
+    """Made on a stream whose waiting work still writes the memory that it gets there."""
+    want, new = make()
+    new()()
+    _, new = make()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    first = new()
+    size = first.ws.numel()
+    first(side)  # the side's memory is there: an allocation from the device would wait for all streams
+    torch.cuda.synchronize()
+    del first
+    got, new = make()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    written = torch.empty(size, dtype=torch.uint8, device=DEV)
+    for _ in range(20):
+        written.fill_(255)
+    del written
+    call = new()
+    call(side)  # where the two streams have a queue each, it runs while the other still sleeps
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("make", [orthogonalize_object, muon_object])
+def test_call_object_that_goes_while_its_call_waits(make):
+    want, new = make()
+    new()()
+    got, new = make()
+    side = torch.cuda.Stream()
+    call = new()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    call(side)
+    del call
+    others = [torch.zeros(1 << k, dtype=torch.uint8, device=DEV) for k in range(10, 25) for _ in range(3)]
+    torch.cuda.current_stream().synchronize()
+    side.synchronize()
+    assert torch.equal(got, want) and all(int(o.max()) == 0 for o in others)
+
+
+@pytest.mark.parametrize("make", [orthogonalize_object, muon_object])
+def test_call_objects_workspaces(make):
+    """One per stream, the same one on every call there; a given one on all of them."""
+    _, new = make()
+    call, side = new(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    seen = []
+    for s in (None, side, None, side):
+        call(s)
+        seen.append(call._ws.on(s, D._stream(s)))
+        torch.cuda.synchronize()
+    assert seen[0] == seen[2] and seen[1] == seen[3] and seen[0][0] != seen[1][0]
+    assert seen[0][0] == call.ws.data_ptr() and seen[0][1] == seen[1][1] == call.ws.numel()
+    given = D._Workspaces(call.ws, None)
+    assert given.on(side, D._stream(side)) == given.on(None, D._stream()) == seen[0]
