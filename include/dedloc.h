@@ -486,7 +486,8 @@ int dedloc_embed(const void *table, int32_t table_dtype, uint64_t vocab, uint32_
  * a token ascending, in groups), so equal calls give equal bits.
  *   grad  device fp32, ld_grad >= width apart; dy: n rows of dy_dtype;
  *   ws    dedloc_embed_workspace_bytes (0 for invalid sizes), 256-byte aligned,
- *         contents arbitrary; calls that share it must not overlap in time.
+ *         contents arbitrary; calls that share it must not overlap in time.  A
+ *         workspace for n and width holds every call of at most those.
  * Errors as for dedloc_embed; ws NULL or too small -> WORKSPACE, not 256-byte
  * aligned -> ALIGN. */
 size_t dedloc_embed_workspace_bytes(uint64_t n, uint64_t vocab, uint32_t width);

@@ -364,18 +364,29 @@ struct EmbedWs {
     size_t pairs, counts, total;
     uint32_t chunk, run;
 };
+// The chunks of a call get shorter below three products of positions and width, so that fewer positions may leave
+// more parts: the workspace has room for every smaller call on it, of fewer positions, narrower rows or both.
 EmbedWs embed_ws(uint64_t n, uint32_t width) {
     EmbedWs w;
     w.pairs = round_up((size_t)n * sizeof(uint2), 256);
     const uint32_t tiles = std::max(1u, blocks(n, kSortTile));
     w.chunk = (tiles + kSortChunks - 1) / kSortChunks * kSortTile;
+    w.counts = ((size_t)std::min(tiles, kSortChunks) << kSortBits) * sizeof(uint32_t);
     // Short chunks where there is little to sum, long ones where the parts of cut runs are many.  4, 8, 16, 32 positions, us: 1000 x
     // 512 14, 16, 21, 29; 8192 x 128 22.9, 22.2, 24.5, 30; 8192 x 768 28.7, 27.3, 30.3, 39; 40000 x 333 88, 81, 76, 95; 65536 x 1024
     // 147, 102, 84, 75.
+    struct {
+        uint32_t run;
+        uint64_t below;
+    } const rules[] = {{4, 1u << 20}, {8, 1u << 23}, {16, 1u << 25}, {32, ~0ull}};
     const uint64_t all = n * width;
-    w.run = all < 1u << 20 ? 4 : all < 1u << 23 ? 8 : all < 1u << 25 ? 16 : 32;
-    w.counts = ((size_t)blocks(n, w.chunk) << kSortBits) * sizeof(uint32_t);
-    w.total = 2 * w.pairs + w.counts + round_up((size_t)blocks(n, w.run) * 2 * width * sizeof(float), 256);
+    uint64_t most = 0;  // whole chunks times their width, of the calls that fit
+    for (const auto &r : rules) {
+        w.run = r.run;
+        most = std::max(most, std::min(all, r.below) / r.run);
+        if (all < r.below) break;
+    }
+    w.total = 2 * w.pairs + w.counts + round_up((size_t)(most + width) * 2 * sizeof(float), 256);  // and a part of a chunk
     w.total = std::max(w.total, (size_t)256);
     return w;
 }

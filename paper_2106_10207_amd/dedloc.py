@@ -854,7 +854,7 @@ def dedloc_embed(table, ids, scale: float = 1.0, out=None, out_dtype=None, strea
 
 
 def make_embed_workspace(n: int, vocab: int, width: int, device="cuda"):
-    """A workspace for dedloc_embed_grad of up to n ids."""
+    """A workspace for dedloc_embed_grad of up to n ids and rows of up to width."""
     import torch
     need = load().dedloc_embed_workspace_bytes(n, vocab, width)
     if need == 0:

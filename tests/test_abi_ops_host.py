@@ -136,3 +136,22 @@ def test_binding_refusals():
         D.dedloc_embed(g, torch.zeros(2))
     with pytest.raises(ValueError, match="at least one"):
         D.OrthogonalizeCall([], [])
+
+
+def test_embed_workspace_never_falls():
+    """A workspace holds every call of fewer ids or narrower rows: over the sizes where the sort's chunks, and the
+    chunks of the sums (products of 2^20, 2^23 and 2^25), change."""
+    need = D.load().dedloc_embed_workspace_bytes
+    steps = lambda at: range(max(0, at - 3), at + 4)  # noqa: E731
+    for width in (1, 2, 7, 128, 333, 1024, 1 << 20):
+        ends = [1, 4, 8, 1024, 2048, 4352, 16384, 1 << 20, 1 << 21, 1 << 29] + [(1 << k) // width for k in (20, 23, 25, 30)]
+        ns = sorted({n for e in ends for n in steps(e) if n <= 1 << 30})
+        sizes = [need(n, 1000, width) for n in ns]
+        assert all(sizes) and sizes == sorted(sizes), width
+    for n in (1, 5, 1000, 8191, 8192, 8193, 65537, 1 << 25):
+        ends = [1, 8, 1 << 20] + [(1 << k) // n for k in (20, 23, 25)]
+        widths = sorted({w for e in ends for w in steps(e) if w <= 1 << 20})
+        sizes = [need(n, 1000, w) for w in widths]
+        assert all(sizes) and sizes == sorted(sizes), n
+    # and it holds the parts: two per chunk of 4 positions at least where there are few
+    assert need(8191, 30000, 128) >= 2 * 8 * 8191 + 2048 * 2 * 128 * 4

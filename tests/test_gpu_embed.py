@@ -254,3 +254,23 @@ def test_embed_grad_of_tokens_past_24_bits(n, vocab):
     want = 6.0 * np.bincount(place, dy[ok, 0], len(named))
     assert np.array_equal(acc[torch.from_numpy(named).to(DEV), 0].double().cpu().numpy(), want)
     assert int(torch.count_nonzero(acc)) == np.count_nonzero(want)
+
+
+@pytest.mark.parametrize("n,width", [(8192, 128), (32768, 256), (32768, 1024)])
+def test_one_workspace_for_fewer_positions_and_narrower_rows(n, width):
+    """A last micro-batch that is shorter, on the workspace of the others, whose end nothing passes.  A token's values
+    are small integers, so that its sum is exact."""
+    vocab = 700
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    size = D.make_embed_workspace(n, vocab, width).numel()
+    buf = torch.full((size + 4096,), 171, dtype=torch.uint8, device=DEV)
+    ws = buf[:size]
+    for k, w in ((n, width), (n - 1, width), (n // 2, width), (4353, width), (n - 1, width - 1), (n // 2 + 1, width // 2), (3, 5)):
+        ids = torch.randint(-1, vocab, (k,), generator=gen, device=DEV)
+        ids[k // 3: k // 2] = 5  # runs over many chunks
+        dy = torch.randint(-8, 9, (k, w), generator=gen, device=DEV).to(torch.bfloat16)
+        acc = D.dedloc_embed_grad(torch.zeros(vocab, w, device=DEV), ids, dy, 2.0, 3.0, ws)
+        want = torch.zeros(vocab + 1, w, dtype=torch.float64, device=DEV)
+        want.index_add_(0, torch.where(ids < 0, vocab, ids), dy.double())
+        assert torch.equal(acc.double(), 6.0 * want[:vocab])
+        assert bool((buf[size:] == 171).all())
