@@ -405,7 +405,7 @@ typedef struct {
  * are rounded once, at the end.  The arithmetic takes entries of X up to 15 and of
  * its symmetric factors (A, a I + B and products of them over up to three steps)
  * up to 255: coefficients that leave that range give infinities or NaN.  A zero
- * matrix gives zeros; one that holds an infinity or NaN gives NaN throughout.
+ * matrix gives zeros, also with eps = 0; one that holds an infinity or NaN gives NaN throughout.
  * Equal calls give equal bits; beside other matrices a matrix' sums may be
  * taken in other pieces, and so differ in their last bits.
  * ws: dedloc_orthogonalize_workspace_bytes (0 for invalid arguments; it looks

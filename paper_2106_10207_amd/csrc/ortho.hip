@@ -229,10 +229,11 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) 
     const uint32_t end = q + 1 < t.n ? t.m[q + 1].part : t.parts;
     for (uint32_t i = m.part + threadIdx.x; i < end; i += 256) sum += a.part[i];
     sum = block_sum(sum);
-    const float scale = (float)((double)kXScale / (sqrt(sum) + (double)a.eps));
+    // in 64 bits: of fp32's smallest numbers, or its largest, the factor is not one of fp32's; and zeros stay zeros if eps is 0
+    const double scale = sum == 0.0 ? 0.0 : (double)kXScale / (sqrt(sum) + (double)a.eps);
     __shared__ float tile[64][65];
 #pragma unroll
-    for (uint32_t i = 0; i < kBlockEntries; i++) tile[threadIdx.x / 64 + 4 * i][threadIdx.x % 64] = v[i] * scale;
+    for (uint32_t i = 0; i < kBlockEntries; i++) tile[threadIdx.x / 64 + 4 * i][threadIdx.x % 64] = (float)((double)v[i] * scale);
     __syncthreads();
     // The block as stored goes to X (wide) or X^T (tall), its transpose to the other, 8 entries of a row
     // at a time: 16 bytes of each plane, from 64 banks.

@@ -365,3 +365,30 @@ def test_fp32_results_as_near_as_fp32_products(shapes):
         err, of = (np.linalg.norm(v - want) / np.linalg.norm(want) for v in (o.double().cpu().numpy(), plain))
         print(tuple(m.shape), f"error {err:.3g}, fp32 products {of:.3g}")
         assert err <= 2 * of + 1e-6
+
+
+@pytest.mark.parametrize("shape", [(64, 100), (300, 200), (600, 1500)])  # narrow, products, products of a 16-bit one in blocks
+@pytest.mark.parametrize("dtype,size", [(torch.float32, 1e-35), (torch.float32, 1e-38), (torch.float32, 1e-42), (torch.float32, 1e38),
+                                        (torch.bfloat16, 1e-38), (torch.bfloat16, 1e38), (torch.float16, 1e-6)])
+def test_ends_of_the_range_without_eps(shape, dtype, size):
+    """Entries up to `size`, around the type's smallest and largest numbers, some of them denormal, beside a matrix
+    of zeros."""
+    g = matrix(*shape, seed=7)
+    g = up(g / np.abs(g).max() * size, dtype)
+    z = torch.zeros(shape, dtype=dtype, device=DEV)
+    out = D.dedloc_orthogonalize([z, g], cfg=D.ortho_cfg(eps=0.0))
+    assert bool((out[0] == 0).all())
+    check(out[1], g, eps=0.0)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-7])
+def test_muon_without_a_gradient(eps):
+    """Nothing in the gradient and the momentum: the parameters decay and no more."""
+    shapes = [(64, 100), (300, 200)]
+    off = [0, 6400, 66400]
+    x0 = torch.randn(66400, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    for part in (slice(0, 1), slice(0, 2)):  # narrow alone, and beside a matrix that takes the products
+        x, zero = x0[:off[part.stop]].clone(), torch.zeros(off[part.stop], device=DEV)
+        cfg = D.muon_cfg(lr=0.25, weight_decay=0.5, ortho=D.ortho_cfg(eps=eps))
+        D.dedloc_muon_step(x, zero.clone(), zero, off[:part.stop + 1], shapes[part], [1] * part.stop, cfg)
+        assert torch.equal(x, x0[:off[part.stop]] * 0.875)
