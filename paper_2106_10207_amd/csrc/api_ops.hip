@@ -93,7 +93,8 @@ constexpr uint32_t kNarrowMost = 512;  // workgroups
 // are 6 s^2 l + 14 s^3 multiply-adds for 15 s^2 l + 5 s^3, in 17 launches for 15: worth it from
 // 9 s^2 (l - s) = 6e8 on.
 // The s x s side keeps A's own roundings, which a Gram matrix of a long X averages out: an fp32 result is
-// worked on in blocks only up to 4 times as long as wide.
+// worked on in blocks only up to 4 times as long as wide.  Muon's update of a longer one is left in blocks: 256 x 2304, the
+// worst of those timed, is 2.5e-6 off for 1.2e-6 at most (plain fp32 products 1.8e-6), against ResNet-50's matrices in 1013 us for 1200.
 bool blocked(uint32_t rows, uint32_t cols, bool fp32) {
     const uint64_t s = std::min(rows, cols), l = std::max(rows, cols);
     return s * s * (l - s) >= kNsBlocked && !(fp32 && l > 4 * s);

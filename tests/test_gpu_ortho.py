@@ -392,3 +392,40 @@ def test_muon_without_a_gradient(eps):
         cfg = D.muon_cfg(lr=0.25, weight_decay=0.5, ortho=D.ortho_cfg(eps=eps))
         D.dedloc_muon_step(x, zero.clone(), zero, off[:part.stop + 1], shapes[part], [1] * part.stop, cfg)
         assert torch.equal(x, x0[:off[part.stop]] * 0.875)
+
+
+@pytest.mark.parametrize("shapes", [[(256, 2304), (2304, 256)], [(1024, 1024), (4096, 512)], [(192, 300), (211, 988)], [(128, 1152)],
+                                    [(64, 3584)], [(3, 5000), (1, 700), (266, 3)],
+                                    [(512, 4608)] * 3 + [(256, 2304)] * 6 + [(2048, 512)] * 3 + [(1024, 256)] * 6 +
+                                    [(2048, 1024), (1000, 2048)]])  # as many as leave long sums uncut
+@pytest.mark.parametrize("kind", ["strong", "noise", "decaying"])
+def test_muon_update_as_near_as_fp32_products(shapes, kind):
+    """Against the same formula in torch's fp32 products, as for fp32 results: at most twice their error, and 1e-6 for
+    where both are small.  (Noise alone, or with directions that fall off into it, as a gradient has: what a sum loses is not hidden behind
+    X0's roundings.)  With x = 0, no decay and a rate of 1 the update is -x', from the momentum that it leaves."""
+    g = [matrix(*s, seed=40 + k, kind=kind) for k, s in enumerate(shapes)]
+    if kind == "decaying":
+        for v in g:
+            rng, r = np.random.default_rng(v.shape[0]), max(1, min(v.shape) // 16)
+            v += 1e-3 * (rng.standard_normal((v.shape[0], r)) * np.logspace(0, -2, r)) @ rng.standard_normal((r, v.shape[1]))
+    off = np.cumsum([0] + [-(-r * c // 8) * 8 for r, c in shapes])
+    flat = np.zeros(off[-1], np.float32)
+    for o, v in zip(off, g):
+        flat[o:o + v.size] = v.reshape(-1)
+    grad = torch.from_numpy(flat).to(DEV)
+    x, m = torch.zeros_like(grad), torch.zeros_like(grad)
+    D.dedloc_muon_step(x, m, grad, off, shapes, [0] * len(shapes), D.muon_cfg(lr=1.0, weight_decay=0.0, nesterov=False))
+    a, b, c = ABC
+    for o, (r, n) in zip(off, shapes):
+        u = m[o:o + r * n].view(r, n)
+        y = (u.t() if r > n else u).contiguous()
+        y = y / (y.norm() + 1e-7)
+        for _ in range(5):
+            A = y @ y.t()
+            y = a * y + (b * A + c * (A @ A)) @ y
+        plain = (y.t() if r > n else y).double().cpu().numpy()
+        want, _ = exact(u.double().cpu().numpy())
+        got = -x[o:o + r * n].view(r, n).double().cpu().numpy()
+        err, of = (np.linalg.norm(v - want) / np.linalg.norm(want) for v in (got, plain))
+        print((r, n), f"error {err:.3g}, fp32 products {of:.3g}")
+        assert err <= 2 * of + 1e-6
