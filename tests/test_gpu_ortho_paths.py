@@ -1,7 +1,7 @@
 """dedloc_orthogonalize and dedloc_muon_step on each way that a call works on
 its matrices, near enough to the definition in 64 bits that one lost product
-of two fp16 planes shows (test_ortho_tolerance.py has the tolerance's
-reason)."""
+of two fp16 planes shows (test_ortho_tolerance.py has the tolerance's reason),
+and calls of more matrices than one table holds."""
 
 import numpy as np
 import pytest
@@ -131,3 +131,43 @@ def test_muon_step_of_parameters(path, wire, first):
     shapes = N.LISTS[path]
     flags = [(3, 1, 2, 0)[(k + first) % 4] for k in range(len(shapes))]
     check_path(path, muon(shapes, wire, True, flags, 0.05, 0.3, 0.2, 0.02))
+
+
+def many(kind):
+    """More products than the 72 that a table holds."""
+    rng = np.random.default_rng(3)
+    side = lambda lo, hi: int(rng.integers(lo, hi))  # noqa: E731
+    if kind == "narrow":
+        return [(side(1, 129), side(1, 400)) for _ in range(160)]
+    if kind == "products":
+        return [(side(129, 200), side(129, 260)) for _ in range(80)]
+    # two products each of the matrices in blocks: the table is full in the middle of them
+    return [(side(1, 129), side(1, 300)) if k % 3 == 0 else (300, 1100 + k) if k % 2 else (1190 - k, 310) for k in range(60)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["narrow", "products", "blocks"])
+def test_orthogonalize_more_than_a_table_holds(kind, dtype):
+    """Batch after batch on the same workspace, whose contents are arbitrary; into other matrices with gaps, and in place."""
+    shapes = many(kind)
+    g = inputs(shapes, dtype, pad=5)
+    bufs = [torch.full((r, c + 2), 7.0, dtype=dtype, device=DEV) for r, c in shapes]
+    out = [b[:, :c] for b, (_, c) in zip(bufs, shapes)]
+    call = D.OrthogonalizeCall(g, out)
+    call.ws.fill_(255)
+    n = launches(call)
+    batches = {"narrow": 3, "products": 2, "blocks": 2}[kind]
+    assert n["ns_sum"] == n["ns_prepare"] == batches, n
+    for o, v, b in zip(out, g, bufs):
+        near(o, v)
+        assert bool((b[:, -2:] == 7.0).all())
+    D.OrthogonalizeCall(g)()
+    for o, v in zip(out, g):
+        assert torch.equal(o, v)
+
+
+@pytest.mark.parametrize("kind", ["narrow", "products", "blocks"])
+def test_muon_more_than_a_table_holds(kind):
+    shapes = many(kind)
+    n = muon(shapes, "fp16", True, [(3, 0, 1)[k % 3] for k in range(len(shapes))], 0.05, 0.3, 0.2, 0.02)
+    assert n["muon_sum"] == n["ns_prepare"] == {"narrow": 3, "products": 2, "blocks": 2}[kind], n
