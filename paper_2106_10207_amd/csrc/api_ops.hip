@@ -169,8 +169,9 @@ struct Cut {
 // one workgroup alone on its CU, or by 256 CUs that hold two each; the join
 // reads its pieces back.  Fitted to 684 launches (the products of 14 calls of 1 to 54
 // matrices, sides of 1 to 8192) timed in tiles of 128 and 64, uncut and in pieces of at most 64,
-// 32, 16 and 8 panels: the choice by this estimate takes 1.02 of the best times' sum, always 128
-// uncut 1.35, always 64 uncut 1.26.
+// 32, 16 and 8 panels.  In all of choose_cut's ways, the 294 launches of 21 calls (those, and sides to 100000): the choice
+// by this estimate takes 1.01 of the best times' sum, always 128 uncut 2.3, always 64 uncut 1.5.  145 launches of nine calls
+// with sides of 60000 to 15 million, which pieces of 256 and 128 are for: 1.06 (without these two 1.18).
 double cost_of(const NsWorks &t, Cut c, size_t room) {
     const bool big = c.edge == 128;
     const double alone = big ? 0.54 : 0.17, once = big ? 9.1 : 5.0, busy = big ? 0.56 : 0.18, item = big ? 4.2 : 2.1,
@@ -191,6 +192,7 @@ double cost_of(const NsWorks &t, Cut c, size_t room) {
     return std::max(longest * alone + once, filled) + (cut > 0 ? 3.2 + cut * 0.29e-6 : 0);
 }
 
+// The host takes 0.07 us a work for it: 1.6 us of a call of one matrix, 77 of one of 72, 5 a launch.
 Cut choose_cut(const NsWorks &t, size_t room) {
     Cut best = {};
     double cost = 0;
@@ -220,9 +222,9 @@ void works_of(const Batch &b, const Program p[2], uint32_t k, NsWorks &t) {
     t.mixed = t.n > 1 && panels_of(t.w[0]) != panels_of(t.w[t.n - 1]);
 }
 
-// Sets every work's pieces and first item: the launch's items, the tiles that are cut and the items that these have.
+// Sets every work's pieces and first item: the launch's items, and the tiles that are cut.
 struct Items {
-    uint32_t all, cut_tiles, cut_items;
+    uint32_t all, cut_tiles;
 };
 Items cut_works(NsWorks &t, Cut c) {
     Items n = {};
@@ -232,10 +234,7 @@ Items cut_works(NsWorks &t, Cut c) {
         w.pieces = pieces_of(panels_of(w), c.most);
         w.begin = n.all;
         n.all += tiles * w.pieces;
-        if (w.pieces > 1) {
-            n.cut_tiles += tiles;
-            n.cut_items = n.all;
-        }
+        if (w.pieces > 1) n.cut_tiles += tiles;
     }
     return n;
 }
