@@ -401,8 +401,8 @@ typedef struct {
  * take part in every launch, so that small ones fill the GPU together.
  * The norm is summed in fp64.  Every factor of a product is held as a pair of
  * fp16 numbers (22 bits) and the products are summed in fp32, so that an fp32
- * result is about as near to the formula as fp32 products make it; 16-bit results
- * are rounded once, at the end.  The arithmetic takes entries of X up to 15 and of
+ * result, or the Muon step's update, is about as near to the formula as fp32
+ * products make it; 16-bit results are rounded once, at the end.  The arithmetic takes entries of X up to 15 and of
  * its symmetric factors (A, a I + B and products of them over up to three steps)
  * up to 255: coefficients that leave that range give infinities or NaN.  A zero
  * matrix gives zeros, also with eps = 0; one that holds an infinity or NaN gives NaN throughout.

@@ -76,8 +76,8 @@ __device__ inline uint32_t token(const void *ids, int wide, uint32_t vocab, uint
 
 // A row of threads (tx of them, a power of two) per position, N elements per
 // thread and turn.  Bound by memory once there is enough to move: 131072 x 1024 bf16
-// 75 us, 7.1 TB/s read and written, 32768 x 1024 21 us, 6.4 TB/s (a plain copy of 2 GB: 5.0);
-// below 16 MB by the launch, 6 us.  Four positions per row of threads, all loaded before the
+// 75 us, 268 MB written and a table of 61 MB read, 4.4 TB/s (as many bytes as are written are loaded, most of them from
+// the caches; a plain copy of 2 GB: 5.0), 131072 x 2048 111 to 117 us, 5.2 to 5.5 TB/s, 32768 x 1024 21 us; below 16 MB by the launch, 6 us.  Four positions per row of threads, all loaded before the
 // first is stored, took the same times within 3 %.
 template <typename TI, typename TO, int N>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, uint32_t tx) {

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void muon_sum_kernel(NsMats<N> t, NsArgs a) {
 
 // X0 and its transpose in two planes, zeros in the padding: one workgroup per
 // block of 64 x 64 of the matrix as it is stored.  Bound by memory: the same elements
-// (12 bytes each without Nesterov's momentum) 126 us, 5.2 TB/s.
+// (12 bytes each without Nesterov's momentum) 127 us, 5.2 TB/s.
 template <int SRC, int N>
 __global__ __launch_bounds__(256) void ns_prepare_kernel(NsMats<N> t, NsArgs a) {
     const uint32_t q = find(t.m, t.n, blockIdx.x);
@@ -459,7 +459,7 @@ constexpr int kSchedMfma = 0x8, kSchedLoad = 0x10, kSchedRead = 0x100;  // class
 
 // A shape of tile: `edge` rows and columns, wi x wj blocks of 32 x 32 per wave, two
 // waves to a row of them.  Two workgroups of either kind fit a CU (64 KB of LDS
-// each): big tiles with one turn of loads in flight beside the one worked on, little ones, whose
+// each, the big ones 65: the two stages that they lack are 16 bytes, aligned to 1024): big tiles with one turn of loads in flight beside the one worked on, little ones, whose
 // turns are short, with three.
 template <uint32_t EDGE, uint32_t WI, uint32_t WJ, uint32_t STAGES, uint32_t PER_SIMD>
 struct Shape {
@@ -481,8 +481,8 @@ typedef Shape<64, 1, 1, 4, 2> Little;
 // and every read took 8 cycles instead of 4); the load writes lanes in order, so
 // the lane picks its source piece instead.
 //
-// Large products are bound by the card's power: those of 8 matrices up to 8192 x 2048 (17 launches, 4.74 ms)
-// run at 0.96 PFLOP/s, three fp16 products for one, the clock between 1.75 and 1.9 GHz (these instructions alone, on random operands, reach
+// Large products are bound by the card's power: those of 8 matrices up to 8192 x 2048 (17 launches, 4.81 ms)
+// run at 0.94 PFLOP/s, three fp16 products for one, the clock between 1.75 and 1.9 GHz (these instructions alone, on random operands, reach
 // 1.6 to 1.7 PFLOP/s, with the loop's loads and reads 1.40; a large library product of fp16 1.20).
 // Small ones are bound by the launch: 4.5 us, and 5.3 for tiles of 64 with 4 turns.
 template <int OUT, typename C, int N>
