@@ -697,11 +697,19 @@ def _allocating_on(stream):
     return torch.cuda.stream(stream)
 
 
+@functools.lru_cache(maxsize=None)
+def _capturing():
+    import torch
+    return torch.cuda.is_current_stream_capturing
+
+
 class _Workspaces:
     """The workspace of a call object on the stream that calls.  One that the
     caller gave serves every call as it is.  Otherwise every stream has its
     own from its own memory: another stream's would be written by work that
-    still waits there, and be given away there while this one still waits."""
+    still waits there, and be given away there while this one still waits.
+    A call that is captured gets one from its graph's memory, which lives as
+    long as the graph, whatever becomes of the call object."""
 
     def __init__(self, given, make):
         self.given = given is not None
@@ -715,11 +723,16 @@ class _Workspaces:
         """(address, bytes) for a call on `stream`, whose handle this is."""
         if self.given:
             return self.args
-        got = self.of.get(handle)
+        capturing = _capturing()()
+        got = None if capturing else self.of.get(handle)
         if got is None:
             with _allocating_on(stream):
                 ws = self.make()
-            got = self.of[handle] = (_dev(ws, name="ws"), _nbytes(ws)), ws
+            got = (_dev(ws, name="ws"), _nbytes(ws)), ws
+            if capturing:
+                self.captured = ws  # held while its launches are recorded
+            else:
+                self.of[handle] = got
         return got[0]
 
 

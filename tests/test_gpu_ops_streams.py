@@ -125,3 +125,30 @@ def test_call_objects_workspaces(make):
     assert seen[0][0] == call.ws.data_ptr() and seen[0][1] == seen[1][1] == call.ws.numel()
     given = D._Workspaces(call.ws, None)
     assert given.on(side, D._stream(side)) == given.on(None, D._stream()) == seen[0]
+
+
+@pytest.mark.parametrize("make", [orthogonalize_object, muon_object])
+def test_captured_calls_outlive_their_object(make):
+    """Two graphs of one call object, of which the second is replayed when the object and the first are gone and their
+    memory is in use again."""
+    want, new = make()
+    new()()
+    got, new = make()
+    start = got.clone()
+    call, graphs, at = new(), [], []
+    torch.cuda.synchronize()
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+        at.append(call._ws.captured.data_ptr())
+    assert len({call.ws.data_ptr(), *at}) == 3
+    graph = graphs.pop()
+    del call, graphs
+    torch.cuda.empty_cache()
+    others = [torch.zeros(1 << 22, dtype=torch.uint8, device=DEV) for _ in range(16)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and not torch.equal(got, start)
+    assert all(int(o.max()) == 0 for o in others)
