@@ -495,6 +495,172 @@ int dedloc_embed_grad(float *grad, uint64_t vocab, uint32_t width, uint64_t ld_g
                       int32_t id_bytes, uint64_t n, const void *dy, int32_t dy_dtype, uint64_t ld_dy,
                       float scale, float batch_samples, void *ws, size_t ws_bytes, void *stream);
 
+/* Dropout whose mask is drawn from a counter and never stored (host struct).
+ * The mask is a function of (seed, site, step, row, column) alone:
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) with the key (seed's low,
+ * high 32 bits) and the counter (column / 8, row0 + row, site, step + *step_at)
+ * gives four words, eight halves (a word's low half first), one for each of the
+ * eight columns.  With T = p * 65536 rounded to the nearest integer (at most
+ * 65535 unless p = 1) an element whose half is below T is dropped.
+ *   site     which dropout of the model; step: of the training; both free;
+ *   row0     of a call on some rows of a larger matrix: the first one's number;
+ *   step_at  device, nullable: one 64-bit integer whose low 32 bits are added
+ *            to step when the kernel runs, so that a captured call draws anew on
+ *            every replay (all sums modulo 2^32). */
+typedef struct {
+    float p;
+    uint32_t site, step, row0;
+    uint64_t seed;
+    const int64_t *step_at;
+} dedloc_dropout_cfg;
+
+/* out = dropped ? 0 : x * 65536 / (65536 - T), in fp32, rounded once.  What
+ * is dropped gives 0 also where x is infinite or NaN.  p = 0 copies, p = 1 gives
+ * zeros.  The gradient is the same call on the output's gradient.
+ *   x, out  device, rows of `width` elements of one dtype (a DEDLOC_DTYPE_*),
+ *           ld >= width elements apart; out may be x with ld_out = ld_x, else
+ *           they must not overlap.
+ * rows and width may be 0; rows at most 2^30, width at most 2^20.
+ * Errors: cfg NULL, p outside [0, 1] or NaN, a size above its limit, an unknown
+ * dtype, a NULL pointer to something that is not empty, a row stride less than
+ * the width -> INVALID_ARG; a pointer not aligned to its elements, step_at not
+ * 8-byte aligned -> ALIGN. */
+int dedloc_dropout(const dedloc_dropout_cfg *cfg, uint64_t rows, uint32_t width, int32_t dtype,
+                   const void *x, uint64_t ld_x, void *out, uint64_t ld_out, void *stream);
+
+/* Norms of rows (host struct):
+ *   N(x) = (x - mean) * rstd * gain + bias
+ *   layer: mean = mean(x), rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   rms:   mean = 0,       rstd = 1 / sqrt(mean(x^2) + eps)
+ *   gain, bias  device fp32[width], nullable (1 and 0).
+ * Statistics are sums in fp32 (in 64 bits where squares would leave it, entries
+ * above 1e18), results are rounded once. */
+enum { DEDLOC_NORM_NONE = 0, DEDLOC_NORM_LAYER = 1, DEDLOC_NORM_RMS = 2 };
+typedef struct {
+    int32_t kind;
+    float eps; /* in [1e-30, 1e30] */
+    const float *gain, *bias;
+} dedloc_norm_cfg;
+#define DEDLOC_NORM_MAX_WIDTH 16384
+
+/* out = N(x) row by row.
+ *   x, out  device, rows of `width` elements of x_dtype and out_dtype (fp32 x
+ *           goes with any, 16-bit x with out of its own type); out may be x
+ *           with the same type and stride, else they must not overlap;
+ *   stats   device, nullable, 8-byte aligned: fp32 (mean, rstd) of every row,
+ *           for the gradient.
+ * A row that holds an infinity or NaN spoils itself only.  rows and width may be
+ * 0; rows at most 2^30, width at most DEDLOC_NORM_MAX_WIDTH.
+ * Errors: cfg NULL or without a norm, an unknown kind, eps out of range or
+ * NaN, a size above its limit, unknown or unfit dtypes, a NULL pointer to
+ * something that is not empty, a row stride less than the width -> INVALID_ARG; a
+ * pointer not aligned to its elements (stats: 8 bytes) -> ALIGN. */
+int dedloc_norm(const dedloc_norm_cfg *cfg, uint64_t rows, uint32_t width, int32_t x_dtype,
+                int32_t out_dtype, const void *x, uint64_t ld_x, void *out, uint64_t ld_out,
+                float *stats, void *stream);
+
+/* The norm's gradient, with xhat = (x - mean) * rstd and g = gain * dout:
+ *   dx = rstd * (g - mean(g) - xhat * mean(g * xhat)) + add    (rms: without mean(g))
+ *   dgain = fma(batch_samples, sum over rows of dout * xhat, dgain)
+ *   dbias = fma(batch_samples, sum over rows of dout, dbias)
+ * The vectors' gradients are added into a peer's accumulator like a
+ * micro-batch's by dedloc_accumulate; the order of every sum is fixed by the
+ * sizes, so equal calls give equal bits.
+ *   dout          as dedloc_norm's out; x, stats: as that call had and left them;
+ *   add           nullable, x_dtype: a gradient that x has from elsewhere (the
+ *                 residual stream's);
+ *   dx            x_dtype; may be add or, where the types are the same, dout, with
+ *                 their stride;
+ *   dgain, dbias  device fp32[width], nullable; only for a vector that cfg has;
+ *   ws            dedloc_residual_workspace_bytes(rows, width, 0), 256-byte
+ *                 aligned, contents arbitrary; not read if dgain and dbias are
+ *                 NULL; calls that share it must not overlap in time.
+ * Errors as for dedloc_norm; ws NULL or too small -> WORKSPACE, not 256-byte
+ * aligned -> ALIGN. */
+int dedloc_norm_grad(const dedloc_norm_cfg *cfg, uint64_t rows, uint32_t width, int32_t x_dtype,
+                     int32_t out_dtype, const void *dout, uint64_t ld_dout, const void *x,
+                     uint64_t ld_x, const float *stats, const void *add, uint64_t ld_add, void *dx,
+                     uint64_t ld_dx, float *dgain, float *dbias, float batch_samples, void *ws,
+                     size_t ws_bytes, void *stream);
+
+/* The end of one block of a model and the start of the next, in one pass over
+ * the rows: the branch f joins the residual stream h (host struct).
+ *   v   = post(f)                              (f without a post norm)
+ *   w   = gate * v                             (v without a gate)
+ *   sum = alpha * h + beta * dropout(w),       rounded to the stream's type
+ *   out = pre(sum)                             (none without a pre norm)
+ * post is the norm behind the block, pre the one before the next block; a kind
+ * of DEDLOC_NORM_NONE leaves a norm out.  LayerNorm(h + dropout(f)) has
+ * no post norm and takes out as the next stream.
+ *   gate   device, nullable.  gate_rows = 0: fp32[width], learned, the same for
+ *          all rows.  gate_rows > 0: row i is scaled by row i / gate_rows of a
+ *          matrix of the branch's type, ceil(rows / gate_rows) rows of width,
+ *          ld_gate apart (what a layer made of each sequence);
+ *   drop   as for dedloc_dropout; p = 0: none. */
+typedef struct {
+    float alpha, beta;
+    dedloc_norm_cfg post, pre;
+    const void *gate;
+    uint64_t ld_gate;
+    uint32_t gate_rows;
+    dedloc_dropout_cfg drop;
+} dedloc_residual_cfg;
+
+/*   h, sum  device, rows of `width` elements of stream_dtype; f, out: of
+ *           branch_dtype.  An fp32 stream goes with any branch, a 16-bit one with
+ *           a branch of its own type.  sum may be h, out may be f, with the
+ *           same stride; otherwise nothing that is written may overlap anything.
+ *           sum may be NULL if there is a pre norm (nothing but out is then wanted).
+ *   stats   device, nullable, 8-byte aligned: fp32 (mean, rstd) of every row for
+ *           the pre norm, then (mean, rstd) of every row for the post norm: 4 *
+ *           rows values (2 * rows without a post norm; those of a norm that is
+ *           not there are not written).
+ * Limits and errors as for dedloc_norm and dedloc_dropout; gate_rows without a gate, out
+ * without a pre norm -> INVALID_ARG. */
+int dedloc_residual(const dedloc_residual_cfg *cfg, uint64_t rows, uint32_t width,
+                    int32_t stream_dtype, int32_t branch_dtype, const void *h, uint64_t ld_h,
+                    const void *f, uint64_t ld_f, void *sum, uint64_t ld_sum, void *out,
+                    uint64_t ld_out, float *stats, void *stream);
+
+/* What dedloc_residual_grad reads and writes (host struct).
+ *   sum, f, stats  as the forward call had and left them; sum may be NULL
+ *                  without a pre norm, f without a post norm if dgate is NULL,
+ *                  stats without norms;
+ *   dsum, dout     the gradients of sum (NULL: none, allowed with a pre norm) and
+ *                  out (NULL without a pre norm);
+ *   dh, df         the gradients of h and f; dh may be dsum, df may be f or
+ *                  dout, with their stride;
+ *   dgate          nullable; fp32[width], added into, for a gate of gate_rows = 0;
+ *                  fp32 rows of width, ld_dgate apart, one per group of rows,
+ *                  written, for gate_rows > 0;
+ *   dpre_gain, dpre_bias, dpost_gain, dpost_bias  fp32[width], nullable, added into. */
+typedef struct {
+    const void *sum, *f, *dsum, *dout;
+    void *dh, *df;
+    const float *stats;
+    uint64_t ld_sum, ld_f, ld_dsum, ld_dout, ld_dh, ld_df;
+    float *dgate;
+    uint64_t ld_dgate;
+    float *dpre_gain, *dpre_bias, *dpost_gain, *dpost_bias;
+} dedloc_residual_grads;
+
+/* The gradient of dedloc_residual, with the same cfg (the mask is drawn again):
+ *   d  = dsum + pre's gradient of dout;   dh = alpha * d
+ *   dw = beta * dropout(d);               df = post's gradient of gate * dw
+ *   learned parameters: grad = fma(batch_samples, sum over rows, grad)
+ *   a gate per group of rows: dgate = sum over the group's rows of dw * v
+ * Every sum's order is fixed by the sizes: equal calls give equal bits.
+ * ws: dedloc_residual_workspace_bytes(rows, width, gate_rows), as for
+ * dedloc_norm_grad; not read if no vector's gradient is wanted.  One for rows and
+ * width holds every call of at most those (one with gate_rows > 0 also those without).
+ * Errors as for dedloc_residual; a gradient of a parameter that cfg lacks ->
+ * INVALID_ARG; ws as for dedloc_norm_grad. */
+size_t dedloc_residual_workspace_bytes(uint64_t rows, uint32_t width, uint32_t gate_rows);
+int dedloc_residual_grad(const dedloc_residual_cfg *cfg, uint64_t rows, uint32_t width,
+                         int32_t stream_dtype, int32_t branch_dtype,
+                         const dedloc_residual_grads *grads, float batch_samples, void *ws,
+                         size_t ws_bytes, void *stream);
+
 /* Load balancer (Section 3.2, Appendix B): the relaxed linear program
  * (Eq. main_problem_appendix_relaxed) that maximises training steps per
  * second xi over the send rates a_ij (peer i -> reducer j), the return rates

@@ -19,7 +19,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdedloc.so")
-SOURCES = ["kernels.hip", "ortho.hip", "embed.hip", "api.hip", "api_ops.hip"]
+SOURCES = ["kernels.hip", "ortho.hip", "embed.hip", "block.hip", "api.hip", "api_ops.hip", "api_block.hip"]
 HOST_SOURCES = ["balance.cpp"]  # host-only C++ (no device code)
 ARCH = "gfx950"
 

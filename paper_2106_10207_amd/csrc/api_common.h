@@ -40,7 +40,8 @@ enum Kind {
     K_LARS_A_F32, K_LARS_A_FP16, K_LARS_A_I8, K_LARS_A_FUSED_FP16, K_LARS_B,
     K_ACCUMULATE, K_FINALIZE_FP16, K_FINALIZE_I8, K_FILL,
     K_NS_SUM, K_NS_PREPARE, K_NS_PRODUCT, K_NS_JOIN, K_NS_NARROW, K_MUON_SUM,
-    K_EMBED, K_EMBED_SORT, K_EMBED_MERGE, K_EMBED_COUNT, K_EMBED_SCATTER, K_EMBED_SUM, K_EMBED_JOIN, K_COUNT
+    K_EMBED, K_EMBED_SORT, K_EMBED_MERGE, K_EMBED_COUNT, K_EMBED_SCATTER, K_EMBED_SUM, K_EMBED_JOIN,
+    K_DROPOUT, K_RESIDUAL, K_RESIDUAL_GRAD, K_RESIDUAL_JOIN, K_GATE_JOIN, K_COUNT
 };
 inline const char *const kKindNames[K_COUNT] = {
     "encode_fp16", "decode_fp16", "encode_i8", "decode_i8", "reduce_fp16", "reduce_i8",
@@ -48,7 +49,8 @@ inline const char *const kKindNames[K_COUNT] = {
     "lars_a_f32", "lars_a_fp16", "lars_a_i8", "lars_a_fused_fp16", "lars_b",
     "accumulate", "finalize_fp16", "finalize_i8", "fill_zero",
     "ns_sum", "ns_prepare", "ns_product", "ns_join", "ns_narrow", "muon_sum",
-    "embed", "embed_sort", "embed_merge", "embed_count", "embed_scatter", "embed_sum", "embed_join"};
+    "embed", "embed_sort", "embed_merge", "embed_count", "embed_scatter", "embed_sum", "embed_join",
+    "dropout", "residual", "residual_grad", "residual_join", "gate_join"};
 
 struct Profiler {
     std::mutex mu;

@@ -102,6 +102,34 @@ def muon_cfg(lr=1e-3, momentum=0.95, weight_decay=0.01, rms=0.2, nesterov=True, 
     return dedloc_muon_cfg(lr, momentum, weight_decay, rms, int(nesterov), ortho if ortho is not None else ortho_cfg())
 
 
+DEDLOC_NORM_NONE = 0
+DEDLOC_NORM_LAYER = 1
+DEDLOC_NORM_RMS = 2
+DEDLOC_NORM_MAX_WIDTH = 16384
+
+
+class dedloc_dropout_cfg(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("step", ctypes.c_uint32), ("row0", ctypes.c_uint32),
+                ("seed", ctypes.c_uint64), ("step_at", ctypes.c_void_p)]
+
+
+class dedloc_norm_cfg(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class dedloc_residual_cfg(ctypes.Structure):
+    _fields_ = [("alpha", ctypes.c_float), ("beta", ctypes.c_float), ("post", dedloc_norm_cfg), ("pre", dedloc_norm_cfg),
+                ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_uint64), ("gate_rows", ctypes.c_uint32),
+                ("drop", dedloc_dropout_cfg)]
+
+
+class dedloc_residual_grads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("sum", "f", "dsum", "dout", "dh", "df", "stats")] + \
+               [(k, ctypes.c_uint64) for k in ("ld_sum", "ld_f", "ld_dsum", "ld_dout", "ld_dh", "ld_df")] + \
+               [("dgate", ctypes.c_void_p), ("ld_dgate", ctypes.c_uint64)] + \
+               [(k, ctypes.c_void_p) for k in ("dpre_gain", "dpre_bias", "dpost_gain", "dpost_bias")]
+
+
 class dedloc_local_peer(ctypes.Structure):
     _fields_ = [("index", ctypes.c_uint32), ("grad", ctypes.c_void_p)]
 
@@ -180,6 +208,22 @@ _SIGS = {
                            ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64,
                            ctypes.c_float, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
                           ctypes.c_int),
+    "dedloc_dropout": ([ctypes.POINTER(dedloc_dropout_cfg), ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32, ctypes.c_void_p,
+                        ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_norm": ([ctypes.POINTER(dedloc_norm_cfg), ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32, ctypes.c_int32,
+                     ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p],
+                    ctypes.c_int),
+    "dedloc_norm_grad": ([ctypes.POINTER(dedloc_norm_cfg), ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32, ctypes.c_int32,
+                          ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p,
+                          ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p,
+                          ctypes.c_void_p, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_residual": ([ctypes.POINTER(dedloc_residual_cfg), ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32, ctypes.c_int32,
+                         ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint64,
+                         ctypes.c_void_p, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
+    "dedloc_residual_workspace_bytes": ([ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint32], ctypes.c_size_t),
+    "dedloc_residual_grad": ([ctypes.POINTER(dedloc_residual_cfg), ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int32,
+                              ctypes.c_int32, ctypes.POINTER(dedloc_residual_grads), ctypes.c_float, ctypes.c_void_p,
+                              ctypes.c_size_t, ctypes.c_void_p], ctypes.c_int),
     "dedloc_balance": ([ctypes.POINTER(dedloc_balance_problem), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p], ctypes.c_int),
     "dedloc_group_size": ([ctypes.c_uint32, ctypes.c_double, ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p],
@@ -891,6 +935,252 @@ def dedloc_embed_grad(grad, ids, dy, scale: float = 1.0, batch_samples: float = 
     _check(load().dedloc_embed_grad(gp, vocab, width, gl, p, size, n, dp, _dtype(dy, "dy"), dl, scale, batch_samples,
                                     _dev(ws, name="ws"), _nbytes(ws), _stream(stream)))
     return grad
+
+
+def dropout_cfg(p: float, seed: int = 0, site: int = 0, step: int = 0, row0: int = 0, step_at=None) -> dedloc_dropout_cfg:
+    """Which mask a dropout draws; seed: 64 bits, the others 32.  step_at: an
+    int64 device tensor of one element, added to step when the kernel runs (a
+    captured call draws anew if the graph advances it)."""
+    cfg = dedloc_dropout_cfg(p, site, step, row0, seed, None)
+    if step_at is not None:
+        import torch
+        if step_at.dtype is not torch.int64 or step_at.numel() != 1:
+            raise ValueError(f"step_at: expected one int64, got {tuple(step_at.shape)} of {step_at.dtype}")
+        cfg.step_at = _dev(step_at, name="step_at")
+        cfg._keep = step_at
+    return cfg
+
+
+def _vector(t, name: str, width: Optional[int] = None):
+    """Device address of a contiguous fp32 vector (None passes as NULL)."""
+    if t is None:
+        return None
+    if width is not None and t.numel() != width:
+        raise ValueError(f"{name}: expected {width} elements, got {t.numel()}")
+    return _dev(t, name=name, f32=True)
+
+
+def norm_cfg(kind: int, gain=None, bias=None, eps: float = 1e-12) -> dedloc_norm_cfg:
+    """A norm of rows: DEDLOC_NORM_LAYER or DEDLOC_NORM_RMS, with fp32 vectors of
+    its width (None: ones, zeros)."""
+    cfg = dedloc_norm_cfg(kind, eps, _vector(gain, "gain"), _vector(bias, "bias"))
+    cfg._keep = gain, bias
+    return cfg
+
+
+def _check_norm(cfg, width: int, name: str):
+    for t, what in zip(cfg._keep, ("gain", "bias")):
+        _vector(t, f"{name}'s {what}", width)
+
+
+def _same(t, like, name: str, dtype=None):
+    """(address, row stride) of a matrix of the shape of `like` (None: NULL)."""
+    if t is None:
+        return None, 0
+    p, ld, r, c = _rows(t, name)
+    if t.shape != like.shape:
+        raise ValueError(f"{name}: expected {tuple(like.shape)}, got {tuple(t.shape)}")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    return p, ld
+
+
+def _stats(t, norms: int, rows: int):
+    if t is not None and t.numel() < 2 * norms * rows:
+        raise ValueError(f"stats: expected (mean, rstd) of {rows} rows for {norms} norm(s), got {t.numel()} values")
+    return _dev(t, name="stats", f32=True)
+
+
+def dedloc_dropout(x, cfg: dedloc_dropout_cfg, out=None, stream=None):
+    """The rows of x with the mask that cfg names; out may be x.  The gradient is
+    the same call on the output's gradient."""
+    p, ld, rows, width = _rows(x, "x")
+    if out is None:
+        import torch
+        with _allocating_on(stream):
+            out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
+    op, ol = _same(out, x, "out", x.dtype)
+    _check(load().dedloc_dropout(cfg, rows, width, _dtype(x, "x"), p, ld, op, ol, _stream(stream)))
+    return out
+
+
+def dedloc_norm(x, norm: dedloc_norm_cfg, out=None, out_dtype=None, stats=None, keep_stats: bool = True, stream=None):
+    """(norm of the rows of x, stats): stats [1, rows, 2] hold (mean, rstd) for
+    dedloc_norm_grad; keep_stats False: None, not written."""
+    p, ld, rows, width = _rows(x, "x")
+    _check_norm(norm, width, "norm")
+    if out is None or (stats is None and keep_stats):
+        import torch
+        with _allocating_on(stream):
+            if out is None:
+                out = torch.empty(rows, width, dtype=out_dtype or x.dtype, device=x.device)
+            if stats is None and keep_stats:
+                stats = torch.empty(1, rows, 2, device=x.device)
+    op, ol = _same(out, x, "out")
+    _check(load().dedloc_norm(norm, rows, width, _dtype(x, "x"), _dtype(out, "out"), p, ld, op, ol, _stats(stats, 1, rows),
+                              _stream(stream)))
+    return out, stats
+
+
+def make_residual_workspace(rows: int, width: int, gate_rows: int = 0, device="cuda"):
+    """A workspace for dedloc_norm_grad and dedloc_residual_grad of up to these
+    rows and this width."""
+    import torch
+    need = load().dedloc_residual_workspace_bytes(rows, width, gate_rows)
+    if need == 0:
+        raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def dedloc_norm_grad(dout, x, stats, norm: dedloc_norm_cfg, dgain=None, dbias=None, batch_samples: float = 1.0, add=None,
+                     dx=None, ws=None, stream=None):
+    """The gradient of dedloc_norm's x (plus `add`); dgain and dbias, fp32
+    accumulators, take batch_samples times theirs.  Returns dx."""
+    p, ld, rows, width = _rows(x, "x")
+    _check_norm(norm, width, "norm")
+    if dx is None or (ws is None and (dgain is not None or dbias is not None)):
+        import torch
+        with _allocating_on(stream):
+            if dx is None:
+                dx = torch.empty(rows, width, dtype=x.dtype, device=x.device)
+            if ws is None and (dgain is not None or dbias is not None):
+                ws = make_residual_workspace(rows, width, 0, x.device)
+    (yp, yl), (ap, al), (dp, dl) = _same(dout, x, "dout"), _same(add, x, "add", x.dtype), _same(dx, x, "dx", x.dtype)
+    if stats is None:
+        raise ValueError("stats: the forward call's are needed")
+    _check(load().dedloc_norm_grad(norm, rows, width, _dtype(x, "x"), _dtype(dout, "dout"), yp, yl, p, ld,
+                                   _stats(stats, 1, rows), ap, al, dp, dl, _vector(dgain, "dgain", width),
+                                   _vector(dbias, "dbias", width), batch_samples, _dev(ws, name="ws"),
+                                   0 if ws is None else _nbytes(ws), _stream(stream)))
+    return dx
+
+
+class _Block:
+    """What the residual calls share: cfg, checked against rows of `like` and a
+    branch of `branch`'s type, and what it points to."""
+
+    def __init__(self, like, branch, alpha, beta, post, pre, gate, gate_rows, drop):
+        rows, width = like.shape
+        none = dedloc_norm_cfg(DEDLOC_NORM_NONE, 0.0, None, None)
+        self.cfg = dedloc_residual_cfg(alpha, beta, post or none, pre or none, None, 0, gate_rows,
+                                       drop or dedloc_dropout_cfg(0.0, 0, 0, 0, 0, None))
+        self.norms = 2 if post is not None else 1 if pre is not None else 0
+        self.gate_shape = None
+        for n, name in ((post, "post"), (pre, "pre")):
+            if n is not None:
+                _check_norm(n, width, name)
+        if gate is not None and gate_rows:
+            self.gate_shape = (-(-rows // gate_rows), width)
+            p, ld, r, c = _rows(gate, "gate")
+            if (r, c) != self.gate_shape or gate.dtype is not branch.dtype:
+                raise ValueError(f"gate: expected {self.gate_shape} of {branch.dtype}, got {tuple(gate.shape)} of {gate.dtype}")
+            self.cfg.gate, self.cfg.ld_gate = p, ld
+        else:
+            self.cfg.gate = _vector(gate, "gate", width)
+        self.keep = post, pre, gate, drop
+
+
+class ResidualCall:
+    """Pre-marshalled arguments of one dedloc_residual call: the branch f joins
+    the residual stream h.  sum None (with a pre norm): not kept; out None: none
+    (without a pre norm); stats None: not kept, else fp32 of at least
+    [2, rows, 2] (the pre norm's, the post norm's).  post, pre: norm_cfg's; gate:
+    an fp32 vector, or with gate_rows a row of the branch's type per gate_rows
+    rows; drop: a dropout_cfg, whose step is changed between calls in cfg.drop."""
+
+    def __init__(self, h, f, sum=None, out=None, stats=None, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None,
+                 gate=None, gate_rows: int = 0, drop=None):
+        p, ld, rows, width = _rows(h, "h")
+        (fp, fl), (sp, sl) = _same(f, h, "f"), _same(sum, h, "sum", h.dtype)
+        op, ol = _same(out, h, "out", f.dtype)
+        self._block = _Block(h, f, alpha, beta, post, pre, gate, gate_rows, drop)
+        self.cfg = self._block.cfg
+        self._keep = h, f, stats
+        self.sum, self.out, self.stats = sum, out, stats
+        self.args = (ctypes.byref(self.cfg), rows, width, _dtype(h, "h"), _dtype(f, "f"), p, ld, fp, fl, sp, sl, op, ol,
+                     _stats(stats, self._block.norms, rows))
+
+    def __call__(self, stream=None):
+        """(sum, out, stats)"""
+        _check(load().dedloc_residual(*self.args, _stream(stream)))
+        return self.sum, self.out, self.stats
+
+
+def dedloc_residual(h, f, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None, gate=None, gate_rows: int = 0,
+                    drop=None, sum=None, out=None, stats=None, keep: bool = True, stream=None):
+    """(sum, out, stats) of the end of a block, new tensors where none are
+    given: sum = alpha * h + beta * dropout(gate * post(f)), out = pre(sum) (None
+    without a pre norm).  keep False: what only the gradient needs (stats, and with a pre
+    norm sum) is not made; it is None unless given."""
+    import torch
+    with _allocating_on(stream):
+        if sum is None and (keep or pre is None):
+            sum = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        if out is None and pre is not None:
+            out = torch.empty(f.shape, dtype=f.dtype, device=f.device)
+        if stats is None and keep and (pre is not None or post is not None):
+            stats = torch.empty(2, h.shape[0], 2, device=h.device)
+    return ResidualCall(h, f, sum, out, stats, alpha, beta, post, pre, gate, gate_rows, drop)(stream)
+
+
+class ResidualGradCall:
+    """Pre-marshalled arguments of one dedloc_residual_grad call, with what
+    dedloc_residual took and left.  dpre, dpost: pairs of fp32 accumulators (gain's,
+    bias'; None where not wanted); dgate: an accumulator of the learned gate, or
+    fp32 [groups, width] that is written.  ws: as for OrthogonalizeCall."""
+
+    def __init__(self, sum, f, stats, dsum, dout, dh, df, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None, gate=None,
+                 gate_rows: int = 0, drop=None, dgate=None, dpre=None, dpost=None, batch_samples: float = 1.0, ws=None):
+        _, _, rows, width = _rows(dh, "dh")
+        self._block = _Block(dh, df, alpha, beta, post, pre, gate, gate_rows, drop)
+        self.cfg = self._block.cfg
+        g = self.grads = dedloc_residual_grads()
+        for name, t, dtype in (("sum", sum, dh.dtype), ("f", f, df.dtype), ("dsum", dsum, dh.dtype), ("dout", dout, df.dtype),
+                               ("dh", dh, dh.dtype), ("df", df, df.dtype)):
+            p, ld = _same(t, dh, name, dtype)
+            setattr(g, name, p)
+            setattr(g, "ld_" + name, ld)
+        g.stats = _stats(stats, self._block.norms, rows)
+        if dgate is not None and self._block.gate_shape:
+            g.dgate, g.ld_dgate, r, c = _rows(dgate, "dgate")
+            if (r, c) != self._block.gate_shape or dgate.dtype is not _float32():
+                raise ValueError(f"dgate: expected {self._block.gate_shape} of float32, got {tuple(dgate.shape)} of {dgate.dtype}")
+        else:
+            g.dgate = _vector(dgate, "dgate", width)
+        for name, pair in (("dpre", dpre), ("dpost", dpost)):
+            for what, t in zip(("gain", "bias"), pair or (None, None)):
+                setattr(g, f"{name}_{what}", _vector(t, f"{name}'s {what}", width))
+        self._keep = sum, f, stats, dsum, dout, dgate, dpre, dpost
+        self.dh, self.df = dh, df
+        device = dh.device
+        self._ws = _Workspaces(ws, lambda: make_residual_workspace(rows, width, gate_rows, device))
+        self.ws = self._ws.first
+        self.args = ctypes.byref(self.cfg), rows, width, _dtype(dh, "dh"), _dtype(df, "df"), ctypes.byref(g), batch_samples
+
+    def __call__(self, stream=None):
+        """(dh, df)"""
+        handle = _stream(stream)
+        _check(load().dedloc_residual_grad(*self.args, *self._ws.on(stream, handle), handle))
+        return self.dh, self.df
+
+
+def dedloc_residual_grad(sum, f, stats, dsum, dout, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None, gate=None,
+                         gate_rows: int = 0, drop=None, dgate=None, dpre=None, dpost=None, batch_samples: float = 1.0, dh=None,
+                         df=None, ws=None, stream=None):
+    """(dh, df) of dedloc_residual, new tensors where none are given; the other
+    arguments as for ResidualGradCall.  f may be None where it is not read (no post
+    norm, no dgate); df then has the type of dout, or of the stream."""
+    import torch
+    stream_like = dsum if dsum is not None else sum
+    branch_like = next(t for t in (f, dout, stream_like) if t is not None)
+    with _allocating_on(stream):
+        if dh is None:
+            dh = torch.empty(stream_like.shape, dtype=stream_like.dtype, device=stream_like.device)
+        if df is None:
+            df = torch.empty(stream_like.shape, dtype=branch_like.dtype, device=stream_like.device)
+        call = ResidualGradCall(sum, f, stats, dsum, dout, dh, df, alpha, beta, post, pre, gate, gate_rows, drop, dgate, dpre,
+                                dpost, batch_samples, ws)
+    return call(stream)
 
 
 def dedloc_balance(s, d, u, B: float, P: float, t=None, can_aggregate=None, c_fixed=None):
