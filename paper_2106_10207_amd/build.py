@@ -19,7 +19,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdedloc.so")
-SOURCES = ["kernels.hip", "ortho.hip", "embed.hip", "block.hip", "api.hip", "api_ops.hip", "api_block.hip"]
+SOURCES = ["kernels.hip", "ortho.hip", "embed.hip", "block.hip", "block_f32.hip", "block_f32_fp16.hip",
+           "block_f32_bf16.hip", "block_fp16.hip", "block_bf16.hip", "api.hip", "api_ops.hip", "api_block.hip"]
 HOST_SOURCES = ["balance.cpp"]  # host-only C++ (no device code)
 ARCH = "gfx950"
 
@@ -44,14 +45,19 @@ def build(verbose: bool = False) -> str:
     cc = hipcc()
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
-    objs = []
+    objs, cmds = [], []
     for src in SOURCES:
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [cc, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        subprocess.check_call(cmd)
+        cmds.append([cc, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
+    if verbose:
+        print("\n".join(" ".join(c) for c in cmds), flush=True)
+    running = [subprocess.Popen(c) for c in cmds]  # side by side: the kernels' files take a minute each
+    for p in running:
+        p.wait()
+    for p, cmd in zip(running, cmds):
+        if p.returncode:
+            raise subprocess.CalledProcessError(p.returncode, cmd)
     for src in HOST_SOURCES:
         obj = os.path.join(objdir, src.replace(".cpp", ".o"))
         cmd = ["g++", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-Werror",

@@ -75,37 +75,39 @@ DropArgs drop_args(const dedloc_dropout_cfg &d) {
 }
 
 // Workgroups of a gradient and the rows of each of their teams.  Every workgroup leaves a part of each vector's
-// gradient, so few with many rows; but enough of them to fill the GPU: 16 waves a CU.
+// gradient that the join reads: no more of them than run at once, kTurns rows a team where there are enough for kFill waves, and
+// one where there are few (8192 rows of 1024 fp16: 4 rows a team 24.1 us, 8 22.6; 1001 rows of 333: 24.6 and 32.7).
 struct Split {
     uint32_t groups, turns;
 };
-Split split_rows(uint32_t rows, const RowShape &r) {
-    constexpr uint32_t kWaves = 4096, kTurns = 4;
-    const uint32_t most = kWaves * 64 / r.threads, teams = r.teams();
-    const uint32_t groups = std::min(most, (rows + teams * kTurns - 1) / (teams * kTurns));
-    const uint32_t turns = (rows + groups * teams - 1) / (groups * teams);
-    return {groups, turns};
+Split split_rows(uint32_t rows, const RowShape &r, int mode) {
+    constexpr uint32_t kTurns = 8, kFill = 2048;
+    const uint32_t most = kSimds * resident(kGradWaves, r.vectors, mode, r.threads) * 64 / r.threads, teams = r.teams();
+    const uint32_t fill = std::min((rows + teams - 1) / teams, kFill * 64 / r.threads);
+    const uint32_t groups = std::min(most, std::max(fill, (rows + teams * kTurns - 1) / (teams * kTurns)));
+    return {groups, (rows + groups * teams - 1) / (groups * teams)};
 }
 
-// Floats of the parts and edges of the largest of all calls of at most these rows and columns.
-size_t part_floats(uint32_t rows, uint32_t width, bool edges, size_t *edge_floats) {
-    size_t parts = 0, most_edges = 0;
-    for (uint32_t w = 64;; w *= 2) {
-        const uint32_t wide = std::min(w, width);
-        const RowShape r = row_shape(wide);
-        const Split s = split_rows(rows, r);
-        parts = std::max(parts, (size_t)s.groups * kBlockSums * wide);
-        most_edges = std::max(most_edges, (size_t)s.groups * r.teams() * 2 * wide);
-        if (wide == width) break;
-    }
-    if (edge_floats) *edge_floats = edges ? most_edges : 0;
-    return parts;
-}
-
-size_t workspace(uint32_t rows, uint32_t width, bool edges) {
-    size_t e = 0;
-    const size_t p = part_floats(rows, width, edges, &e);
-    return std::max((size_t)256, round_up(p * sizeof(float), 256) + round_up(e * sizeof(float), 256));
+// Floats of the parts, and of the edges, of the largest of all calls of at most these rows and columns.
+struct Room {
+    size_t parts, edges;
+    size_t bytes() const { return std::max((size_t)256, round_up(parts * sizeof(float), 256) + round_up(edges * sizeof(float), 256)); }
+};
+Room room(uint32_t rows, uint32_t width, bool edges) {
+    Room most = {0, 0};
+    const auto count = [&](uint32_t w) {
+        for (int k = 0; k < 8; k++) {
+            const int mode = k & 3;
+            const RowShape r = grad_shape(w, mode, k & 4);
+            const uint32_t groups = split_rows(rows, r, mode).groups;
+            most.parts = std::max(most.parts, (size_t)groups * kBlockSums * w);
+            if (edges) most.edges = std::max(most.edges, (size_t)groups * r.teams() * 2 * w);
+        }
+    };
+    // the widest row of each shape that is narrower
+    for (uint32_t w = 64; w < width; w += w < 512 ? w : 512) count(w);
+    count(width);
+    return most;
 }
 
 int check_ws(const void *ws, size_t bytes, size_t need) {
@@ -137,19 +139,19 @@ int check_grad(const float *grad, bool exists, const char *name) {
 
 int run_grad(ResidualGradArgs &a, int32_t stream_dtype, int32_t branch_dtype, void *ws, size_t ws_bytes, hipStream_t s) {
     const bool shared = a.gate && !a.gate_rows;
-    a.cut = a.gate_rows && a.dgate;
     a.want = (a.dpre_gain ? 1u : 0u) | (a.dpre_bias ? 2u : 0u) | (a.dpost_gain || (shared && a.dgate) ? 4u : 0u) |
              (a.dpost_bias || (shared && a.dgate && a.post.bias) ? 8u : 0u);
-    const RowShape r = row_shape(a.width);
-    const Split split = split_rows(a.rows, r);
+    a.f32 = stream_dtype == DEDLOC_DTYPE_F32;
+    const Split split = split_rows(a.rows, grad_shape(a.width, grad_mode(a), a.f32), grad_mode(a));
     a.groups = split.groups;
     a.turns = split.turns;
-    if (a.want || a.cut) {
-        const size_t need = workspace(a.rows, a.width, a.cut);
-        const int rc = check_ws(ws, ws_bytes, need);
+    const bool cut = a.gate_rows && a.dgate;
+    if (a.want || cut) {
+        const Room need = room(a.rows, a.width, cut);
+        const int rc = check_ws(ws, ws_bytes, need.bytes());
         if (rc) return rc;
         a.part = (float *)ws;
-        a.edge = (float *)((char *)ws + round_up(part_floats(a.rows, a.width, false, nullptr) * sizeof(float), 256));
+        a.edge = (float *)((char *)ws + round_up(need.parts * sizeof(float), 256));
     }
     hipError_t e = timed(K_RESIDUAL_GRAD, s, [&] { return launch_residual_grad(stream_dtype, branch_dtype, a, s); });
     if (e != hipSuccess) return hip_fail(e, "residual gradient launch");
@@ -157,7 +159,7 @@ int run_grad(ResidualGradArgs &a, int32_t stream_dtype, int32_t branch_dtype, vo
         e = timed(K_RESIDUAL_JOIN, s, [&] { return launch_residual_join(a, s); });
         if (e != hipSuccess) return hip_fail(e, "residual join launch");
     }
-    if (a.cut) {
+    if (cut) {
         e = timed(K_GATE_JOIN, s, [&] { return launch_gate_join(a, s); });
         if (e != hipSuccess) return hip_fail(e, "gate join launch");
     }
@@ -178,9 +180,7 @@ int dedloc_dropout(const dedloc_dropout_cfg *cfg, uint64_t rows, uint32_t width,
     rc = check_matrix(x, dtype, width, ld_x, true, "x");
     if (!rc) rc = check_matrix(out, dtype, width, ld_out, true, "out");
     if (rc) return rc;
-    const uint32_t vectors = (width + 7) / 8, per = std::max(1u, kDropVectors / vectors);
-    const DropoutArgs a = {x, out, ld_x, ld_out, (uint32_t)rows, width, per, (uint32_t)(((1ull << 32) + vectors - 1) / vectors),
-                           drop_args(*cfg)};
+    const DropoutArgs a = {x, out, ld_x, ld_out, (uint32_t)rows, width, drop_args(*cfg), 0, 0, 0};
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = timed(K_DROPOUT, s, [&] { return launch_dropout(dtype, a, s); });
     return e == hipSuccess ? DEDLOC_OK : hip_fail(e, "dropout launch");
@@ -236,7 +236,7 @@ int dedloc_residual(const dedloc_residual_cfg *cfg, uint64_t rows, uint32_t widt
 
 size_t dedloc_residual_workspace_bytes(uint64_t rows, uint32_t width, uint32_t gate_rows) {
     if (check_sizes(rows, width, kNormMaxWidth)) return 0;
-    return workspace((uint32_t)std::max<uint64_t>(rows, 1), std::max(width, 1u), gate_rows != 0);
+    return room((uint32_t)std::max<uint64_t>(rows, 1), std::max(width, 1u), gate_rows != 0).bytes();
 }
 
 int dedloc_norm_grad(const dedloc_norm_cfg *cfg, uint64_t rows, uint32_t width, int32_t x_dtype, int32_t out_dtype, const void *dout,

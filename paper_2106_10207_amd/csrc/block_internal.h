@@ -6,15 +6,23 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
+#include "ops_internal.h"
+
 namespace dedloc {
 
 constexpr uint32_t kBlockMaxRows = 1u << 30;
 constexpr uint32_t kDropMaxWidth = 1u << 20;
 constexpr uint32_t kNormMaxWidth = 16384;  // a row is held by one workgroup: 1024 threads of 16 columns
-constexpr uint32_t kBlockParts = 1024;     // workgroups of a gradient at most: each leaves a part of every vector's gradient
-constexpr uint32_t kBlockGrid = 1u << 20;  // workgroups of the other launches at most, of up to 1024 threads
-constexpr uint32_t kDropVectors = 2048;    // vectors of a workgroup of the dropout at a time
+constexpr uint32_t kBlockGrid = 1u << 20;  // workgroups of a launch at most
+constexpr uint32_t kDropThreads = 512;     // of a workgroup of the dropout at most
+constexpr uint32_t kDropBatch = 4;         // rows of a thread of it that are loaded at a time
+constexpr uint32_t kDropGroups = 4096;     // its workgroups at least before a thread takes more rows
+// Calls whose inputs take more read them past the caches: less is likely to be there still from the kernel that wrote it.
+constexpr uint64_t kStreamBytes = 96ull << 20;
 constexpr uint32_t kBlockSums = 4;         // vectors that the rows are summed into
+constexpr uint32_t kSimds = 1024;          // 256 CUs of 4
 
 struct DropArgs {
     uint32_t threshold;  // halves below it drop; 0: no dropout
@@ -36,9 +44,10 @@ struct DropoutArgs {
     void *out;
     uint64_t ld_x, ld_out;
     uint32_t rows, width;
-    uint32_t per;    // rows of a workgroup
-    uint32_t magic;  // ceil(2^32 / vectors of a row)
     DropArgs drop;
+    // set by the launch
+    uint32_t per;           // rows of a workgroup
+    uint32_t across, down;  // threads of a row, and rows at a time
 };
 
 // stats: (mean, 1 / deviation) of every row's pre norm, then of every row's post norm.
@@ -75,7 +84,7 @@ struct ResidualGradArgs {
     uint32_t want;
     uint32_t groups;  // workgroups
     uint32_t turns;   // rows of a team at most
-    int32_t cut;      // a gate per group of rows: a team takes rows that follow each other
+    int32_t f32;      // the stream's type is fp32
     float *part;      // [groups][wanted sums][width]
     float *edge;      // [2][teams][width]: sums of the group of rows at a team's start, and at its end, that its range cuts
 };
@@ -84,12 +93,73 @@ struct ResidualGradArgs {
 struct RowShape {
     uint32_t lanes;    // 8, 16, 32 or 64 times the waves of a row
     uint32_t vectors;  // 1 or 2
-    uint32_t threads;  // of a workgroup
+    uint32_t threads;  // of a workgroup: whole rows of threads, one where a row takes several waves
+    uint32_t waves() const { return lanes / 64; }
     uint32_t teams() const { return threads / lanes; }
 };
-RowShape row_shape(uint32_t width);
+// columns: of a wave, where a row takes more than a part of one; 512 or 1024
+inline RowShape row_shape(uint32_t width, uint32_t columns) {
+    if (width <= 64) return {8, 1, 256};
+    if (width <= 128) return {16, 1, 256};
+    if (width <= 256) return {32, 1, 256};
+    const uint32_t few = (width + columns - 1) / columns, waves = few < 16 ? few : 16;
+    return {64 * waves, waves * 512 < width ? 2u : 1u, waves == 1 ? 256 : 64 * waves};
+}
+// Two vectors a thread take fewer meetings of waves and fewer sums over lanes for a row; their registers fit four waves at most.
+// 65536 rows of 1024 bf16, one vector and two: residual 101 and 96 us, norm_grad 105 and 94, residual_grad 134 and 122 (8192 columns,
+// forward: 185 and 269).  What keeps most in registers stays at one: gates of groups (218 and 362), and fp32 streams with the sums of a
+// post norm (65536 x 2048: 468 and 525).
+inline RowShape forward_shape(uint32_t width) { return row_shape(width, width <= 4096 ? 1024 : 512); }
+inline RowShape grad_shape(uint32_t width, int mode, bool f32) { return row_shape(width, width <= 4096 && mode < (f32 ? 2 : 3) ? 1024 : 512); }
 
-hipError_t launch_dropout(int dtype, const DropoutArgs &a, hipStream_t s);
+// What a call works on decides the kernel: see the kernels' MODE.
+inline int forward_mode(const ResidualArgs &a) { return !a.f ? 0 : a.gate_rows ? 3 : a.post.kind ? 2 : 1; }
+inline int grad_mode(const ResidualGradArgs &a) { return !a.df ? 0 : a.gate_rows ? 3 : a.f ? 2 : 1; }
+// Waves of a SIMD that the kernels' registers leave room for, by mode and by vectors of a thread; a launch has as many workgroups as run at once.
+constexpr int kForwardWaves[2][4] = {{6, 5, 4, 4}, {4, 3, 3, 2}}, kGradWaves[2][4] = {{4, 4, 3, 3}, {2, 2, 2, 2}};
+constexpr int resident(const int (&waves)[2][4], uint32_t vectors, int mode, uint32_t threads) {
+    return threads > 256 ? 4 : waves[vectors - 1][mode];  // 1024 threads leave no less than four
+}
+
+// f(a type that names the lanes of a wave that share a row, a thread's vectors and a workgroup's most threads)
+template <int T_, int V_, int MOST_>
+struct Shape {
+    static constexpr int T = T_, V = V_, MOST = MOST_;
+};
+template <typename F>
+void with_shape(const RowShape &r, F f) {
+    if (r.lanes == 8) return f(Shape<8, 1, 256>());
+    if (r.lanes == 16) return f(Shape<16, 1, 256>());
+    if (r.lanes == 32) return f(Shape<32, 1, 256>());
+    if (r.threads <= 256 && r.vectors == 1) return f(Shape<64, 1, 256>());
+    if (r.threads <= 256) return f(Shape<64, 2, 256>());
+    if (r.vectors == 1) return f(Shape<64, 1, 1024>());
+    f(Shape<64, 2, 1024>());
+}
+template <typename F>
+void with_mode(int mode, F f) {
+    if (mode == 0) return f(std::integral_constant<int, 0>());
+    if (mode == 1) return f(std::integral_constant<int, 1>());
+    if (mode == 2) return f(std::integral_constant<int, 2>());
+    f(std::integral_constant<int, 3>());
+}
+
+// f(whether to read past the caches, whether the row's end cuts a piece of the columns): ragged rows are read through the caches.
+// piece: columns that are read at once.
+template <typename F>
+void with_access(uint32_t width, uint32_t piece, bool stream, F f) {
+    if (width % piece) return f(std::false_type(), std::true_type());
+    if (stream) return f(std::true_type(), std::false_type());
+    f(std::false_type(), std::false_type());
+}
+
+// The kernels of one pair of types, each in a source file of its own: the stream's type TS, the branch's TB.
+template <typename TS, typename TB>
+void launch_forward(const ResidualArgs &a, hipStream_t s);
+template <typename TS, typename TB>
+void launch_grad(const ResidualGradArgs &a, hipStream_t s);
+
+hipError_t launch_dropout(int dtype, DropoutArgs a, hipStream_t s);
 hipError_t launch_residual(int stream, int branch, const ResidualArgs &a, hipStream_t s);
 hipError_t launch_residual_grad(int stream, int branch, const ResidualGradArgs &a, hipStream_t s);
 hipError_t launch_residual_join(const ResidualGradArgs &a, hipStream_t s);

@@ -2,7 +2,7 @@
 the CPU, with bounds of what fp32 arithmetic may be off.
 
 U = 2^-24 is half a step of fp32.  A row's sum of n terms runs through at most 16 terms
-of a thread, 6 levels over lanes and 16 waves: K = 40 roundings, so it is off by at
+of a thread, 6 levels over lanes and 16 waves, and one product makes it a mean: K = 40 roundings, so it is off by at
 most K U sum |terms|, plus what the terms are off.  Each value comes with its
 bound, carried through the formulas to first order with a factor of 1.01 for the rest."""
 
@@ -95,7 +95,8 @@ def norm_back(dy, edy, x, mean, rstd, n):
     if n.kind == "layer":
         mg, emg = g.mean(1, keepdim=True), ((K + 2) * U * g.abs() + eg).mean(1, keepdim=True)
     inner = g - mg - xhat * mgx
-    e = eg + emg + ex * mgx.abs() + xhat.abs() * emgx + U * (2 * (g - mg).abs() + 2 * (xhat * mgx).abs() + inner.abs())
+    # the means are multiplied by rstd first: one rounding each, then xhat's fused product with the other, then the sum
+    e = eg + emg + ex * mgx.abs() + xhat.abs() * emgx + U * (2 * mg.abs() + 3 * (xhat * mgx).abs() + 2 * (g - mg).abs() + inner.abs())
     dx = rstd * inner
     return dx, SLACK * (rstd * e + U * dx.abs()), dy * xhat, SLACK * (edy * xhat.abs() + dy.abs() * ex), dy, edy
 
@@ -124,7 +125,10 @@ def residual_sum(h, f, alpha, beta, post, gate, gate_rows, mask):
         v, ev, *st = norm(f, post)
     if gate is not None:
         q = gate_of(gate, gate_rows, rows)
-        v, ev = v * q, ev * q.abs()
+        # a norm's gain and bias may be multiplied by the gate first: one rounding each
+        bias = post.b(f.shape[1]) if post is not None else 0.0
+        size = (v - bias).abs() + abs(bias)
+        v, ev = v * q, ev * q.abs() + U * size * q.abs()
         ev = ev + U * v.abs()
     if mask is not None:
         keep, factor = torch.from_numpy(mask[0]), float(mask[1])
