@@ -88,7 +88,8 @@ Split split_rows(uint32_t rows, const RowShape &r, int mode) {
     return {groups, (rows + groups * teams - 1) / (groups * teams)};
 }
 
-// Floats of the parts, and of the edges, of the largest of all calls of at most these rows and columns.
+// Floats of the parts, and of the edges, of the largest of all calls of at most these rows and columns, whatever shape
+// (one or two vectors a thread) and mode they have.
 struct Room {
     size_t parts, edges;
     size_t bytes() const { return std::max((size_t)256, round_up(parts * sizeof(float), 256) + round_up(edges * sizeof(float), 256)); }
@@ -97,9 +98,8 @@ Room room(uint32_t rows, uint32_t width, bool edges) {
     Room most = {0, 0};
     const auto count = [&](uint32_t w) {
         for (int k = 0; k < 8; k++) {
-            const int mode = k & 3;
-            const RowShape r = grad_shape(w, mode, k & 4);
-            const uint32_t groups = split_rows(rows, r, mode).groups;
+            const RowShape r = row_shape(w, k & 4 ? 1024 : 512);
+            const uint32_t groups = split_rows(rows, r, k & 3).groups;
             most.parts = std::max(most.parts, (size_t)groups * kBlockSums * w);
             if (edges) most.edges = std::max(most.edges, (size_t)groups * r.teams() * 2 * w);
         }

@@ -72,7 +72,7 @@ hipError_t launch_dropout(int dtype, DropoutArgs a, hipStream_t s) {
     const dim3 groups((a.rows + a.per - 1) / a.per, pieces);
     const auto go = [&](auto t) {
         typedef decltype(t) T;
-        with_access(a.width, E, (uint64_t)a.rows * a.width * sizeof(T) >= kStreamBytes, [&](auto streaming, auto ragged) {
+        with_access<Shape<64, 1, 256>>(a.width % E, (uint64_t)a.rows * a.width * sizeof(T) >= kStreamBytes, [&](auto streaming, auto ragged) {
             dropout_kernel<T, decltype(streaming)::value, decltype(ragged)::value><<<groups, threads, 0, s>>>(a);
         });
     };

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
 
 template <typename TS, typename TB>
 void launch_forward(const ResidualArgs &a, hipStream_t s) {
-    const RowShape r = forward_shape(a.width);
+    const RowShape r = forward_shape(a.width, sizeof(TS) == 4);
     const int mode = forward_mode(a);
     const uint32_t most = kSimds * resident(kForwardWaves, r.vectors, mode, r.threads) * 64 / r.threads;
     const uint32_t groups = std::min((a.rows + r.teams() - 1) / r.teams(), most);
@@ -127,7 +127,7 @@ void launch_forward(const ResidualArgs &a, hipStream_t s) {
     with_shape(r, [&](auto sh) {
         with_mode(mode, [&](auto m) {
             typedef decltype(sh) S;
-            with_access(a.width, sizeof(TS) == 4 ? 4 : 8, stream, [&](auto streaming, auto ragged) {
+            with_access<S>(ragged_row(a.width, sizeof(TS) == 4), stream, [&](auto streaming, auto ragged) {
                 residual_kernel<TS, TB, S::T, S::V, S::MOST, decltype(m)::value, decltype(streaming)::value, decltype(ragged)::value>
                     <<<groups, r.threads, 0, s>>>(a, r.waves(), groups * r.teams());
             });

@@ -238,10 +238,12 @@ void launch_grad(const ResidualGradArgs &a, hipStream_t s) {
     with_shape(r, [&](auto sh) {
         with_mode(mode, [&](auto m) {
             typedef decltype(sh) S;
-            with_access(a.width, sizeof(TS) == 4 ? 4 : 8, stream, [&](auto streaming, auto ragged) {
-                residual_grad_kernel<TS, TB, S::T, S::V, S::MOST, decltype(m)::value, decltype(streaming)::value, decltype(ragged)::value>
-                    <<<a.groups, r.threads, 0, s>>>(a, r.waves(), a.groups * r.teams());
-            });
+            constexpr int MODE = decltype(m)::value;
+            if constexpr (S::V == 1 || S::MOST == 1024 || MODE < (sizeof(TS) == 4 ? 2 : 3))  // what grad_shape gives
+                with_access<S>(ragged_row(a.width, sizeof(TS) == 4), stream, [&](auto streaming, auto ragged) {
+                    residual_grad_kernel<TS, TB, S::T, S::V, S::MOST, MODE, decltype(streaming)::value, decltype(ragged)::value>
+                        <<<a.groups, r.threads, 0, s>>>(a, r.waves(), a.groups * r.teams());
+                });
         });
     });
 }

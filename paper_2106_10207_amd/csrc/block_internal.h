@@ -109,8 +109,12 @@ inline RowShape row_shape(uint32_t width, uint32_t columns) {
 // 65536 rows of 1024 bf16, one vector and two: residual 101 and 96 us, norm_grad 105 and 94, residual_grad 134 and 122 (8192 columns,
 // forward: 185 and 269).  What keeps most in registers stays at one: gates of groups (218 and 362), and fp32 streams with the sums of a
 // post norm (65536 x 2048: 468 and 525).
-inline RowShape forward_shape(uint32_t width) { return row_shape(width, width <= 4096 ? 1024 : 512); }
-inline RowShape grad_shape(uint32_t width, int mode, bool f32) { return row_shape(width, width <= 4096 && mode < (f32 ? 2 : 3) ? 1024 : 512); }
+// Ragged rows (see with_access) stay at one too, for the sake of the code's size.
+inline bool ragged_row(uint32_t width, bool f32) { return width % (f32 ? 4 : 8); }
+inline RowShape forward_shape(uint32_t width, bool f32) { return row_shape(width, width <= 4096 && !ragged_row(width, f32) ? 1024 : 512); }
+inline RowShape grad_shape(uint32_t width, int mode, bool f32) {
+    return row_shape(width, width <= 4096 && mode < (f32 ? 2 : 3) && !ragged_row(width, f32) ? 1024 : 512);
+}
 
 // What a call works on decides the kernel: see the kernels' MODE.
 inline int forward_mode(const ResidualArgs &a) { return !a.f ? 0 : a.gate_rows ? 3 : a.post.kind ? 2 : 1; }
@@ -144,12 +148,15 @@ void with_mode(int mode, F f) {
     f(std::integral_constant<int, 3>());
 }
 
-// f(whether to read past the caches, whether the row's end cuts a piece of the columns): ragged rows are read through the caches.
-// piece: columns that are read at once.
-template <typename F>
-void with_access(uint32_t width, uint32_t piece, bool stream, F f) {
-    if (width % piece) return f(std::false_type(), std::true_type());
-    if (stream) return f(std::true_type(), std::false_type());
+// f(whether to read past the caches, whether the row's end cuts a piece of the columns that are read at once).  Only rows of
+// whole waves are read past the caches, and only those that a thread holds in one vector may be ragged, or in two of more than 8192 columns.
+template <typename S, typename F>
+void with_access(bool ragged, bool stream, F f) {
+    constexpr bool wide = S::V == 2 && S::MOST == 1024;
+    if constexpr (S::V == 1 || wide)
+        if (ragged) return f(std::false_type(), std::true_type());
+    if constexpr (S::T == 64 && !wide)
+        if (stream) return f(std::true_type(), std::false_type());
     f(std::false_type(), std::false_type());
 }
 

@@ -40,7 +40,9 @@ __device__ inline void load_part(const T *row, uint32_t c, uint32_t width, T *o)
         __builtin_memcpy(o, w, sizeof w);
     } else {
 #pragma unroll
-        for (int i = 0; i < N; i++) o[i] = c + i < width ? row[c + i] : (T)0.0f;
+        for (int i = 0; i < N; i++) o[i] = row[min(c + i, width - 1)];
+#pragma unroll
+        for (int i = 0; i < N; i++) o[i] = c + i < width ? o[i] : (T)0.0f;
     }
 }
 template <int N, bool STREAM, bool RAGGED, typename T>

@@ -114,6 +114,7 @@ class dedloc_dropout_cfg(ctypes.Structure):
 
 
 class dedloc_norm_cfg(ctypes.Structure):
+    _width = None  # of the vectors, where norm_cfg was given any
     _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
@@ -965,19 +966,44 @@ def norm_cfg(kind: int, gain=None, bias=None, eps: float = 1e-12) -> dedloc_norm
     its width (None: ones, zeros)."""
     cfg = dedloc_norm_cfg(kind, eps, _vector(gain, "gain"), _vector(bias, "bias"))
     cfg._keep = gain, bias
+    widths = {t.numel() for t in cfg._keep if t is not None}
+    if len(widths) > 1:
+        raise ValueError(f"gain and bias differ in length: {sorted(widths)}")
+    cfg._width = widths.pop() if widths else None
     return cfg
 
 
 def _check_norm(cfg, width: int, name: str):
-    for t, what in zip(cfg._keep, ("gain", "bias")):
-        _vector(t, f"{name}'s {what}", width)
+    if cfg._width is not None and cfg._width != width:
+        raise ValueError(f"{name}: its vectors have {cfg._width} elements, the rows {width}")
+
+
+@functools.lru_cache(maxsize=None)
+def _current_device():
+    import torch
+    try:
+        return torch._C._cuda_getDevice
+    except AttributeError:
+        return torch.cuda.current_device
+
+
+def _first(t, name: str):
+    """_rows of a call's first matrix, which must be on the current device: the
+    call's stream is that device's."""
+    got = _rows(t, name)
+    if t.get_device() != _current_device()():
+        raise ValueError(f"{name}: on device {t.get_device()}, the current one is {_current_device()()}")
+    return got
 
 
 def _same(t, like, name: str, dtype=None):
-    """(address, row stride) of a matrix of the shape of `like` (None: NULL)."""
+    """(address, row stride) of a matrix of the shape and on the device of `like`
+    (None: NULL)."""
     if t is None:
         return None, 0
     p, ld, r, c = _rows(t, name)
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name}: on device {t.get_device()}, expected {like.get_device()}")
     if t.shape != like.shape:
         raise ValueError(f"{name}: expected {tuple(like.shape)}, got {tuple(t.shape)}")
     if dtype is not None and t.dtype is not dtype:
@@ -994,7 +1020,7 @@ def _stats(t, norms: int, rows: int):
 def dedloc_dropout(x, cfg: dedloc_dropout_cfg, out=None, stream=None):
     """The rows of x with the mask that cfg names; out may be x.  The gradient is
     the same call on the output's gradient."""
-    p, ld, rows, width = _rows(x, "x")
+    p, ld, rows, width = _first(x, "x")
     if out is None:
         import torch
         with _allocating_on(stream):
@@ -1007,7 +1033,7 @@ def dedloc_dropout(x, cfg: dedloc_dropout_cfg, out=None, stream=None):
 def dedloc_norm(x, norm: dedloc_norm_cfg, out=None, out_dtype=None, stats=None, keep_stats: bool = True, stream=None):
     """(norm of the rows of x, stats): stats [1, rows, 2] hold (mean, rstd) for
     dedloc_norm_grad; keep_stats False: None, not written."""
-    p, ld, rows, width = _rows(x, "x")
+    p, ld, rows, width = _first(x, "x")
     _check_norm(norm, width, "norm")
     if out is None or (stats is None and keep_stats):
         import torch
@@ -1036,7 +1062,7 @@ def dedloc_norm_grad(dout, x, stats, norm: dedloc_norm_cfg, dgain=None, dbias=No
                      dx=None, ws=None, stream=None):
     """The gradient of dedloc_norm's x (plus `add`); dgain and dbias, fp32
     accumulators, take batch_samples times theirs.  Returns dx."""
-    p, ld, rows, width = _rows(x, "x")
+    p, ld, rows, width = _first(x, "x")
     _check_norm(norm, width, "norm")
     if dx is None or (ws is None and (dgain is not None or dbias is not None)):
         import torch
@@ -1090,7 +1116,7 @@ class ResidualCall:
 
     def __init__(self, h, f, sum=None, out=None, stats=None, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None,
                  gate=None, gate_rows: int = 0, drop=None):
-        p, ld, rows, width = _rows(h, "h")
+        p, ld, rows, width = _first(h, "h")
         (fp, fl), (sp, sl) = _same(f, h, "f"), _same(sum, h, "sum", h.dtype)
         op, ol = _same(out, h, "out", f.dtype)
         self._block = _Block(h, f, alpha, beta, post, pre, gate, gate_rows, drop)
@@ -1131,7 +1157,7 @@ class ResidualGradCall:
 
     def __init__(self, sum, f, stats, dsum, dout, dh, df, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None, gate=None,
                  gate_rows: int = 0, drop=None, dgate=None, dpre=None, dpost=None, batch_samples: float = 1.0, ws=None):
-        _, _, rows, width = _rows(dh, "dh")
+        _, _, rows, width = _first(dh, "dh")
         self._block = _Block(dh, df, alpha, beta, post, pre, gate, gate_rows, drop)
         self.cfg = self._block.cfg
         g = self.grads = dedloc_residual_grads()

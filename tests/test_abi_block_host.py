@@ -165,6 +165,10 @@ def test_binding_refusals():
         D.norm_cfg(D.DEDLOC_NORM_LAYER, torch.ones(6))
     with pytest.raises(ValueError, match="device tensor"):
         D.dedloc_norm(x, D.norm_cfg(D.DEDLOC_NORM_RMS))
+    cfg = D.norm_cfg(D.DEDLOC_NORM_LAYER)
+    cfg._width = 7  # as norm_cfg leaves it, had it been given vectors of 7
+    with pytest.raises(ValueError, match="7 elements"):
+        D._check_norm(cfg, 6, "norm")
     with pytest.raises(ValueError, match="one int64"):
         D.dropout_cfg(0.1, step_at=torch.zeros(2, dtype=torch.int64))
     with pytest.raises(ValueError, match="device tensor"):
