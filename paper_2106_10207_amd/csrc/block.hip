@@ -36,6 +36,9 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
             float v[E];
 #pragma unroll
             for (int i = 0; i < E; i++) v[i] = (float)r[k + i / P][i % P];
+            if constexpr (RAGGED)
+#pragma unroll
+                for (int i = 0; i < E; i += P) align<P>(v + i, c, a.width);
             const uint64_t at = row + k * a.down;
             if (at >= end) break;
             if (a.drop.threshold) {

@@ -76,11 +76,11 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
         if (row < a.rows) fetch(row);
         float x[N];
 #pragma unroll
-        for (int v = 0; v < V; v++) unpack(h[v], x + v * E);
+        for (int v = 0; v < V; v++) team.unpack(h[v], v, x + v * E);
         if constexpr (MODE > 0) {
             float y[N];
 #pragma unroll
-            for (int v = 0; v < V; v++) unpack(f[v], y + v * E);
+            for (int v = 0; v < V; v++) team.unpack(f[v], v, y + v * E);
             float2 st = make_float2(0.0f, 1.0f);
             if (MODE == 2 || (MODE == 3 && a.post.kind)) {
                 st = team.stats(y, a.post);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
                     z[i] = MODE > 1 ? fmaf((z[i] - st.x) * st.y, times[v * E + i], plus[v * E + i]) : z[i] * times[v * E + i];
                 if constexpr (MODE == 3) {
                     float g[E];
-                    unpack(gate[v], g);
+                    team.unpack(gate[v], v, g);
 #pragma unroll
                     for (int i = 0; i < E; i++) z[i] *= g[i];
                 }

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
                 for (int v = 0; v < V; v++) {
                     Raw<TB> r = {};
                     team.pieces(v, [&](int p) { team.template load<false>(r, (const TB *)a.gate + group * a.ld_gate, v, p); });
-                    unpack(r, q + v * E);
+                    team.unpack(r, v, q + v * E);
                     team.parameters(post ? a.post.gain : nullptr, v, 1.0f, times + v * E);
 #pragma unroll
                     for (int i = v * E; i < (v + 1) * E; i++) {
@@ -105,13 +105,13 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
         float d[N] = {};
         if (a.dsum)
 #pragma unroll
-            for (int v = 0; v < V; v++) unpack(dsum[v], d + v * E);
+            for (int v = 0; v < V; v++) team.unpack(dsum[v], v, d + v * E);
         if (pre) {
             float xhat[N], g[N], sg = 0.0f, sx = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; v++) {
-                unpack(x[v], xhat + v * E);
-                unpack(dout[v], g + v * E);
+                team.unpack(x[v], v, xhat + v * E);
+                team.unpack(dout[v], v, g + v * E);
                 // columns behind the row's end hold no gradient: whatever they add is zero
 #pragma unroll
                 for (int i = v * E; i < (v + 1) * E; i++) {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
                     for (int i = 0; i < E; i++) w[i] *= factor;
                 }
                 if constexpr (SUMS) {
-                    unpack(f[v], y);
+                    team.unpack(f[v], v, y);
 #pragma unroll
                     for (int i = 0; i < E; i++) y[i] = (y[i] - st_f.x) * st_f.y;
                 }

@@ -21,29 +21,44 @@ struct Unaligned {
     T v[N];
 } __attribute__((packed, aligned(sizeof(T))));
 
-// N columns from c on of a row, read past the caches (STREAM) or through them.  RAGGED: those behind the row's end are zeros; else
-// all are there.
+// N columns from c on of a row, read past the caches (STREAM) or through them.  RAGGED: where the
+// row's end cuts them, the row's last N instead, which align() puts in place once they have arrived; else all are there.
 typedef unsigned Word2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef unsigned Word4 __attribute__((ext_vector_type(4), aligned(2)));
 template <int N, bool STREAM, bool RAGGED, typename T>
 __device__ inline void load_part(const T *row, uint32_t c, uint32_t width, T *o) {
     typedef std::conditional_t<N * sizeof(T) == 8, Word2, Word4> Word;
     constexpr int WORDS = N * sizeof(T) / sizeof(Word);
-    if (!RAGGED || c + N <= width) {
-        Word w[WORDS];
+    if (RAGGED && width < N) {
 #pragma unroll
-        for (int i = 0; i < WORDS; i++)
-            if constexpr (STREAM)
-                w[i] = __builtin_nontemporal_load((const Word *)(row + c) + i);
-            else
-                w[i] = ((const Word *)(row + c))[i];
-        __builtin_memcpy(o, w, sizeof w);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++) o[i] = row[min(c + i, width - 1)];
-#pragma unroll
-        for (int i = 0; i < N; i++) o[i] = c + i < width ? o[i] : (T)0.0f;
+        for (int i = 0; i < N; i++) o[i] = row[min((uint32_t)i, width - 1)];
+        return;
     }
+    if (RAGGED) c = min(c, width - N);
+    Word w[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; i++)
+        if constexpr (STREAM)
+            w[i] = __builtin_nontemporal_load((const Word *)(row + c) + i);
+        else
+            w[i] = ((const Word *)(row + c))[i];
+    __builtin_memcpy(o, w, sizeof w);
+}
+// What load_part<N, .., true> took for columns from c on, moved to their places, zeros behind the row's end.
+template <int N>
+__device__ inline void align(float *o, uint32_t c, uint32_t width) {
+    if (c + N <= width) return;
+    if (width >= N) {
+        const uint32_t s = c - (width - N);
+#pragma unroll
+        for (uint32_t k = 1; k < N; k *= 2) {
+            const bool by = s & k;
+#pragma unroll
+            for (uint32_t i = 0; i < N; i++) o[i] = by ? (i + k < N ? o[i + k] : 0.0f) : o[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) o[i] = c + i < width ? o[i] : 0.0f;
 }
 template <int N, bool STREAM, bool RAGGED, typename T>
 __device__ inline void store_part(T *row, uint32_t c, uint32_t width, const float *o) {
@@ -67,12 +82,6 @@ __device__ inline void store_part(T *row, uint32_t c, uint32_t width, const floa
             if (c + i < width) row[c + i] = (T)o[i];
     }
 }
-template <typename T>
-__device__ inline void unpack(const Raw<T> &r, float *o) {
-#pragma unroll
-    for (int i = 0; i < E; i++) o[i] = (float)r.v[i];
-}
-
 // fp32 v rounded to T and back: the result of the fp32 operation before it (without this an fp16 one becomes a single
 // instruction with a rounding of its own).
 template <typename T>
@@ -269,12 +278,20 @@ struct Team {
     __device__ void store(D *row, int v, int p, const float *o) const {
         store_part<P, STREAM, RAGGED>(row, column(v, p), width, o + p * P);
     }
+    template <typename D>
+    __device__ void unpack(const Raw<D> &r, int v, float *o) const {
+#pragma unroll
+        for (int i = 0; i < E; i++) o[i] = (float)r.v[i];
+        if constexpr (RAGGED)
+#pragma unroll
+            for (int p = 0; p < PARTS; p++) align<P>(o + p * P, column(v, p), width);
+    }
     // A vector of parameters; `other` where there is none.
     __device__ void parameters(const float *q, int v, float other, float *o) const {
         if (q) {
             Raw<float> r = {};
             pieces(v, [&](int p) { load<false>(r, q, v, p); });
-            unpack(r, o);
+            unpack(r, v, o);
         } else {
 #pragma unroll
             for (int i = 0; i < E; i++) o[i] = other;
