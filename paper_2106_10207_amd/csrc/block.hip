@@ -155,15 +155,20 @@ __global__ __launch_bounds__(1024) void residual_join_kernel(ResidualGradArgs a)
 }
 
 // The gate's gradient of groups of rows that more than one team has: team `id` holds the start, the next ones the rest.
-__global__ __launch_bounds__(1024) void gate_join_kernel(ResidualGradArgs a, uint32_t all) {
+// A workgroup per group, or, where teams are fewer, per team: of those that start in its range only the last can be cut.
+__global__ __launch_bounds__(1024) void gate_join_kernel(ResidualGradArgs a, uint32_t all, bool by_group) {
     __shared__ float cells[16][64];
-    const uint32_t id = blockIdx.x, x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.y * 64 + x;
-    const uint64_t begin = (uint64_t)id * a.turns, end = min(begin + a.turns, (uint64_t)a.rows);
-    if (begin >= end) return;
-    const uint32_t group = (uint32_t)((end - 1) / a.gate_rows);
+    const uint32_t x = threadIdx.x & 63, y = threadIdx.x >> 6, c = blockIdx.y * 64 + x;
+    uint32_t group = blockIdx.x;
+    if (!by_group) {
+        const uint64_t begin = (uint64_t)blockIdx.x * a.turns, end = min(begin + a.turns, (uint64_t)a.rows);
+        if (begin >= end) return;
+        group = (uint32_t)((end - 1) / a.gate_rows);
+        if ((uint64_t)group * a.gate_rows < begin) return;  // another team's
+    }
     const uint64_t from = (uint64_t)group * a.gate_rows, to = min(from + a.gate_rows, (uint64_t)a.rows);
-    if (from < begin || to <= end) return;  // another team's to join, or whole
-    const uint32_t last = (uint32_t)((to - 1) / a.turns);
+    const uint32_t id = (uint32_t)(from / a.turns), last = (uint32_t)((to - 1) / a.turns);
+    if (id == last) return;  // whole
     float t = 0.0f;
     if (c < a.width)
         for (uint32_t k = id + y; k <= last; k += 16) t += a.edge[((uint64_t)(k == id) * all + k) * a.width + c];
@@ -206,8 +211,9 @@ hipError_t launch_residual_join(const ResidualGradArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_gate_join(const ResidualGradArgs &a, hipStream_t s) {
-    const uint32_t all = a.groups * grad_shape(a.width, 3, a.f32).teams();
-    gate_join_kernel<<<dim3(all, (a.width + 63) / 64), 1024, 0, s>>>(a, all);
+    if (a.turns % a.gate_rows == 0) return hipSuccess;  // no range of rows cuts a group
+    const uint32_t all = a.groups * grad_shape(a.width, 3, a.f32).teams(), gates = (a.rows + a.gate_rows - 1) / a.gate_rows;
+    gate_join_kernel<<<dim3(std::min(all, gates), (a.width + 63) / 64), 1024, 0, s>>>(a, all, gates < all);
     return hipGetLastError();
 }
 

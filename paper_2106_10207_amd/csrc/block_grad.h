@@ -71,8 +71,11 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
     const uint64_t first = GROUPS ? (uint64_t)id * a.turns : id;
     const uint32_t end = GROUPS ? (uint32_t)min(first + a.turns, (uint64_t)a.rows) : a.rows;
     uint32_t row = (uint32_t)min(first, (uint64_t)a.rows), begun = row;
-    if (row < end) fetch(row);
+    // two vectors of 16 waves leave no registers for a row on its way
+    constexpr bool AHEAD = V == 1 || MOST == 256;
+    if (AHEAD && row < end) fetch(row);
     while (row < end) {
+        if (!AHEAD) fetch(row);
 #pragma unroll
         for (int v = 0; v < V; v++) {
             x[v] = next_x[v];
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
         st_f = next_st_f;
         const uint32_t at = row;
         row += GROUPS ? 1 : all;
-        if (row < end) fetch(row);
+        if (AHEAD && row < end) fetch(row);
         if constexpr (GROUPS) {
             if (at / a.gate_rows != group) {
                 group = at / a.gate_rows;

@@ -991,7 +991,7 @@ def _first(t, name: str):
     """_rows of a call's first matrix, which must be on the current device: the
     call's stream is that device's."""
     shape = t.shape
-    if len(shape) == 2 and t.get_device() == _current_device()() and t.is_contiguous():
+    if t.is_cuda and len(shape) == 2 and t.get_device() == _current_device()() and t.is_contiguous():
         return t.data_ptr(), shape[1] or 1, shape[0], shape[1]
     got = _rows(t, name)
     if t.get_device() != _current_device()():
@@ -1005,7 +1005,7 @@ def _same(t, like, name: str, dtype=None):
     if t is None:
         return None, 0
     shape = like.shape
-    if t.get_device() == like.get_device() and t.shape == shape and (dtype is None or t.dtype is dtype) and t.is_contiguous():
+    if t.is_cuda and t.get_device() == like.get_device() and t.shape == shape and (dtype is None or t.dtype is dtype) and t.is_contiguous():
         return t.data_ptr(), shape[1] or 1  # the usual case, without what takes a microsecond more
     p, ld, r, c = _rows(t, name)
     if t.get_device() != like.get_device():
@@ -1204,6 +1204,8 @@ def dedloc_residual_grad(sum, f, stats, dsum, dout, alpha: float = 1.0, beta: fl
     norm, no dgate); df then has the type of dout, or of the stream."""
     import torch
     stream_like = dsum if dsum is not None else sum
+    if stream_like is None:
+        raise ValueError("sum or dsum is needed")
     branch_like = next(t for t in (f, dout, stream_like) if t is not None)
     with _allocating_on(stream):
         if dh is None:

@@ -173,3 +173,5 @@ def test_binding_refusals():
         D.dropout_cfg(0.1, step_at=torch.zeros(2, dtype=torch.int64))
     with pytest.raises(ValueError, match="device tensor"):
         D.dedloc_residual(x, x)
+    with pytest.raises(ValueError, match="sum or dsum"):
+        D.dedloc_residual_grad(None, None, None, None, x)

@@ -408,6 +408,34 @@ def test_gradients_against_differences(post, pre, gate):
         assert abs(mine - slope) <= (1e-7 + 200 * R.U) * (size + float(R.f64(dout).abs().sum()) / width), name
 
 
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^32 elements, in place: their last rows against the definitions, and the sums over all rows."""
+    n, width = 66000, 65600
+    x = torch.ones(n, width, dtype=BF16, device=DEV)
+    D.dedloc_dropout(x, D.dropout_cfg(0.25, 9), out=x)
+    assert torch.equal(x[-3:].cpu(), dropped(torch.ones(3, width, dtype=BF16, device=DEV), 0.25, seed=9, row0=n - 3))
+    del x
+    n, width = 270000, 16000
+    part, _ = rows(9, width, BF16, gen(41))
+    x = part.repeat(n // 9, 1)
+    cfg, ref = make_norm("layer", width, gen(42))
+    drop = D.dropout_cfg(0.25, 9)
+    total, _, stats = D.dedloc_residual(x, x, pre=cfg, drop=drop, out=torch.empty_like(x))
+    keep = R.kept(9, width, 0.25, seed=9, row0=n - 9)
+    want, bound, _ = R.residual_sum(R.f64(part), R.f64(part), 1.0, 1.0, None, None, 0, keep)
+    check(total[-9:], want, bound, BF16, "sum")
+    dgain, dbias = torch.zeros(2, width, device=DEV)
+    # every nine rows' gradient of the bias is the same: whole numbers, exact in any order below 2^24
+    ones = torch.ones(n, width, dtype=BF16, device=DEV)
+    dh, df = D.dedloc_residual_grad(total, None, stats, None, ones, pre=cfg, drop=drop, dpre=(dgain, dbias), dh=ones, df=x)
+    assert bool((dbias == n).all()) and dh is ones
+    d, e, *_ = R.norm_back(torch.ones(9, width, dtype=torch.float64), torch.zeros(9, width, dtype=torch.float64), R.f64(total[-9:]),
+                           R.f64(stats[0, -9:, :1]), R.f64(stats[0, -9:, 1:]), ref)
+    check(dh[-9:], d, e, BF16, "dh")
+    kept, factor = torch.from_numpy(keep[0]), float(keep[1])
+    check(df[-9:], torch.where(kept, d * factor, 0.0), torch.where(kept, e * factor + R.U * (d * factor).abs(), 0.0), BF16, "df")
+
+
 # --------------------------------------------------------- streams and graphs
 
 def test_captured_calls_draw_anew():
