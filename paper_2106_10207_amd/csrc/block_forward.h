@@ -63,7 +63,18 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
             });
         }
     };
+    // Loads and stores are counted as one: a wait for the next row's loads would be one for this row's stores too, of which some may
+    // have been left out, so the loads have to arrive before the last stores begin.
+    const auto arrived = [&] {
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            arrive(next_h[v]);
+            if constexpr (MODE > 0) arrive(next_f[v]);
+            if constexpr (MODE == 3) arrive(next_gate[v]);
+        }
+    };
     if (row < a.rows) fetch(row);
+    arrived();
     while (row < a.rows) {
 #pragma unroll
         for (int v = 0; v < V; v++) {
@@ -88,6 +99,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
                 st = team.stats(y, a.post);
                 if (a.stats && team.t == 0) a.stats[a.rows + at] = st;
             }
+            if (!a.pre.kind) arrived();
 #pragma unroll
             for (int v = 0; v < V; v++) {
                 float *z = y + v * E;
@@ -109,6 +121,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
         }
         if (!a.pre.kind) continue;
         const float2 st = team.stats(x, a.pre);
+        arrived();
         if (a.stats && team.t == 0) a.stats[at] = st;
 #pragma unroll
         for (int v = 0; v < V; v++) {

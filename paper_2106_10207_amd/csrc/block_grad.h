@@ -75,7 +75,20 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
     uint32_t row = (uint32_t)min(first, (uint64_t)a.rows), begun = row;
     // two vectors of 16 waves leave no registers for a row on its way
     constexpr bool AHEAD = V == 1 || MOST == 256;
+    // as in the forward pass: before the last stores of a row the next one's loads have arrived
+    const auto arrived = [&] {
+        if (!AHEAD) return;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            arrive(next_x[v]);
+            arrive(next_dout[v]);
+            arrive(next_dsum[v]);
+            if constexpr (SUMS) arrive(next_f[v]);
+        }
+        asm volatile("" : "+v"(next_st.x), "+v"(next_st.y), "+v"(next_st_f.x), "+v"(next_st_f.y));
+    };
     if (AHEAD && row < end) fetch(row);
+    arrived();
     while (row < end) {
         if (!AHEAD) fetch(row);
 #pragma unroll
@@ -133,6 +146,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
 #pragma unroll
             for (int i = 0; i < N; i++) d[i] += fmaf(g[i], st.y, fmaf(xhat[i], k1, k0));
         }
+        if (!BRANCH) arrived();
 #pragma unroll
         for (int v = 0; v < V; v++) {
             float o[E];
@@ -178,6 +192,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
 #pragma unroll
                 for (int i = 0; i < N; i++) d[i] = fmaf(d[i], st_f.y, fmaf(fhat[i], k1, k0));
             }
+            arrived();
 #pragma unroll
             for (int v = 0; v < V; v++) team.pieces(v, [&](int p) { team.template store<true>((TB *)a.df + at * a.ld_df, v, p, d + v * E); });
         }

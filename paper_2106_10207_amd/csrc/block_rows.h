@@ -82,6 +82,16 @@ __device__ inline void store_part(T *row, uint32_t c, uint32_t width, const floa
             if (c + i < width) row[c + i] = (T)o[i];
     }
 }
+// A use of what is on its way, so that it has arrived here.
+template <typename T>
+__device__ inline void arrive(Raw<T> &r) {
+    uint32_t w[sizeof(r) / 4];
+    __builtin_memcpy(w, &r, sizeof w);
+#pragma unroll
+    for (uint32_t i = 0; i < sizeof(r) / 4; i++) asm volatile("" : "+v"(w[i]));
+    __builtin_memcpy(&r, w, sizeof w);
+}
+
 // fp32 v rounded to T and back: the result of the fp32 operation before it (without this an fp16 one becomes a single
 // instruction with a rounding of its own).
 template <typename T>

@@ -127,7 +127,8 @@ def test_dropout_many_rows():
 
 SIZES = [(1, 1, 0, 0), (3, 7, 0, 1), (9, 64, 0, 0), (33, 65, 1, 0), (50, 128, 0, 0), (17, 200, 3, 1), (9, 256, 0, 0), (70, 333, 5, 3),
          (5, 512, 0, 0), (6, 513, 1, 0), (7, 1024, 0, 0), (3, 1500, 0, 2), (5, 2048, 0, 0), (3, 4001, 0, 1), (2, 8192, 0, 0),
-         (3, 8193, 0, 0), (2, 16384, 0, 0), (1, 16000, 7, 1)]
+         (3, 8193, 0, 0), (2, 16384, 0, 0), (1, 16000, 7, 1),
+         (5, 768, 0, 0), (3, 2560, 0, 0), (2, 6144, 0, 0), (2, 12000, 0, 0)]
 
 
 @pytest.mark.parametrize("n,width,pad,offset", SIZES)
@@ -406,6 +407,36 @@ def test_gradients_against_differences(post, pre, gate):
         mine = float((R.f64(got[name]) * d).sum())
         size = float((R.f64(got[name]).abs() * d.abs()).sum())
         assert abs(mine - slope) <= (1e-7 + 200 * R.U) * (size + float(R.f64(dout).abs().sum()) / width), name
+
+
+@pytest.mark.parametrize("width", [512, 1000, 4096, 5120])
+@pytest.mark.parametrize("post,pre,gate", [("layer", "rms", "channel"), (None, "layer", None), ("rms", "layer", "group")])
+@pytest.mark.parametrize("types", PAIRS)
+def test_large_calls_are_their_parts(types, post, pre, gate, width):
+    """A call that reads past the caches (96 MiB and more) gives the bits of calls on a few rows; the sums over its rows are those
+    of the definition with dout = dsum = 1, in 64 bits of the rows' own values."""
+    stream, branch = types
+    n, g = (100 << 20) // (2 * width) // 64 * 64 + 24, gen(width)
+    h, f = (rows(n, width, t, g)[0] for t in types)
+    (post_c, post_r), (pre_c, pre_r) = make_norm(post, width, g), make_norm(pre, width, g)
+    gate_rows = 64 if gate == "group" else 0
+    gate_t = vector(width, g, 0.5) if gate == "channel" else rows(-(-n // 64), width, branch, g)[0].contiguous() if gate else None
+    common = lambda a: dict(alpha=1.0, beta=0.5, post=post_c, pre=pre_c, gate_rows=gate_rows, drop=D.dropout_cfg(0.1, 3, row0=a),  # noqa: E731
+                            gate=gate_t[a // 64:a // 64 + 2] if gate_rows and a else gate_t)
+    total, out, stats = D.dedloc_residual(h, f, **common(0))
+    ones = torch.ones(n, width, dtype=branch, device=DEV)
+    dpre = torch.zeros(2, width, device=DEV)
+    dh, df = D.dedloc_residual_grad(total, f, stats, None, ones, dpre=(dpre[0], dpre[1]), **common(0))
+    for a in (n // 2 // 64 * 64, n - 88):  # at a group of rows
+        b = min(a + 88, n)
+        t, o, st = D.dedloc_residual(h[a:b], f[a:b], **common(a))
+        assert torch.equal(t, total[a:b]) and torch.equal(o, out[a:b]) and torch.equal(st[0], stats[0, a:b])
+        x, y = D.dedloc_residual_grad(t, f[a:b], st, None, ones[a:b], **common(a))
+        assert torch.equal(x, dh[a:b]) and torch.equal(y, df[a:b])
+    assert bool((dpre[1] == n).all())
+    xhat = (total.double() - stats[0, :, :1].double()) * stats[0, :, 1:].double()
+    want, size = xhat.sum(0).cpu(), xhat.abs().sum(0).cpu()
+    check(dpre[0], want, (n + 6) * R.U * size, F32, "dgain")
 
 
 def test_offsets_past_32_bits():
