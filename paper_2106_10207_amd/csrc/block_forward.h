@@ -10,10 +10,11 @@
 
 namespace dedloc {
 
-// The teams of a launch take the rows in turn; a row's vectors are on their way while the one before is worked on.  What a thread's columns are
-// scaled by stays in its registers.  Bound by memory: 65536 x 2048 fp32 with bf16 branches, two norms, a gate and dropout 308 us, 5.2 TB/s (the generator
-// and the norms take about half of that time of the vector units); 65536 x 1024 bf16 with one norm and dropout 96 us, 5.6 TB/s; the rms norm
-// of 65536 x 2048 bf16 89 us, 6.0 TB/s.  8192 x 1024 fp16 12.7 us: three rows a team, ramp and end.  MODE 0: the norm of h; 1: a branch without a post norm; 2: with one; 3: with a gate per group of rows.
+// The teams of a launch take the rows in turn; a row's vectors are on their way while the one before is worked on.  What a
+// thread's columns are scaled by stays in its registers.  MODE 0: the norm of h; 1: a branch without a post norm; 2: with one; 3: with
+// a gate per group of rows.  Bound by memory: 65536 x 2048 fp32 with bf16 branches, two norms, a gate and dropout 295 us, 5.5 TB/s
+// (vector instructions in 0.4 of the cycles); 65536 x 1024 bf16 with one norm and dropout 96 us, 5.6 TB/s; the rms norm of 65536 x
+// 2048 bf16 89 us, 6.0 TB/s.  8192 x 1024 fp16 12.5 us: three rows a team, ramp and end.
 template <typename TS, typename TB, int T, int V, int MOST, int MODE, bool STREAM, bool RAGGED>
 __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void residual_kernel(ResidualArgs a, uint32_t waves, uint32_t all) {
     constexpr int N = V * E;

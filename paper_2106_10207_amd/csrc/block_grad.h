@@ -13,9 +13,10 @@ namespace dedloc {
 // The formulas, with x the sum and f the branch, xhat = (x - mean) r, fhat likewise with r', g = gain dout:
 //   d = dsum + r (g - mean(g) - xhat mean(g xhat)),  dh = alpha d,  w = beta dropout(d)
 //   p = times w (times: gate and post's gain),  df = r' (p - mean(p) - fhat mean(p fhat))
-// Rows are taken as in the forward pass.  Bound by memory with the vector units busy about half the time: 65536 x 2048 bf16 with two norms, a
-// gate and dropout 309 us, 5.2 TB/s; 65536 x 1024 with one norm and dropout 117 us, 5.7 TB/s; fp32 streams 444 to 458 us, 5.3 TB/s; 262144 x
-// 64 bf16 18 us.  8192 x 1024 fp16 15 us: four rows a team.  Past 8192 columns two vectors in 128 registers spill: 8192 x 16384 406 us, 3.3 TB/s.
+// Rows are taken as in the forward pass.  Bound by memory, with vector instructions in half of the cycles: 65536 x 2048 bf16 with
+// two norms, a gate and dropout 304 us, 5.3 TB/s; 65536 x 1024 with one norm and dropout 123 with the join, 5.4 TB/s; an fp32 stream
+// of 65536 x 2048 445, 5.4 TB/s; 262144 x 64 bf16 18 us.  8192 x 1024 fp16 15 us: four rows a team.  Past 8192 columns two vectors
+// do not fit 128 registers: 8192 x 16384 415 us, 3.2 TB/s.
 template <typename TS, typename TB, int T, int V, int MOST, int MODE, bool STREAM, bool RAGGED>
 __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void residual_grad_kernel(ResidualGradArgs a, uint32_t waves,
                                                                                                   uint32_t all) {
@@ -173,7 +174,8 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
                 if constexpr (SUMS)
 #pragma unroll
                     for (int i = 0; i < E; i++) {
-                        float &s = GROUPS ? by_f[GROUPS ? v * E + i : 0] : acc[2][v * E + i], &t = GROUPS ? plain[GROUPS ? v * E + i : 0] : acc[3][v * E + i];
+                        float &s = GROUPS ? by_f[GROUPS ? v * E + i : 0] : acc[2][v * E + i],
+                              &t = GROUPS ? plain[GROUPS ? v * E + i : 0] : acc[3][v * E + i];
                         s = fmaf(w[i], y[i], s);
                         t += w[i];
                     }

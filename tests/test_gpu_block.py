@@ -70,7 +70,7 @@ def dropped(x, p, **cfg):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,width,pad,offset,p", [(1, 1, 0, 0, 0.5), (3, 7, 0, 1, 0.5), (1, 8, 0, 0, 0.9), (65, 9, 3, 1, 0.1),
                                                   (257, 64, 0, 0, 0.1), (31, 333, 5, 3, 0.25), (5, 16383, 1, 0, 0.3),
-                                                  (2, 16385, 1, 1, 0.3), (3, 40001, 0, 0, 0.7), (1000, 128, 0, 0, 1e-4)])
+                                                  (2, 16385, 1, 1, 0.3), (3, 40001, 0, 0, 0.7), (1000, 128, 0, 0, 1e-4), (37, 2049, 0, 0, 0.2), (19, 4098, 1, 0, 0.2), (1, 1, 0, 0, 0.25)])
 def test_dropout(dtype, n, width, pad, offset, p):
     g = gen(n + width)
     x, _ = rows(n, width, dtype, g, pad, offset)
