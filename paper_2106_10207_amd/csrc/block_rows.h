@@ -296,16 +296,18 @@ struct Team {
 #pragma unroll
             for (int p = 0; p < PARTS; p++) align<P>(o + p * P, column(v, p), width);
     }
-    // A vector of parameters; `other` where there is none.
+    // A vector of parameters; `other` where there is none.  Behind the row's end they are zero, and with them what they scale.
     __device__ void parameters(const float *q, int v, float other, float *o) const {
+        Raw<float> r = {};
         if (q) {
-            Raw<float> r = {};
             pieces(v, [&](int p) { load<false>(r, q, v, p); });
-            unpack(r, v, o);
         } else {
+            pieces(v, [&](int p) {
 #pragma unroll
-            for (int i = 0; i < E; i++) o[i] = other;
+                for (int i = 0; i < P; i++) r.v[p * P + i] = other;
+            });
         }
+        unpack(r, v, o);
     }
     // columns of a row that wave w of it holds
     __device__ uint32_t held(uint32_t w) const {

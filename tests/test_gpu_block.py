@@ -348,6 +348,15 @@ def test_residual_without_vectors(gain, bias):
     block(70, 100, F16, F16, "rms", "layer", "group", None, seed=9, gate_rows=9, gain=gain, bias=bias)
 
 
+@pytest.mark.parametrize("types", PAIRS)
+@pytest.mark.parametrize("n,width", [(1, 1), (20, 5), (33, 100), (21, 300), (17, 333), (9, 768), (7, 1000), (5, 2500), (3, 6100), (2, 12001)])
+def test_residual_of_bare_norms(types, n, width):
+    """Norms without a gain and no gate: nothing makes what the threads behind the row's end hold zero but themselves."""
+    for post, pre in (("layer", "layer"), ("layer", "rms"), ("rms", "layer")):
+        block(n, width, *types, post, pre, None, 0.2, seed=n, gain=False, bias=False)
+        block(n, width, *types, post, pre, None, None, seed=n, gain=False, bias=True)
+
+
 def test_residual_ends_of_p():
     block(20, 100, F32, F32, None, "layer", None, 1.0, seed=1)
     block(20, 100, F32, F32, None, "layer", None, 0.0, seed=1)
