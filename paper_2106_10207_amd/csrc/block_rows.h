@@ -1,4 +1,4 @@
-// Device code that the kernels of rows share (block.hip, block_grad.hip): vectors of a row, the
+// Device code that the kernels of rows share (block.hip, block_forward.h, block_grad.h): vectors of a row, the
 // generator of the dropout masks, and the sums of the threads that share a row.
 #pragma once
 

@@ -357,6 +357,37 @@ def test_residual_of_bare_norms(types, n, width):
         block(n, width, *types, post, pre, None, None, seed=n, gain=False, bias=True)
 
 
+@pytest.mark.parametrize("gate", ["channel", "group", None])
+@pytest.mark.parametrize("post,pre", [("layer", "rms"), (None, "layer"), ("rms", None), (None, None)])
+def test_gradients_that_are_not_wanted(post, pre, gate):
+    """Any of the vectors' gradients left out leaves the others as they are (other sums and shapes of the rows: a few roundings of sums
+    of at most 300 terms, 600 U of the largest value), and untouched what is not named."""
+    n, width, g = 300, 520, gen(51)
+    total, f, dsum, dout = (rows(n, width, F32, g)[0] for _ in range(4))
+    (post_c, post_r), (pre_c, pre_r) = make_norm(post, width, g), make_norm(pre, width, g)
+    gate_t = vector(width, g, 0.5) if gate == "channel" else rows(6, width, F32, g)[0].contiguous() if gate else None
+    st = torch.zeros(2, n, 2, device=DEV)
+    for k, (x, r) in enumerate(((total, pre_r), (f, post_r))):
+        if r is not None:
+            st[k] = torch.cat(R.stats(R.f64(x), r)[:2], 1).float()
+    common = dict(alpha=1.0, beta=0.5, post=post_c, pre=pre_c, gate=gate_t, gate_rows=50 if gate == "group" else 0, drop=D.dropout_cfg(0.2, 8))
+    names = (["dgate"] if gate else []) + (["pre gain", "pre bias"] if pre else []) + (["post gain", "post bias"] if post else [])
+
+    def run(wanted):
+        accs = {k: torch.zeros_like(gate_t) if k == "dgate" else torch.zeros(width, device=DEV) for k in wanted}
+        get = accs.get
+        dh, df = D.dedloc_residual_grad(total if pre else None, f, st, dsum, dout if pre else None, dgate=get("dgate"),
+                                        dpre=(get("pre gain"), get("pre bias")), dpost=(get("post gain"), get("post bias")), **common)
+        return dict(accs, dh=dh, df=df)
+
+    every = run(names)
+    for wanted in [[]] + [[k] for k in names] + [[k for k in names if k != out] for out in names]:
+        got = run(wanted)
+        for k, v in got.items():
+            assert float((v - every[k]).abs().max()) <= 600 * R.U * float(every[k].abs().max()), (wanted, k)
+        assert all(float(got[k].abs().max()) > 0 for k in wanted)
+
+
 def test_residual_ends_of_p():
     block(20, 100, F32, F32, None, "layer", None, 1.0, seed=1)
     block(20, 100, F32, F32, None, "layer", None, 0.0, seed=1)
