@@ -215,7 +215,8 @@ hipError_t launch_residual_join(const ResidualGradArgs &a, hipStream_t s) {
 
 hipError_t launch_gate_join(const ResidualGradArgs &a, hipStream_t s) {
     if (a.turns % a.gate_rows == 0) return hipSuccess;  // no range of rows cuts a group
-    const uint32_t all = a.groups * grad_shape(a.width, 3, a.f32).teams(), gates = (a.rows + a.gate_rows - 1) / a.gate_rows;
+    // gate_rows may be any number of 32 bits: no sum with it
+    const uint32_t all = a.groups * grad_shape(a.width, 3, a.f32).teams(), gates = (a.rows - 1) / a.gate_rows + 1;
     gate_join_kernel<<<dim3(std::min(all, gates), (a.width + 63) / 64), 1024, 0, s>>>(a, all, gates < all);
     return hipGetLastError();
 }
