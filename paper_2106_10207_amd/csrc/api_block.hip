@@ -59,7 +59,11 @@ int check_norm(const dedloc_norm_cfg &n, const char *name) {
     return rc ? rc : check_vector(n.bias, "bias");
 }
 
-NormArgs norm_args(const dedloc_norm_cfg &n) { return {n.kind, n.eps, n.gain, n.bias}; }
+// A norm that is left out has no vectors, whatever its struct points to: the kernels and the join ask for the vectors alone.
+NormArgs norm_args(const dedloc_norm_cfg &n) {
+    if (n.kind == DEDLOC_NORM_NONE) return {};
+    return {n.kind, n.eps, n.gain, n.bias};
+}
 
 int check_dropout(const dedloc_dropout_cfg &d) {
     if (!(d.p >= 0.0f && d.p <= 1.0f)) return fail(DEDLOC_ERR_INVALID_ARG, "p must be in [0, 1] (got %g)", (double)d.p);

@@ -973,6 +973,11 @@ def norm_cfg(kind: int, gain=None, bias=None, eps: float = 1e-12) -> dedloc_norm
     return cfg
 
 
+def _norm(cfg):
+    """None for a norm that its kind leaves out."""
+    return None if cfg is None or cfg.kind == DEDLOC_NORM_NONE else cfg
+
+
 def _check_norm(cfg, width: int, name: str):
     if cfg._width is not None and cfg._width != width:
         raise ValueError(f"{name}: its vectors have {cfg._width} elements, the rows {width}")
@@ -1093,7 +1098,7 @@ class _Block:
 
     def __init__(self, like, branch, alpha, beta, post, pre, gate, gate_rows, drop):
         rows, width = like.shape
-        none = dedloc_norm_cfg(DEDLOC_NORM_NONE, 0.0, None, None)
+        none, post, pre = dedloc_norm_cfg(DEDLOC_NORM_NONE, 0.0, None, None), _norm(post), _norm(pre)
         self.cfg = dedloc_residual_cfg(alpha, beta, post or none, pre or none, None, 0, gate_rows,
                                        drop or dedloc_dropout_cfg(0.0, 0, 0, 0, 0, None))
         self.norms = 2 if post is not None else 1 if pre is not None else 0
@@ -1145,6 +1150,7 @@ def dedloc_residual(h, f, alpha: float = 1.0, beta: float = 1.0, post=None, pre=
     without a pre norm).  keep False: what only the gradient needs (stats, and with a pre
     norm sum) is not made; it is None unless given."""
     import torch
+    post, pre = _norm(post), _norm(pre)
     with _allocating_on(stream):
         if sum is None and (keep or pre is None):
             sum = torch.empty(h.shape, dtype=h.dtype, device=h.device)

@@ -31,3 +31,46 @@ def test_a_group_longer_than_all_rows(n, width):
     want = run(n)
     for gate_rows in (n + 1, (1 << 31) + 5, (1 << 32) - n, (1 << 32) - 1):
         assert all(torch.equal(a, b) for a, b in zip(run(gate_rows), want)), gate_rows
+
+
+# ------------------------------------------------------------ norms left out
+
+@pytest.mark.parametrize("gate", [None, "channel", "group"])
+@pytest.mark.parametrize("left_out", ["post", "pre"])
+def test_what_a_norm_left_out_points_to_is_not_there(left_out, gate):
+    """A kind of DEDLOC_NORM_NONE leaves a norm out, whatever else its struct holds: the same bits as with NULL vectors, forward and backward."""
+    n, width, g = 300, 520, gen(61)
+    h, f, dsum, dout = (rows(n, width, BF16, g)[0] for _ in range(4))
+    gate_t = vector(width, g, 0.5) if gate == "channel" else rows(6, width, BF16, g)[0].contiguous() if gate else None
+    gain, bias = vector(width, g, 3.0), vector(width, g, -2.0)
+    other = make_norm("layer", width, g)[0]
+    post, pre = (None, other) if left_out == "post" else (other, None)
+    common = dict(alpha=1.0, beta=0.5, post=post, pre=pre, gate=gate_t, gate_rows=50 if gate == "group" else 0, drop=D.dropout_cfg(0.2, 8))
+
+    def run(vectors):
+        total, out, stats = torch.empty_like(h), torch.empty_like(h) if pre else None, torch.zeros(2, n, 2, device=DEV)
+        dh, df, acc = torch.empty_like(h), torch.empty_like(h), torch.zeros(2, width, device=DEV)
+        dgate = torch.zeros_like(gate_t, dtype=F32) if gate else None
+        calls = [D.ResidualCall(h, f, total, out, stats, **common),
+                 D.ResidualGradCall(total, f, stats, dsum, dout if pre else None, dh, df, dgate=dgate,
+                                    **{"dpre" if pre else "dpost": (acc[0], acc[1])}, **common)]
+        for call in calls:
+            norm = getattr(call.cfg, left_out)
+            assert norm.kind == D.DEDLOC_NORM_NONE
+            if vectors:
+                norm.gain, norm.bias, norm.eps = gain.data_ptr(), bias.data_ptr(), 1e-6
+            call()
+        return [t for t in (total, out, stats, dh, df, acc, dgate) if t is not None]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+def test_calls_without_a_norm_by_its_kind():
+    """A norm_cfg of DEDLOC_NORM_NONE through the binding is no norm."""
+    g = gen(62)
+    h, f, dsum = (rows(20, 96, F32, g)[0] for _ in range(3))
+    none = D.norm_cfg(D.DEDLOC_NORM_NONE)
+    total, out, stats = D.dedloc_residual(h, f, post=none, pre=none)
+    assert out is None and stats is None and torch.equal(total, D.dedloc_residual(h, f)[0])
+    got = D.dedloc_residual_grad(None, None, None, dsum, None, post=none, pre=none)
+    assert all(torch.equal(a, b) for a, b in zip(got, D.dedloc_residual_grad(None, None, None, dsum, None)))
