@@ -106,7 +106,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
                 float *z = y + v * E;
 #pragma unroll
                 for (int i = 0; i < E; i++)
-                    z[i] = MODE > 1 ? fmaf((z[i] - st.x) * st.y, times[v * E + i], plus[v * E + i]) : z[i] * times[v * E + i];
+                    z[i] = MODE > 1 ? fmaf((z[i] - team.about(v, i, st.x)) * st.y, times[v * E + i], plus[v * E + i]) : z[i] * times[v * E + i];
                 if constexpr (MODE == 3) {
                     float g[E];
                     team.unpack(gate[v], v, g);

@@ -134,7 +134,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
                 // columns behind the row's end hold no gradient: whatever they add is zero
 #pragma unroll
                 for (int i = v * E; i < (v + 1) * E; i++) {
-                    xhat[i] = (xhat[i] - st.x) * st.y;
+                    xhat[i] = (xhat[i] - team.about(v, i - v * E, st.x)) * st.y;
                     acc[0][i] = fmaf(g[i], xhat[i], acc[0][i]);
                     acc[1][i] += g[i];
                     g[i] *= gain[i];
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void res
                 if constexpr (SUMS) {
                     team.unpack(f[v], v, y);
 #pragma unroll
-                    for (int i = 0; i < E; i++) y[i] = (y[i] - st_f.x) * st_f.y;
+                    for (int i = 0; i < E; i++) y[i] = (y[i] - team.about(v, i, st_f.x)) * st_f.y;
                 }
                 if constexpr (SUMS)
 #pragma unroll

@@ -309,6 +309,9 @@ struct Team {
         }
         unpack(r, v, o);
     }
+    // The mean for vector v's column i, zero behind the row's end: x is zero there, and so has to be x - mean, whose product with a
+    // large 1 / deviation (equal entries of 2^117 and eps 1e-12: 2^137) no zero of a parameter would make zero again.
+    __device__ float about(int v, int i, float mean) const { return column(v, i / P) + (RAGGED ? i % P : 0) < width ? mean : 0.0f; }
     // columns of a row that wave w of it holds
     __device__ uint32_t held(uint32_t w) const {
         uint32_t n = 0;

@@ -74,3 +74,34 @@ def test_calls_without_a_norm_by_its_kind():
     assert out is None and stats is None and torch.equal(total, D.dedloc_residual(h, f)[0])
     got = D.dedloc_residual_grad(None, None, None, dsum, None, post=none, pre=none)
     assert all(torch.equal(a, b) for a, b in zip(got, D.dedloc_residual_grad(None, None, None, dsum, None)))
+
+
+# ------------------------------------------------------ rows of equal entries
+
+@pytest.mark.parametrize("width", [1, 4, 8, 16, 32])
+def test_equal_entries_whose_mean_times_rstd_overflows(width):
+    """Rows of 2^117, eps 1e-12: the mean is exact, 1e6 times it is none of fp32.  What the threads behind the row's end
+    hold stays zero all the same, forward and backward, for the norm before the sum and the one behind it."""
+    n, big = 5, 2.0 ** 117
+    g = gen(width)
+    cfg, _ = make_norm("layer", width, g)
+    gain, bias = (v for v in cfg._keep)
+    x = torch.full((n, width), big, device=DEV)
+    out, stats = D.dedloc_norm(x, cfg)
+    assert bool((out == bias).all()) and bool((stats[0, :, 0] == big).all())
+    dout, _ = rows(n, width, F32, g)
+    acc = torch.zeros(2, width, device=DEV)
+    stats[0, :, 1] = 1e6
+    dx = D.dedloc_norm_grad(dout, x, stats, cfg, acc[0], acc[1])
+    gy = R.f64(dout) * R.f64(gain)
+    want = 1e6 * (gy - gy.mean(1, keepdim=True))  # xhat = 0
+    assert float((R.f64(dx) - want).abs().max()) <= (R.K + 8) * R.U * float(want.abs().max() + 1e6 * gy.abs().max())
+    assert bool((acc[0] == 0).all())
+    # the branch's norm, then the sum's
+    h, _ = rows(n, width, F32, g)
+    total, out, st = D.dedloc_residual(h, x, post=cfg, pre=cfg)
+    assert torch.equal(total, h + bias)
+    assert bool(torch.isfinite(out).all()) and bool((st[1, :, 0] == big).all())
+    st[1, :, 1] = 1e6
+    dh, df = D.dedloc_residual_grad(total, x, st, dout, dout, post=cfg, pre=cfg)
+    assert bool(torch.isfinite(dh).all()) and bool(torch.isfinite(df).all())
