@@ -404,11 +404,14 @@ struct Team {
         sums(x, n.kind, mean, m2);
         if (__builtin_expect(!(m2 < 0x1p120f), 0)) {
             unit = kUnit;
-            eps *= kUnit;
-            eps *= kUnit;
 #pragma unroll
             for (int i = 0; i < V * E; i++) x[i] *= kUnit;
             sums(x, n.kind, mean, m2);
+            // eps counts in units of 2^192, if at all; of entries that are all equal there is nothing else
+            if (m2 == 0.0f)
+                unit = 1.0f;
+            else
+                eps = eps * kUnit * kUnit;
 #pragma unroll
             for (int i = 0; i < V * E; i++) x[i] *= 1.0f / kUnit;
             mean *= 1.0f / kUnit;

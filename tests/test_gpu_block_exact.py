@@ -105,3 +105,17 @@ def test_equal_entries_whose_mean_times_rstd_overflows(width):
     st[1, :, 1] = 1e6
     dh, df = D.dedloc_residual_grad(total, x, st, dout, dout, post=cfg, pre=cfg)
     assert bool(torch.isfinite(dh).all()) and bool(torch.isfinite(df).all())
+
+
+@pytest.mark.parametrize("width", [4, 32, 64, 512, 1024, 8192])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_equal_entries_whose_squares_leave_fp32(dtype, width):
+    """Rows of 2^126 have no squares in fp32 and no variance: eps alone makes their deviation, as for smaller entries."""
+    x = torch.full((3, width), 2.0 ** 126, device=DEV, dtype=dtype)
+    x[1] = -x[1]
+    bias = vector(width, gen(1), 0.0)
+    out, stats = D.dedloc_norm(x, D.norm_cfg(KINDS["layer"], None, bias, 1e-12))
+    assert bool((stats[0, :, 0] == x[:, 0].float()).all())
+    want = 1 / float(torch.tensor(1e-12)) ** 0.5
+    assert float((stats[0, :, 1].double() - want).abs().max()) <= 4 * R.U * want
+    assert torch.equal(out, bias.to(dtype).expand_as(out))
