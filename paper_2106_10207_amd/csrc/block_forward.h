@@ -97,7 +97,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
             for (int v = 0; v < V; v++) team.unpack(f[v], v, y + v * E);
             float2 st = make_float2(0.0f, 1.0f);
             if (MODE == 2 || (MODE == 3 && a.post.kind)) {
-                st = team.stats(y, a.post);
+                st = team.template stats<TB>(y, a.post);
                 if (a.stats && team.t == 0) a.stats[a.rows + at] = st;
             }
             if (!a.pre.kind) arrived();
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(MOST, resident(kForwardWaves, V, MODE, MOST)) void 
             }
         }
         if (!a.pre.kind) continue;
-        const float2 st = team.stats(x, a.pre);
+        const float2 st = team.template stats<TS>(x, a.pre);
         arrived();
         if (a.stats && team.t == 0) a.stats[at] = st;
 #pragma unroll

@@ -325,22 +325,29 @@ struct Team {
         }
         return n;
     }
-    // Both sums in all threads of the row.  In a wave the two are folded into the halves of one register first.
-    __device__ void sum2(float &a, float &b) const {
+    // Both sums over the lanes that share a row, in a whole wave folded into the halves of one register first: then the first is in the
+    // lower lanes of `a`, the second in the upper ones.
+    __device__ static void fold2(float &a, float &b) {
         if (T < 64) {
             a = lanes_sum<T>(a);
             b = lanes_sum<T>(b);
-            return;
+        } else {
+            const Pair p = swap32(a, b);
+            a = lanes_sum<32>(p.x + p.y);
         }
-        const Pair p = swap32(a, b);
-        const float s = lanes_sum<32>(p.x + p.y);
-        if (waves == 1) {
-            a = lane_of(s, 0);
-            b = lane_of(s, 32);
-            return;
-        }
+    }
+    __device__ static void unfold2(float &a, float &b) {
+        if (T < 64) return;
+        const Pair p = swap32(a, a);
+        a = p.x;
+        b = p.y;
+    }
+    // Both sums in all threads of the row.
+    __device__ void sum2(float &a, float &b) const {
+        fold2(a, b);
+        if (T < 64 || waves == 1) return unfold2(a, b);
         float4 *cell = meet->cell[turn];
-        if ((threadIdx.x & 31) == 0) ((float *)(cell + wave))[threadIdx.x >> 5 & 1] = s;
+        if ((threadIdx.x & 31) == 0) ((float *)(cell + wave))[threadIdx.x >> 5 & 1] = a;
         barrier();
         const float2 mine = *(const float2 *)(cell + (threadIdx.x & (MOST / 64 - 1)));
         a = waves_sum(mine.x);
@@ -353,40 +360,59 @@ struct Team {
         v += moved<0x4E>(v);
         return v + moved<0xB1>(v);
     }
-    // (mean, sum of squares about it) from the waves' own: no subtraction of large squares.
+    // From a first mean of n terms, the sum of their differences from it and that of the differences' squares: the mean, rounded
+    // once, what it lacks, and the squares about the two together.  What the first mean was off by (a rounded sum times
+    // a rounded 1 / n) is small whole steps of it, so where all terms are equal nothing here is rounded and m2 becomes zero.
+    __device__ static void centre(float n, float inv_n, float sum, float &mean, float &rest, float &m2) {
+        const float to = fmaf(sum, inv_n, mean), by = to - mean;
+        const float left = fmaf(-n, by, sum);  // the sum of differences from `to`
+        m2 = fmaf(-by, sum + left, m2);
+        rest = left * inv_n;
+        m2 = fmaf(-rest, left, m2);
+        m2 = m2 < 0.0f ? 0.0f : m2;  // NaN stays
+        mean = to;
+    }
+    // (mean, sum of squares about it) from the waves' own: no subtraction of large squares.  D: the type that the entries have been
+    // rounded to.  The mean of equal entries has to be that entry, or what it is off by stands beside eps as their variance.
+    // 16 bits: a wave's sum of equal entries is exact (11 bits, at most 1024 of them) and a quotient put right by its remainder is the entry;
+    // of other rows the sum is off by less than the steps between such entries.  fp32: put right by the sum of the differences.
+    template <typename D>
     __device__ void moments(const float *x, float &mean, float &m2) const {
-        float s = 0.0f;
+        float s = 0.0f, sum = 0.0f, rest = 0.0f;
 #pragma unroll
         for (int i = 0; i < V * E; i++) s += x[i];
         s = lanes_sum<T>(s);
         mean = s * inv_held;
-        m2 = lanes_sum<T>(squares(x, mean));
+        if (sizeof(D) == 2) mean = fmaf(fmaf(-here, mean, s), inv_held, mean);
+        m2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V * E; i++) {
+            const float d = x[i] - about(i / E, i % E, mean);
+            if (sizeof(D) == 4) sum += d;
+            m2 = fmaf(d, d, m2);
+        }
+        if (sizeof(D) == 4) {
+            fold2(sum, m2);
+            unfold2(sum, m2);
+            centre(here, inv_held, sum, mean, rest, m2);
+        } else {
+            m2 = lanes_sum<T>(m2);
+        }
         if (T < 64 || waves == 1) return;
         float4 *cell = meet->cell[turn];
-        if ((threadIdx.x & 63) == 0) cell[wave] = make_float4(mean, m2, here, 0.0f);
+        if ((threadIdx.x & 63) == 0) cell[wave] = make_float4(mean, m2, here, rest);
         barrier();
         const float4 mine = cell[threadIdx.x & (MOST / 64 - 1)];
         mean = waves_sum(mine.z * mine.x) * inv_width;
-        const float d = mine.x - mean;
+        const float d = mine.x - mean + mine.w;
+        sum = waves_sum(mine.z * d);
         m2 = waves_sum(fmaf(mine.z * d, d, mine.y));
+        centre((float)width, inv_width, sum, mean, rest, m2);
         turn ^= 1;
     }
-    __device__ float squares(const float *x, float about) const {
-        float q = 0.0f;
-#pragma unroll
-        for (int v = 0; v < V; v++)
-            pieces(v, [&](int p) {
-                const uint32_t c = column(v, p);
-#pragma unroll
-                for (int i = 0; i < P; i++) {
-                    const float d = x[v * E + p * P + i] - about;
-                    if (!RAGGED || c + i < width) q = fmaf(d, d, q);
-                }
-            });
-        return q;
-    }
+    template <typename D>
     __device__ void sums(const float *x, int kind, float &mean, float &m2) const {
-        if (kind == kNormLayer) return moments(x, mean, m2);
+        if (kind == kNormLayer) return moments<D>(x, mean, m2);
         mean = m2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < V * E; i++) m2 = fmaf(x[i], x[i], m2);  // zeros behind the row's end
@@ -398,15 +424,16 @@ struct Team {
     }
     // The statistics of a norm.  Sums of squares that leave fp32 (entries above 1e18) are taken again of x / 2^96: what that makes
     // too small to square is below 2^-50 of the sum.  Every thread of the row sees the same sum, so all take that way or none.
+    template <typename D>
     __device__ float2 stats(float *x, const NormArgs &n) const {
         constexpr float kUnit = 0x1p-96f;
         float mean, m2, eps = n.eps, unit = 1.0f;
-        sums(x, n.kind, mean, m2);
+        sums<D>(x, n.kind, mean, m2);
         if (__builtin_expect(!(m2 < 0x1p120f), 0)) {
             unit = kUnit;
 #pragma unroll
             for (int i = 0; i < V * E; i++) x[i] *= kUnit;
-            sums(x, n.kind, mean, m2);
+            sums<D>(x, n.kind, mean, m2);
             // eps counts in units of 2^192, if at all; of entries that are all equal there is nothing else
             if (m2 == 0.0f)
                 unit = 1.0f;

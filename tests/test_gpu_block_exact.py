@@ -119,3 +119,60 @@ def test_equal_entries_whose_squares_leave_fp32(dtype, width):
     want = 1 / float(torch.tensor(1e-12)) ** 0.5
     assert float((stats[0, :, 1].double() - want).abs().max()) <= 4 * R.U * want
     assert torch.equal(out, bias.to(dtype).expand_as(out))
+
+
+WIDTHS = [1, 5, 32, 48, 100, 300, 333, 520, 768, 1000, 2000, 2560, 4001, 5120, 9000, 12000, 16384]
+
+
+@pytest.mark.parametrize("types", PAIRS)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_equal_entries_give_the_bias(types, width):
+    """(x - mean) is zero: the mean is the entry, the deviation sqrt(eps), the output the bias, each to its last bit but for rstd's
+    (four roundings)."""
+    stream, branch = types
+    values = [1000.0, 15.9375, -3.140625, 2.5, 3 * 2.0 ** -20, 0.0]
+    values += [] if stream is F16 else [3e37, -1e35, 2.0 ** 126, 1e-30]
+    values += [1000.1, 1e4 / 3, 1e9 / 7] if stream is F32 else []
+    x = torch.tensor(values, device=DEV)[:, None].expand(-1, width).to(stream).contiguous()
+    for eps in (1e-12, 1e-5):
+        g = gen(width)
+        gain, bias = vector(width, g, 1.0), vector(width, g, 0.0)
+        out, stats = D.dedloc_norm(x, D.norm_cfg(KINDS["layer"], gain, bias, eps), out_dtype=branch)
+        assert torch.equal(stats[0, :, 0], x[:, 0].float())
+        want = 1 / float(torch.tensor(eps)) ** 0.5
+        assert float((stats[0, :, 1].double() - want).abs().max()) <= 4 * R.U * want
+        assert torch.equal(out, bias.to(branch).expand_as(out))
+
+
+def centred_stats(x, eps):
+    """(mean, rstd, bound of the mean, relative bound of rstd) where the sum of what entries differ from a first mean puts that right.
+
+    The first mean is off by at most a = (K + 2) U mean |x|.  The differences from it are exact to U, their mean is off by
+    (K + 4) U mean |d| with |d| <= |x - mean| + a; the corrected mean is rounded once.  What squares about the first mean exceed the
+    variance by is taken off from the same sums, so they are off by the roundings of sums of d^2 <= 2 (x - mean)^2 + 2 a^2: K + 8 of
+    the squares and 4 of what is taken off; waves that differ in their means count theirs once more: twice 2 (K + 12)."""
+    mean = x.mean(1, keepdim=True)
+    spread, a = (x - mean).abs().mean(1, keepdim=True), (R.K + 2) * R.U * x.abs().mean(1, keepdim=True)
+    var = (x - mean).square().mean(1, keepdim=True)
+    dvar = 4 * (R.K + 12) * R.U * (var + a ** 2)
+    dm = R.U * mean.abs() + (R.K + 6) * R.U * (spread + a)
+    return mean, 1 / (var + eps).sqrt(), R.SLACK * dm, R.SLACK * (dvar / (var + eps) / 2 + 4 * R.U)
+
+
+@pytest.mark.parametrize("width", WIDTHS[2:])
+def test_rows_far_from_zero(width):
+    """Rows whose mean is up to 2^22 deviations: the mean is the rounded one, the deviation that about the true mean."""
+    g = gen(width)
+    base = torch.tensor([1000.0, -777.7, 3e4, 16777.215, 0.0, 4e6], device=DEV)[:, None]
+    x = base.repeat(20, 1) + torch.randn(120, width, generator=g, device=DEV) * torch.tensor([0.01, 1.0], device=DEV).repeat(60)[:, None]
+    gain, bias = vector(width, g, 1.0), vector(width, g, 0.0)
+    out, stats = D.dedloc_norm(x, D.norm_cfg(KINDS["layer"], gain, bias, 1e-12))
+    eps = float(torch.tensor(1e-12))
+    mean, rstd, dm, dr = centred_stats(R.f64(x), eps)
+    got, got_r = R.f64(stats[0, :, :1]), R.f64(stats[0, :, 1:])
+    assert bool(((got - mean).abs() <= dm).all()), float(((got - mean).abs() / dm).max())
+    assert bool(((got_r - rstd).abs() <= dr * rstd).all()), float(((got_r / rstd - 1).abs() / dr).max())
+    y = (R.f64(x) - mean) * rstd * R.f64(gain) + R.f64(bias)
+    c = (R.f64(x) - mean).abs() * rstd
+    bound = R.SLACK * (R.f64(gain).abs() * (dm * rstd + c * (dr + 3 * R.U)) + 2 * R.U * y.abs())
+    assert bool(((R.f64(out) - y).abs() <= bound).all())
