@@ -176,3 +176,69 @@ def test_rows_far_from_zero(width):
     c = (R.f64(x) - mean).abs() * rstd
     bound = R.SLACK * (R.f64(gain).abs() * (dm * rstd + c * (dr + 3 * R.U)) + 2 * R.U * y.abs())
     assert bool(((R.f64(out) - y).abs() <= bound).all())
+
+
+# ------------------------------------------------------ sums of whole numbers
+
+def whole(n, width, dtype, g, most=2):
+    return torch.randint(-most, most + 1, (n, width), generator=g, device=DEV).to(dtype)
+
+
+def unit_stats(norms, n):
+    """(mean 0, rstd 1): the gradient takes the statistics that it is given, so every product is a whole number."""
+    st = torch.zeros(norms, n, 2, device=DEV)
+    st[..., 1] = 1
+    return st
+
+
+def same(got, want, what):
+    assert float(want.abs().max()) < 2 ** 24, what  # exact in fp32 in any order
+    assert torch.equal(got.double(), want), (what, int((got.double() != want).sum()))
+
+
+MANY = [(9001, 512), (9000, 64), (4097, 333), (2500, 2560), (1500, 5120), (300, 16384), ((100 << 20) // 2048 + 3, 1024),
+        ((100 << 20) // 5120 + 3, 2560)]
+
+
+@pytest.mark.parametrize("types", PAIRS)
+@pytest.mark.parametrize("n,width", MANY)
+def test_sums_of_a_norm_count_every_row_once(types, n, width):
+    g = gen(n)
+    stream, branch = types
+    x, dout = whole(n, width, stream, g), whole(n, width, branch, g)
+    for kind in ("layer", "rms"):
+        acc = torch.ones(2, width, device=DEV)
+        cfg = D.norm_cfg(KINDS[kind], torch.ones(width, device=DEV), torch.zeros(width, device=DEV), EPS[kind])
+        D.dedloc_norm_grad(dout, x, unit_stats(1, n), cfg, acc[0], acc[1], 4.0)
+        same(acc[0], 1 + 4 * (dout.double() * x.double()).sum(0), "dgain")
+        same(acc[1], 1 + 4 * dout.double().sum(0), "dbias")
+
+
+@pytest.mark.parametrize("gate", [None, "channel", 1, 7, 512, 1 << 20])
+@pytest.mark.parametrize("types", [(F32, BF16), (F32, F32), (BF16, BF16), (F16, F16)])
+@pytest.mark.parametrize("n,width", MANY)
+def test_sums_of_a_block_count_every_row_once(types, n, width, gate):
+    """Without a pre norm the sum's gradient is dsum itself: dw = 2 dsum, fhat = f, gates, gains and biases whole."""
+    g = gen(n + width)
+    stream, branch = types
+    f, dsum = whole(n, width, branch, g), whole(n, width, stream, g)
+    gain, bias = (whole(1, width, F32, g)[0] for _ in range(2))
+    gate_rows = gate if isinstance(gate, int) else 0
+    q = whole(1, width, F32, g)[0] if gate == "channel" else whole(-(-n // gate_rows), width, branch, g) if gate_rows else None
+    acc = torch.zeros(2, width, device=DEV)
+    dgate = torch.zeros(q.shape, device=DEV) if gate else None
+    dh, df = D.dedloc_residual_grad(None, f, unit_stats(2, n), dsum, None, beta=2.0, post=D.norm_cfg(KINDS["rms"], gain, bias, 1e-6), gate=q,
+                                    gate_rows=gate_rows, dgate=dgate, dpost=(acc[0], acc[1]))
+    assert torch.equal(dh, dsum)
+    dw, f = 2 * dsum.double(), f.double()
+    each = 1.0 if q is None else q.double().repeat_interleave(gate_rows, 0)[:n] if gate_rows else q.double()
+    same(acc[0], (dw * each * f).sum(0), "dgain")
+    same(acc[1], (dw * each).sum(0), "dbias")
+    if gate is None:
+        return
+    terms = dw * (gain.double() * f + bias.double())
+    if gate_rows:
+        want = torch.zeros(q.shape, dtype=torch.float64, device=DEV).index_add_(0, torch.arange(n, device=DEV) // gate_rows, terms)
+    else:
+        want = terms.sum(0)
+    same(dgate, want, "dgate")
