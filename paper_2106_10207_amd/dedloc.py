@@ -717,6 +717,13 @@ def _dtype(t, name: str) -> int:
         raise ValueError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}") from None
 
 
+def _word(v: int, name: str) -> int:
+    """v where the ABI has 32 bits for it: ctypes would take it modulo 2^32."""
+    if not 0 <= v < 1 << 32:
+        raise ValueError(f"{name}: expected a number of 32 bits, got {v}")
+    return v
+
+
 def _rows(t, name: str):
     """(address, row stride in elements, rows, columns) of a 2-D device tensor
     whose rows are contiguous."""
@@ -726,6 +733,7 @@ def _rows(t, name: str):
     if len(shape) != 2:
         raise ValueError(f"{name}: expected a matrix, got {len(shape)} dimensions")
     r, c = shape
+    _word(c, f"{name}'s width")
     sr, sc = t.stride()
     if c > 1 and sc != 1 or r > 1 and sr < c:
         raise ValueError(f"{name}: expected contiguous rows that do not overlap")
@@ -996,7 +1004,7 @@ def _first(t, name: str):
     """_rows of a call's first matrix, which must be on the current device: the
     call's stream is that device's."""
     shape = t.shape
-    if t.is_cuda and len(shape) == 2 and t.get_device() == _current_device()() and t.is_contiguous():
+    if t.is_cuda and len(shape) == 2 and shape[1] < 1 << 32 and t.get_device() == _current_device()() and t.is_contiguous():
         return t.data_ptr(), shape[1] or 1, shape[0], shape[1]
     got = _rows(t, name)
     if t.get_device() != _current_device()():
@@ -1063,7 +1071,7 @@ def make_residual_workspace(rows: int, width: int, gate_rows: int = 0, device="c
     """A workspace for dedloc_norm_grad and dedloc_residual_grad of up to these
     rows and this width."""
     import torch
-    need = load().dedloc_residual_workspace_bytes(rows, width, gate_rows)
+    need = load().dedloc_residual_workspace_bytes(rows, _word(width, "width"), _word(gate_rows, "gate_rows"))
     if need == 0:
         raise DedlocError(DEDLOC_ERR_INVALID_ARG, load().dedloc_last_error().decode())
     return torch.empty(need, dtype=torch.uint8, device=device)
@@ -1098,6 +1106,7 @@ class _Block:
 
     def __init__(self, like, branch, alpha, beta, post, pre, gate, gate_rows, drop):
         rows, width = like.shape
+        _word(gate_rows, "gate_rows")
         none, post, pre = dedloc_norm_cfg(DEDLOC_NORM_NONE, 0.0, None, None), _norm(post), _norm(pre)
         self.cfg = dedloc_residual_cfg(alpha, beta, post or none, pre or none, None, 0, gate_rows,
                                        drop or dedloc_dropout_cfg(0.0, 0, 0, 0, 0, None))
