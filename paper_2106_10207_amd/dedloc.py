@@ -109,12 +109,13 @@ DEDLOC_NORM_MAX_WIDTH = 16384
 
 
 class dedloc_dropout_cfg(ctypes.Structure):
+    _device = None  # of step_at, where dropout_cfg was given one
     _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("step", ctypes.c_uint32), ("row0", ctypes.c_uint32),
                 ("seed", ctypes.c_uint64), ("step_at", ctypes.c_void_p)]
 
 
 class dedloc_norm_cfg(ctypes.Structure):
-    _width = None  # of the vectors, where norm_cfg was given any
+    _width = _device = None  # of the vectors, where norm_cfg was given any
     _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("gain", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
 
 
@@ -336,6 +337,16 @@ def _current_stream():
         return lambda: torch.cuda.current_stream().cuda_stream
     # without the Stream object that current_stream() builds (2.5 us a call)
     return lambda: raw(device())
+
+
+@functools.lru_cache(maxsize=None)
+def _stream_of():
+    """A function returning a device's current stream handle."""
+    import torch
+    try:
+        return torch._C._cuda_getCurrentRawStream
+    except AttributeError:
+        return lambda device: torch.cuda.current_stream(device).cuda_stream
 
 
 def _stream(stream=None) -> Optional[int]:
@@ -956,16 +967,24 @@ def dropout_cfg(p: float, seed: int = 0, site: int = 0, step: int = 0, row0: int
         if step_at.dtype is not torch.int64 or step_at.numel() != 1:
             raise ValueError(f"step_at: expected one int64, got {tuple(step_at.shape)} of {step_at.dtype}")
         cfg.step_at = _dev(step_at, name="step_at")
-        cfg._keep = step_at
+        cfg._keep, cfg._device = step_at, step_at.get_device()
     return cfg
 
 
-def _vector(t, name: str, width: Optional[int] = None):
+def _on(got: Optional[int], device: Optional[int], name: str):
+    """What a call reads and writes beside its first matrix has to be on that one's device (None: nothing, or any)."""
+    if got != device and got is not None and device is not None:
+        raise ValueError(f"{name}: on device {got}, expected {device}")
+
+
+def _vector(t, name: str, width: Optional[int] = None, device: Optional[int] = None):
     """Device address of a contiguous fp32 vector (None passes as NULL)."""
     if t is None:
         return None
     if width is not None and t.numel() != width:
         raise ValueError(f"{name}: expected {width} elements, got {t.numel()}")
+    if device is not None and t.get_device() != device and t.is_cuda:  # of the host's, _dev speaks
+        _on(t.get_device(), device, name)
     return _dev(t, name=name, f32=True)
 
 
@@ -978,6 +997,10 @@ def norm_cfg(kind: int, gain=None, bias=None, eps: float = 1e-12) -> dedloc_norm
     if len(widths) > 1:
         raise ValueError(f"gain and bias differ in length: {sorted(widths)}")
     cfg._width = widths.pop() if widths else None
+    devices = {t.get_device() for t in cfg._keep if t is not None}
+    if len(devices) > 1:
+        raise ValueError(f"gain and bias are on devices {sorted(devices)}")
+    cfg._device = devices.pop() if devices else None
     return cfg
 
 
@@ -986,9 +1009,11 @@ def _norm(cfg):
     return None if cfg is None or cfg.kind == DEDLOC_NORM_NONE else cfg
 
 
-def _check_norm(cfg, width: int, name: str):
+def _check_norm(cfg, width: int, name: str, device: Optional[int] = None):
     if cfg._width is not None and cfg._width != width:
         raise ValueError(f"{name}: its vectors have {cfg._width} elements, the rows {width}")
+    if cfg._device is not None:
+        _on(cfg._device, device, name)
 
 
 @functools.lru_cache(maxsize=None)
@@ -1001,28 +1026,43 @@ def _current_device():
 
 
 def _first(t, name: str):
-    """_rows of a call's first matrix, which must be on the current device: the
-    call's stream is that device's."""
-    shape = t.shape
-    if t.is_cuda and len(shape) == 2 and shape[1] < 1 << 32 and t.get_device() == _current_device()() and t.is_contiguous():
-        return t.data_ptr(), shape[1] or 1, shape[0], shape[1]
+    """_rows of a call's first matrix, and its device, which must be the current
+    one: the call is launched there."""
+    if t.is_cuda:
+        device, shape = _current_device()(), t.shape
+        if t.get_device() == device and len(shape) == 2 and shape[1] < 1 << 32 and t.is_contiguous():  # the usual case
+            return t.data_ptr(), shape[1] or 1, shape[0], shape[1], device
     got = _rows(t, name)
-    if t.get_device() != _current_device()():
-        raise ValueError(f"{name}: on device {t.get_device()}, the current one is {_current_device()()}")
-    return got
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, the current one is {device}")
+    return *got, device
 
 
-def _same(t, like, name: str, dtype=None):
-    """(address, row stride) of a matrix of the shape and on the device of `like`
-    (None: NULL)."""
+def _stream_on(stream, device: int):
+    """_stream of a call whose matrices are on `device`, the current one."""
+    if stream is None:
+        return _stream_of()(device)
+    _on(stream.device_index, device, "stream")
+    return stream.cuda_stream
+
+
+def _stream_back_on(stream, device: int):
+    """The same for a call object, which may be called where another device is current."""
+    if _current_device()() != device:
+        raise ValueError(f"the call's matrices are on device {device}, the current one is {_current_device()()}")
+    return _stream_on(stream, device)
+
+
+def _same(t, like, device: int, name: str, dtype=None):
+    """(address, row stride) of a matrix of the shape of `like`, on the device that
+    that one is on (None: NULL)."""
     if t is None:
         return None, 0
     shape = like.shape
-    if t.is_cuda and t.get_device() == like.get_device() and t.shape == shape and (dtype is None or t.dtype is dtype) and t.is_contiguous():
+    if t.is_cuda and t.get_device() == device and t.shape == shape and (dtype is None or t.dtype is dtype) and t.is_contiguous():
         return t.data_ptr(), shape[1] or 1  # the usual case, without what takes a microsecond more
     p, ld, r, c = _rows(t, name)
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name}: on device {t.get_device()}, expected {like.get_device()}")
+    _on(t.get_device(), device, name)
     if t.shape != like.shape:
         raise ValueError(f"{name}: expected {tuple(like.shape)}, got {tuple(t.shape)}")
     if dtype is not None and t.dtype is not dtype:
@@ -1030,30 +1070,36 @@ def _same(t, like, name: str, dtype=None):
     return p, ld
 
 
-def _stats(t, norms: int, rows: int):
-    if t is not None and t.numel() < 2 * norms * rows:
+def _stats(t, norms: int, rows: int, device: int):
+    if t is None:
+        return None
+    if t.numel() < 2 * norms * rows:
         raise ValueError(f"stats: expected (mean, rstd) of {rows} rows for {norms} norm(s), got {t.numel()} values")
+    if t.get_device() != device and t.is_cuda:
+        _on(t.get_device(), device, "stats")
     return _dev(t, name="stats", f32=True)
 
 
 def dedloc_dropout(x, cfg: dedloc_dropout_cfg, out=None, stream=None):
     """The rows of x with the mask that cfg names; out may be x.  The gradient is
     the same call on the output's gradient."""
-    p, ld, rows, width = _first(x, "x")
+    p, ld, rows, width, device = _first(x, "x")
+    if cfg._device is not None:
+        _on(cfg._device, device, "step_at")
     if out is None:
         import torch
         with _allocating_on(stream):
             out = torch.empty(rows, width, dtype=x.dtype, device=x.device)
-    op, ol = _same(out, x, "out", x.dtype)
-    _check(load().dedloc_dropout(cfg, rows, width, _dtype(x, "x"), p, ld, op, ol, _stream(stream)))
+    op, ol = _same(out, x, device, "out", x.dtype)
+    _check(load().dedloc_dropout(cfg, rows, width, _dtype(x, "x"), p, ld, op, ol, _stream_on(stream, device)))
     return out
 
 
 def dedloc_norm(x, norm: dedloc_norm_cfg, out=None, out_dtype=None, stats=None, keep_stats: bool = True, stream=None):
     """(norm of the rows of x, stats): stats [1, rows, 2] hold (mean, rstd) for
     dedloc_norm_grad; keep_stats False: None, not written."""
-    p, ld, rows, width = _first(x, "x")
-    _check_norm(norm, width, "norm")
+    p, ld, rows, width, device = _first(x, "x")
+    _check_norm(norm, width, "norm", device)
     if out is None or (stats is None and keep_stats):
         import torch
         with _allocating_on(stream):
@@ -1061,9 +1107,9 @@ def dedloc_norm(x, norm: dedloc_norm_cfg, out=None, out_dtype=None, stats=None, 
                 out = torch.empty(rows, width, dtype=out_dtype or x.dtype, device=x.device)
             if stats is None and keep_stats:
                 stats = torch.empty(1, rows, 2, device=x.device)
-    op, ol = _same(out, x, "out")
-    _check(load().dedloc_norm(norm, rows, width, _dtype(x, "x"), _dtype(out, "out"), p, ld, op, ol, _stats(stats, 1, rows),
-                              _stream(stream)))
+    op, ol = _same(out, x, device, "out")
+    _check(load().dedloc_norm(norm, rows, width, _dtype(x, "x"), _dtype(out, "out"), p, ld, op, ol,
+                              _stats(stats, 1, rows, device), _stream_on(stream, device)))
     return out, stats
 
 
@@ -1081,8 +1127,8 @@ def dedloc_norm_grad(dout, x, stats, norm: dedloc_norm_cfg, dgain=None, dbias=No
                      dx=None, ws=None, stream=None):
     """The gradient of dedloc_norm's x (plus `add`); dgain and dbias, fp32
     accumulators, take batch_samples times theirs.  Returns dx."""
-    p, ld, rows, width = _first(x, "x")
-    _check_norm(norm, width, "norm")
+    p, ld, rows, width, device = _first(x, "x")
+    _check_norm(norm, width, "norm", device)
     if dx is None or (ws is None and (dgain is not None or dbias is not None)):
         import torch
         with _allocating_on(stream):
@@ -1090,13 +1136,15 @@ def dedloc_norm_grad(dout, x, stats, norm: dedloc_norm_cfg, dgain=None, dbias=No
                 dx = torch.empty(rows, width, dtype=x.dtype, device=x.device)
             if ws is None and (dgain is not None or dbias is not None):
                 ws = make_residual_workspace(rows, width, 0, x.device)
-    (yp, yl), (ap, al), (dp, dl) = _same(dout, x, "dout"), _same(add, x, "add", x.dtype), _same(dx, x, "dx", x.dtype)
+    (yp, yl), (ap, al), (dp, dl) = _same(dout, x, device, "dout"), _same(add, x, device, "add", x.dtype), _same(dx, x, device, "dx", x.dtype)
     if stats is None:
         raise ValueError("stats: the forward call's are needed")
+    if ws is not None and ws.get_device() != device:
+        _on(ws.get_device(), device, "ws")
     _check(load().dedloc_norm_grad(norm, rows, width, _dtype(x, "x"), _dtype(dout, "dout"), yp, yl, p, ld,
-                                   _stats(stats, 1, rows), ap, al, dp, dl, _vector(dgain, "dgain", width),
-                                   _vector(dbias, "dbias", width), batch_samples, _dev(ws, name="ws"),
-                                   0 if ws is None else _nbytes(ws), _stream(stream)))
+                                   _stats(stats, 1, rows, device), ap, al, dp, dl, _vector(dgain, "dgain", width, device),
+                                   _vector(dbias, "dbias", width, device), batch_samples, _dev(ws, name="ws"),
+                                   0 if ws is None else _nbytes(ws), _stream_on(stream, device)))
     return dx
 
 
@@ -1111,18 +1159,21 @@ class _Block:
         self.cfg = dedloc_residual_cfg(alpha, beta, post or none, pre or none, None, 0, gate_rows,
                                        drop or dedloc_dropout_cfg(0.0, 0, 0, 0, 0, None))
         self.norms = 2 if post is not None else 1 if pre is not None else 0
-        self.gate_shape = None
+        self.gate_shape, device = None, like.get_device()
         for n, name in ((post, "post"), (pre, "pre")):
             if n is not None:
-                _check_norm(n, width, name)
+                _check_norm(n, width, name, device)
+        if drop is not None:
+            _on(drop._device, device, "step_at")
         if gate is not None and gate_rows:
             self.gate_shape = (-(-rows // gate_rows), width)
             p, ld, r, c = _rows(gate, "gate")
             if (r, c) != self.gate_shape or gate.dtype is not branch.dtype:
                 raise ValueError(f"gate: expected {self.gate_shape} of {branch.dtype}, got {tuple(gate.shape)} of {gate.dtype}")
+            _on(gate.get_device(), device, "gate")
             self.cfg.gate, self.cfg.ld_gate = p, ld
         else:
-            self.cfg.gate = _vector(gate, "gate", width)
+            self.cfg.gate = _vector(gate, "gate", width, device)
         self.keep = post, pre, gate, drop
 
 
@@ -1136,19 +1187,19 @@ class ResidualCall:
 
     def __init__(self, h, f, sum=None, out=None, stats=None, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None,
                  gate=None, gate_rows: int = 0, drop=None):
-        p, ld, rows, width = _first(h, "h")
-        (fp, fl), (sp, sl) = _same(f, h, "f"), _same(sum, h, "sum", h.dtype)
-        op, ol = _same(out, h, "out", f.dtype)
+        p, ld, rows, width, self.device = _first(h, "h")
+        (fp, fl), (sp, sl) = _same(f, h, self.device, "f"), _same(sum, h, self.device, "sum", h.dtype)
+        op, ol = _same(out, h, self.device, "out", f.dtype)
         self._block = _Block(h, f, alpha, beta, post, pre, gate, gate_rows, drop)
         self.cfg = self._block.cfg
         self._keep = h, f, stats
         self.sum, self.out, self.stats = sum, out, stats
         self.args = (ctypes.byref(self.cfg), rows, width, _dtype(h, "h"), _dtype(f, "f"), p, ld, fp, fl, sp, sl, op, ol,
-                     _stats(stats, self._block.norms, rows))
+                     _stats(stats, self._block.norms, rows, self.device))
 
     def __call__(self, stream=None):
         """(sum, out, stats)"""
-        _check(load().dedloc_residual(*self.args, _stream(stream)))
+        _check(load().dedloc_residual(*self.args, _stream_back_on(stream, self.device)))
         return self.sum, self.out, self.stats
 
 
@@ -1178,35 +1229,38 @@ class ResidualGradCall:
 
     def __init__(self, sum, f, stats, dsum, dout, dh, df, alpha: float = 1.0, beta: float = 1.0, post=None, pre=None, gate=None,
                  gate_rows: int = 0, drop=None, dgate=None, dpre=None, dpost=None, batch_samples: float = 1.0, ws=None):
-        _, _, rows, width = _first(dh, "dh")
+        _, _, rows, width, index = _first(dh, "dh")
         self._block = _Block(dh, df, alpha, beta, post, pre, gate, gate_rows, drop)
         self.cfg = self._block.cfg
         g = self.grads = dedloc_residual_grads()
         for name, t, dtype in (("sum", sum, dh.dtype), ("f", f, df.dtype), ("dsum", dsum, dh.dtype), ("dout", dout, df.dtype),
                                ("dh", dh, dh.dtype), ("df", df, df.dtype)):
-            p, ld = _same(t, dh, name, dtype)
+            p, ld = _same(t, dh, index, name, dtype)
             setattr(g, name, p)
             setattr(g, "ld_" + name, ld)
-        g.stats = _stats(stats, self._block.norms, rows)
+        g.stats = _stats(stats, self._block.norms, rows, index)
         if dgate is not None and self._block.gate_shape:
+            _on(dgate.get_device(), index, "dgate")
             g.dgate, g.ld_dgate, r, c = _rows(dgate, "dgate")
             if (r, c) != self._block.gate_shape or dgate.dtype is not _float32():
                 raise ValueError(f"dgate: expected {self._block.gate_shape} of float32, got {tuple(dgate.shape)} of {dgate.dtype}")
         else:
-            g.dgate = _vector(dgate, "dgate", width)
+            g.dgate = _vector(dgate, "dgate", width, index)
         for name, pair in (("dpre", dpre), ("dpost", dpost)):
             for what, t in zip(("gain", "bias"), pair or (None, None)):
-                setattr(g, f"{name}_{what}", _vector(t, f"{name}'s {what}", width))
+                setattr(g, f"{name}_{what}", _vector(t, f"{name}'s {what}", width, index))
+        if ws is not None:
+            _on(ws.get_device(), index, "ws")
         self._keep = sum, f, stats, dsum, dout, dgate, dpre, dpost
         self.dh, self.df = dh, df
-        device = dh.device
+        device, self.device = dh.device, index
         self._ws = _Workspaces(ws, lambda: make_residual_workspace(rows, width, gate_rows, device))
         self.ws = self._ws.first
         self.args = ctypes.byref(self.cfg), rows, width, _dtype(dh, "dh"), _dtype(df, "df"), ctypes.byref(g), batch_samples
 
     def __call__(self, stream=None):
         """(dh, df)"""
-        handle = _stream(stream)
+        handle = _stream_back_on(stream, self.device)
         _check(load().dedloc_residual_grad(*self.args, *self._ws.on(stream, handle), handle))
         return self.dh, self.df
 

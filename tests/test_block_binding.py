@@ -68,3 +68,71 @@ def test_widths_are_numbers_of_32_bits(width):
                  lambda: D.make_residual_workspace(4, width, device="cpu")):
         with pytest.raises(ValueError, match="width.*32 bits"):
             call()
+
+
+def elsewhere(*shape, dtype=torch.float32):
+    return Matrix(*shape, dtype=dtype, device=1)
+
+
+def here(*shape, dtype=torch.float32):
+    return Matrix(*shape, dtype=dtype)
+
+
+RMS = D.DEDLOC_NORM_RMS
+AWAY = "on device 1, expected 0"
+
+
+def test_vectors_of_another_device():
+    """What a call reads and writes beside its matrices, each on another GPU: refused, by its name."""
+    x, v, st = here(4, 8), here(8), here(2, 4, 2)
+    norm, drop = D.norm_cfg(RMS, v, v), D.dropout_cfg(0.1)
+    far_norm, far_drop = D.norm_cfg(RMS, elsewhere(8), elsewhere(8)), D.dropout_cfg(0.1, step_at=elsewhere(1, dtype=torch.int64))
+    with pytest.raises(ValueError, match="gain and bias are on devices"):
+        D.norm_cfg(RMS, v, elsewhere(8))
+
+    def block(**more):
+        return lambda: D.ResidualCall(x, x, **{**dict(sum=x, out=x, stats=st, pre=norm), **more})
+
+    def grad(**more):
+        kw = {**dict(sum=x, f=x, stats=st, dsum=x, dout=x, dh=x, df=x, pre=norm, ws=here(1 << 20, dtype=torch.uint8)), **more}
+        return lambda: D.ResidualGradCall(**kw)
+
+    def norm_grad(stats=st, dgain=v, dbias=v, ws=here(1 << 20, dtype=torch.uint8), cfg=norm):
+        return lambda: D.dedloc_norm_grad(x, x, stats, cfg, dgain, dbias, dx=x, ws=ws)
+
+    for name, call in (
+            ("step_at", lambda: D.dedloc_dropout(x, far_drop, out=x)),
+            ("norm", lambda: D.dedloc_norm(x, far_norm, out=x, keep_stats=False)),
+            ("stats", lambda: D.dedloc_norm(x, norm, out=x, stats=elsewhere(1, 4, 2))),
+            ("norm", norm_grad(cfg=far_norm)), ("stats", norm_grad(stats=elsewhere(1, 4, 2))), ("dgain", norm_grad(dgain=elsewhere(8))),
+            ("dbias", norm_grad(dbias=elsewhere(8))), ("ws", norm_grad(ws=elsewhere(1 << 20, dtype=torch.uint8))),
+            ("pre", block(pre=far_norm)), ("post", block(post=far_norm)), ("stats", block(stats=elsewhere(2, 4, 2))),
+            ("gate", block(gate=elsewhere(8))), ("gate", block(gate=elsewhere(1, 8), gate_rows=4)), ("step_at", block(drop=far_drop)),
+            ("pre", grad(pre=far_norm)), ("post", grad(post=far_norm)), ("stats", grad(stats=elsewhere(2, 4, 2))),
+            ("gate", grad(gate=elsewhere(8))), ("dgate", grad(gate=v, dgate=elsewhere(8))),
+            ("dgate", grad(gate=here(1, 8), gate_rows=4, dgate=elsewhere(1, 8))), ("step_at", grad(drop=far_drop)),
+            ("dpre's gain", grad(dpre=(elsewhere(8), v))), ("dpre's bias", grad(dpre=(v, elsewhere(8)))),
+            ("dpost's gain", grad(post=norm, dpost=(elsewhere(8), None))), ("ws", grad(ws=elsewhere(1 << 20, dtype=torch.uint8)))):
+        with pytest.raises(ValueError, match=f"^{name}: {AWAY}"):
+            call()
+
+
+def test_calls_from_another_device(monkeypatch):
+    """A call object whose matrices are not on the current device any more, and a stream of another one."""
+    x = here(4, 8)
+    calls = [D.ResidualCall(x, x, sum=x), D.ResidualGradCall(None, None, None, x, None, x, x, ws=here(1 << 20, dtype=torch.uint8))]
+
+    class Stream:
+        device_index, cuda_stream = 1, 0
+
+    for call in calls:
+        with pytest.raises(ValueError, match=f"stream: {AWAY}"):
+            call(Stream())
+    with pytest.raises(ValueError, match=f"stream: {AWAY}"):
+        D.dedloc_norm(x, D.norm_cfg(RMS), out=x, keep_stats=False, stream=Stream())
+    monkeypatch.setattr(D, "_current_device", lambda: lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="are on device 0, the current one is 1"):
+            call()
+    with pytest.raises(ValueError, match="x: on device 0, the current one is 1"):
+        D.dedloc_norm(x, D.norm_cfg(RMS), out=x, keep_stats=False)
