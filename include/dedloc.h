@@ -533,8 +533,11 @@ int dedloc_dropout(const dedloc_dropout_cfg *cfg, uint64_t rows, uint32_t width,
  *   layer: mean = mean(x), rstd = 1 / sqrt(mean((x - mean)^2) + eps)
  *   rms:   mean = 0,       rstd = 1 / sqrt(mean(x^2) + eps)
  *   gain, bias  device fp32[width], nullable (1 and 0).
- * Statistics are sums in fp32 (in 64 bits where squares would leave it, entries
- * above 1e18), results are rounded once. */
+ * Statistics are sums in fp32, of the entries and of their squares (about the mean
+ * for a layer norm, whose mean is put right by what the entries differ from it: that
+ * of equal entries is the entry).  Where the squares' sum reaches 2^120 or is not
+ * finite the sums are taken again of x / 2^96.  Results are rounded once.  Entries
+ * above 2^126 in magnitude may differ from their mean by more than fp32 holds. */
 enum { DEDLOC_NORM_NONE = 0, DEDLOC_NORM_LAYER = 1, DEDLOC_NORM_RMS = 2 };
 typedef struct {
     int32_t kind;
@@ -590,11 +593,12 @@ int dedloc_norm_grad(const dedloc_norm_cfg *cfg, uint64_t rows, uint32_t width, 
  *   sum = alpha * h + beta * dropout(w),       rounded to the stream's type
  *   out = pre(sum)                             (none without a pre norm)
  * post is the norm behind the block, pre the one before the next block; a kind
- * of DEDLOC_NORM_NONE leaves a norm out.  LayerNorm(h + dropout(f)) has
+ * of DEDLOC_NORM_NONE leaves a norm out, its vectors with it.  LayerNorm(h + dropout(f)) has
  * no post norm and takes out as the next stream.
  *   gate   device, nullable.  gate_rows = 0: fp32[width], learned, the same for
  *          all rows.  gate_rows > 0: row i is scaled by row i / gate_rows of a
- *          matrix of the branch's type, ceil(rows / gate_rows) rows of width,
+ *          matrix of the branch's type, ceil(rows / gate_rows) rows of width (one
+ *          if gate_rows is more than the rows),
  *          ld_gate apart (what a layer made of each sequence);
  *   drop   as for dedloc_dropout; p = 0: none. */
 typedef struct {

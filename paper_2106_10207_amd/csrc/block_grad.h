@@ -16,7 +16,9 @@ namespace dedloc {
 // Rows are taken as in the forward pass.  Bound by memory, with vector instructions in half of the cycles: 65536 x 2048 bf16 with
 // two norms, a gate and dropout 304 us, 5.3 TB/s; 65536 x 1024 with one norm and dropout 123 with the join, 5.4 TB/s; an fp32 stream
 // of 65536 x 2048 445, 5.4 TB/s; 262144 x 64 bf16 18 us.  8192 x 1024 fp16 15 us: four rows a team.  Past 8192 columns two vectors
-// do not fit 128 registers: 8192 x 16384 462 us, 2.9 TB/s.
+// do not fit 128 registers, up to 764 bytes a thread lie in scratch: 8192 x 16384 bf16 with one norm 419 us, 2.6 TB/s, with two
+// and a gate 1003.  Gates of groups do not fit their 168 registers either (12 to 80 bytes of scratch in 16 bits, 80 to 232 in fp32): 65536 x 1024
+// with a gate per 512 rows 197 to 204 us, 4.0 TB/s.
 template <typename TS, typename TB, int T, int V, int MOST, int MODE, bool STREAM, bool RAGGED>
 __global__ __launch_bounds__(MOST, resident(kGradWaves, V, MODE, MOST)) void residual_grad_kernel(ResidualGradArgs a, uint32_t waves,
                                                                                                   uint32_t all) {

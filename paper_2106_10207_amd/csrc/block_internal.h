@@ -107,7 +107,10 @@ inline RowShape row_shape(uint32_t width, uint32_t columns) {
     const uint32_t few = (width + columns - 1) / columns, waves = few < 16 ? few : 16;
     return {64 * waves, waves * 512 < width ? 2u : 1u, waves == 1 ? 256 : 64 * waves};
 }
-// Two vectors a thread take fewer meetings of waves and fewer sums over lanes for a row; their registers fit four waves at most.
+// Two vectors a thread take fewer meetings of waves and fewer sums over lanes for a row.  They are taken up to 4096 columns, four waves:
+// longer rows are compiled for 1024 threads and so for 128 registers, which hold one vector of the forward pass and of a norm's gradient
+// alone.  The other gradients of one vector, too, keep up to 68 bytes a thread in scratch, with the sums of a post norm or gate 40 to 232, with groups 208 to 356:
+// 32768 x 4096, fp32 stream, 770 us for 412 of its bytes at 5.87 TB/s; 16384 x 8192 bf16 371 for 275.
 // 65536 rows of 1024 bf16, one vector and two: residual 101 and 96 us, norm_grad 105 and 94, residual_grad 134 and 122 (8192 columns,
 // forward: 185 and 269).  What keeps most in registers stays at one: gates of groups (218 and 362), and fp32 streams with the sums of a
 // post norm (65536 x 2048: 468 and 525).
@@ -121,7 +124,10 @@ inline RowShape grad_shape(uint32_t width, int mode, bool f32) {
 // What a call works on decides the kernel: see the kernels' MODE.
 inline int forward_mode(const ResidualArgs &a) { return !a.f ? 0 : a.gate_rows ? 3 : a.post.kind ? 2 : 1; }
 inline int grad_mode(const ResidualGradArgs &a) { return !a.df ? 0 : a.gate_rows ? 3 : a.f ? 2 : 1; }
-// Waves of a SIMD that the kernels' registers leave room for, by mode and by vectors of a thread; a launch has as many workgroups as run at once.
+// Waves of a SIMD that the kernels' registers leave room for, by mode and by vectors of a thread.  A launch has that many waves in whole
+// workgroups: as many as run at once where a row takes a part of a wave or 1, 2, 4, 8 or 16 of them.  Other numbers of waves leave
+// some of a CU's places empty, which this does not count, and the workgroups that do not fit run after the others (gradients of 2560 columns bf16:
+// 682 workgroups, 512 at once): residual_grad with one norm 65536 x 2048 5.5 TB/s, 65536 x 2560 3.8; with two and a gate 5.1 and 4.3.
 constexpr int kForwardWaves[2][4] = {{6, 5, 4, 4}, {4, 3, 3, 2}}, kGradWaves[2][4] = {{4, 4, 3, 3}, {2, 2, 2, 2}};
 constexpr int resident(const int (&waves)[2][4], uint32_t vectors, int mode, uint32_t threads) {
     return threads > 256 ? 4 : waves[vectors - 1][mode];  // 1024 threads leave no less than four

@@ -16,10 +16,6 @@ template <typename T>
 struct Raw {
     T v[E];
 };
-template <int N, typename T>
-struct Unaligned {
-    T v[N];
-} __attribute__((packed, aligned(sizeof(T))));
 
 // N columns from c on of a row, read past the caches (STREAM) or through them.  RAGGED: where the
 // row's end cuts them, the row's last N instead, which align() puts in place once they have arrived; else all are there.
