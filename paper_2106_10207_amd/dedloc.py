@@ -1084,7 +1084,7 @@ def dedloc_dropout(x, cfg: dedloc_dropout_cfg, out=None, stream=None):
     """The rows of x with the mask that cfg names; out may be x.  The gradient is
     the same call on the output's gradient."""
     p, ld, rows, width, device = _first(x, "x")
-    if cfg._device is not None:
+    if cfg is not None and cfg._device is not None:
         _on(cfg._device, device, "step_at")
     if out is None:
         import torch

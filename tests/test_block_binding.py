@@ -117,6 +117,11 @@ def test_vectors_of_another_device():
             call()
 
 
+def test_a_dropout_without_its_cfg_is_the_librarys_to_refuse():
+    with pytest.raises(D.DedlocError, match="cfg"):
+        D.dedloc_dropout(here(4, 8), None, out=here(4, 8), stream=type("Stream", (), dict(device_index=0, cuda_stream=0)))
+
+
 def test_calls_from_another_device(monkeypatch):
     """A call object whose matrices are not on the current device any more, and a stream of another one."""
     x = here(4, 8)

@@ -196,7 +196,7 @@ def same(got, want, what):
     assert torch.equal(got.double(), want), (what, int((got.double() != want).sum()))
 
 
-MANY = [(9001, 512), (9000, 64), (4097, 333), (2500, 2560), (1500, 5120), (300, 16384), ((100 << 20) // 2048 + 3, 1024),
+MANY = [(9001, 512), (9000, 64), (4097, 333), (2500, 2560), (1500, 5120), (2000, 3000), (1400, 6144), (300, 16384), ((100 << 20) // 2048 + 3, 1024),
         ((100 << 20) // 5120 + 3, 2560)]
 
 
